@@ -35,7 +35,8 @@ sys.path.insert(0, ROOT)
 METRIC = "MSA useful TFLOP/s and % bf16 MFMA peak; µs/layer-call at Llama-8B shape"
 PEAK_BF16_TFLOPS = 2500.0   # MI355X dense bf16 MFMA
 PEAK_HBM_GBS = 8000.0       # MI355X HBM3E
-KERNEL_SOURCES = ["paper_2606_02964_amd/csrc/attn.hip", "paper_2606_02964_amd/csrc/msa_internal.h"]
+KERNEL_SOURCES = ["paper_2606_02964_amd/csrc/attn.hip", "paper_2606_02964_amd/csrc/attn_device.h",
+                  "paper_2606_02964_amd/csrc/msa_internal.h"]
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "msa_attn_llama8b_traffic.json")
 
 

@@ -8,7 +8,8 @@ fallback: importing this package without a built library raises.
 Functions carry the C names: ``msa_plan``, ``msa_plan_info``,
 ``msa_forward``, ``msa_kv_append``, ``msa_plan_destroy``,
 ``msa_last_error``, ``msa_plan_export``, ``msa_check_block_table``,
-``msa_forward_noalloc``.  Device buffers are passed as objects with a
+``msa_forward_noalloc``; those of ``tree.py`` and ``cache.py`` are re-exported.
+Device buffers are passed as objects with a
 ``data_ptr()`` method (e.g. torch tensors) or as integer addresses; streams
 as ``hipStream_t`` integers or objects with ``cuda_stream`` (torch streams).
 """
@@ -125,6 +126,16 @@ EXPORTED = ("msa_plan", "msa_plan_info", "msa_forward", "msa_kv_append", "msa_pl
             "msa_evictor_create", "msa_evictor_destroy", "msa_evictor_add", "msa_evictor_remove",
             "msa_evictor_evict", "msa_evictor_set_lambda", "msa_evictor_set_lifespan",
             "msa_evictor_size", "msa_evictor_log_weight", "msa_evictor_replay")
+
+
+
+def _bind(name, argtypes) -> None:
+    """Argument types of an entry point of msa_tree.h or msa_cache.h.  A build
+    of the host code alone (the host-sanitizer test's) lacks most of them."""
+    fn = getattr(_lib, name, None)
+    if fn is not None:
+        fn.restype, fn.argtypes = _i32, argtypes
+
 
 MSA_EVICTOR_LINEAR = 1
 EVICTOR_OP_ADD, EVICTOR_OP_REMOVE, EVICTOR_OP_EVICT, EVICTOR_OP_LIFESPAN = 0, 1, 2, 3
@@ -379,3 +390,8 @@ class Evictor:
         if st != MSA_OK:
             raise MsaError(st, f"op {failed.value}: {msa_last_error()}")
         return out
+
+
+# the entry points of msa_tree.h and msa_cache.h
+from .tree import *  # noqa: E402,F401,F403
+from .tree import EXPORTED_TREE  # noqa: E402,F401

@@ -13,20 +13,8 @@
 #include "errors.h"
 #include "forward.h"
 #include "msa_internal.h"
-#include "plan.h"
-
-struct msa_plan_s {
-  msa::HostPlan hp;
-  bool host_only = true;
-  int device = -1;
-  std::vector<char> staging;  // host image of the device buffer (kept alive for the async copy)
-  char* dev = nullptr;        // device buffer: row_pos | work | merge | append | heads
-  const int32_t* d_row_pos = nullptr;
-  const msa::WorkItem* d_work = nullptr;
-  const msa::WgHead* d_heads = nullptr;
-  const msa::MergeItem* d_merge = nullptr;
-  const msa::AppendItem* d_append = nullptr;
-};
+#include "msa_tree.h"
+#include "plan_handle.h"
 
 namespace {
 
@@ -45,9 +33,9 @@ bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p
 
 void msa::set_last_error(const std::string& msg) { g_last_error = msg; }
 
-msa_status msa::forward_impl(const char* who, msa_plan_t plan, const void* q, const void* k_cache,
-                        const void* v_cache, const int32_t* block_table, void* o, float* lse,
-                        void* workspace, size_t workspace_bytes, void* hip_stream) {
+msa_status msa::forward_params(const char* who, msa_plan_t plan, const void* q, const void* k_cache,
+                               const void* v_cache, const int32_t* block_table, void* o, float* lse,
+                               void* workspace, size_t workspace_bytes, AttnParams* out) {
   const std::string w(who);
   if (!plan) return set_error(MSA_ERR_INVALID_ARG, w + ": null plan");
   if (plan->host_only)
@@ -70,7 +58,8 @@ msa_status msa::forward_impl(const char* who, msa_plan_t plan, const void* q, co
     return set_error(MSA_ERR_INVALID_ARG, w + ": current device differs from the plan's device");
 
   const msa_shape& s = hp.shape;
-  msa::AttnParams p{};
+  msa::AttnParams& p = *out;
+  p = msa::AttnParams{};
   p.q = static_cast<const uint16_t*>(q);
   p.k = static_cast<const uint16_t*>(k_cache);
   p.v = static_cast<const uint16_t*>(v_cache);
@@ -98,10 +87,19 @@ msa_status msa::forward_impl(const char* who, msa_plan_t plan, const void* q, co
   p.slot_rows = hp.tile_rows;
   p.scale_log2 = s.scale * 1.4426950408889634f;
   p.precise = hp.precise_weights ? 1 : 0;
-  const int num_wg = hp.wg_ptr.empty() ? 0 : (int)hp.wg_ptr.size() - 1;
-  int rc = msa::launch_attn(p, s.head_dim, hp.item_rows, num_wg, hip_stream);
-  if (rc != 0) return set_error(MSA_ERR_DEVICE, std::string(w + ": attention launch failed: ") +
-                                                    hipGetErrorString((hipError_t)rc));
+  return MSA_OK;
+}
+
+msa_status msa::launched(const char* who, const char* what, int rc) {
+  if (rc == 0) return MSA_OK;
+  return set_error(MSA_ERR_DEVICE,
+                   std::string(who) + ": " + what + " launch failed: " + hipGetErrorString((hipError_t)rc));
+}
+
+msa_status msa::merge_splits(const char* who, msa_plan_t plan, void* o, float* lse, void* workspace,
+                             void* hip_stream) {
+  const msa::HostPlan& hp = plan->hp;
+  const msa_shape& s = hp.shape;
   if (!hp.merge.empty()) {
     msa::MergeParams m{};
     m.merge = plan->d_merge;
@@ -114,11 +112,20 @@ msa_status msa::forward_impl(const char* who, msa_plan_t plan, const void* q, co
     m.group = hp.group;
     m.tile_rows = hp.tile_rows;
     m.max_rows = hp.max_merge_rows;
-    rc = msa::launch_merge(m, s.head_dim, (int)hp.merge.size(), hip_stream);
-    if (rc != 0) return set_error(MSA_ERR_DEVICE, std::string(w + ": merge launch failed: ") +
-                                                      hipGetErrorString((hipError_t)rc));
+    return launched(who, "merge", msa::launch_merge(m, s.head_dim, (int)hp.merge.size(), hip_stream));
   }
   return MSA_OK;
+}
+
+msa_status msa::forward_impl(const char* who, msa_plan_t plan, const void* q, const void* k_cache,
+                             const void* v_cache, const int32_t* block_table, void* o, float* lse,
+                             void* workspace, size_t workspace_bytes, void* hip_stream) {
+  msa::AttnParams p;
+  msa_status st = forward_params(who, plan, q, k_cache, v_cache, block_table, o, lse, workspace, workspace_bytes, &p);
+  if (st != MSA_OK || plan->hp.work.empty()) return st;
+  const msa::HostPlan& hp = plan->hp;
+  st = launched(who, "attention", msa::launch_attn(p, hp.shape.head_dim, hp.item_rows, hp.num_workgroups(), hip_stream));
+  return st != MSA_OK ? st : merge_splits(who, plan, o, lse, workspace, hip_stream);
 }
 
 int64_t msa::plan_workspace_bytes(msa_plan_t plan) { return plan->hp.workspace_bytes; }
@@ -127,24 +134,30 @@ extern "C" {
 
 const char* msa_last_error(void) { return g_last_error.c_str(); }
 
-msa_status msa_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
-                    const int32_t* seg_start, const int32_t* seg_len, const msa_plan_opts* opts,
-                    void* hip_stream, msa_plan_t* out) {
-  if (!out) return set_error(MSA_ERR_INVALID_ARG, "msa_plan: out must be non-null");
+}  // extern "C"
+
+namespace {
+
+msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
+                     const int32_t* seg_start, const int32_t* seg_len, bool with_trees, const int32_t* seg_tree,
+                     const msa_plan_opts* opts, void* hip_stream, msa_plan_t* out) {
+  const std::string w(who);
+  if (!out) return set_error(MSA_ERR_INVALID_ARG, w + ": out must be non-null");
   *out = nullptr;
   msa_plan_s* plan = new (std::nothrow) msa_plan_s();
-  if (!plan) return set_error(MSA_ERR_OUT_OF_MEMORY, "msa_plan: host allocation failed");
+  if (!plan) return set_error(MSA_ERR_OUT_OF_MEMORY, w + ": host allocation failed");
   std::string err;
   msa_status st;
   try {
-    st = msa::build_plan(shape, seq_kv_len, seg_indptr, seg_start, seg_len, opts, &plan->hp, &err);
+    st = msa::build_plan(shape, seq_kv_len, seg_indptr, seg_start, seg_len, opts, with_trees, seg_tree,
+                         &plan->hp, &err);
   } catch (const std::bad_alloc&) {
     st = MSA_ERR_OUT_OF_MEMORY;
     err = "host allocation failed while planning";
   }
   if (st != MSA_OK) {
     delete plan;
-    return set_error(st, "msa_plan: " + err);
+    return set_error(st, w + ": " + err);
   }
   plan->host_only = opts && (opts->flags & MSA_PLAN_HOST_ONLY);
   if (!plan->host_only) {
@@ -158,17 +171,26 @@ msa_status msa_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int
     const size_t off_merge = off_work + align_up(n_work, 256);
     const size_t off_append = off_merge + align_up(n_merge, 256);
     const size_t off_heads = off_append + align_up(n_append, 256);
-    const size_t bytes = std::max<size_t>(off_heads + n_wg * sizeof(msa::WgHead), 256);
+    const size_t n_seq = hp.seq_row0.size() * sizeof(int32_t);
+    const size_t n_row_tree = hp.row_tree.size() * sizeof(msa::RowTree);
+    const size_t n_trees = hp.trees.size() * sizeof(msa::TreeSpan);
+    const size_t off_seq = off_heads + align_up(n_wg * sizeof(msa::WgHead), 256);
+    const size_t off_row_tree = off_seq + align_up(n_seq, 256);
+    const size_t off_trees = off_row_tree + align_up(n_row_tree, 256);
+    const size_t bytes = std::max<size_t>(off_trees + n_trees, 256);
     try {
       plan->staging.assign(bytes, 0);
     } catch (const std::bad_alloc&) {
       delete plan;
-      return set_error(MSA_ERR_OUT_OF_MEMORY, "msa_plan: host allocation failed");
+      return set_error(MSA_ERR_OUT_OF_MEMORY, w + ": host allocation failed");
     }
     if (n_row) std::memcpy(plan->staging.data(), hp.row_pos.data(), n_row);
     if (n_work) std::memcpy(plan->staging.data() + off_work, hp.work.data(), n_work);
     if (n_merge) std::memcpy(plan->staging.data() + off_merge, hp.merge.data(), n_merge);
     if (n_append) std::memcpy(plan->staging.data() + off_append, hp.append.data(), n_append);
+    if (n_seq) std::memcpy(plan->staging.data() + off_seq, hp.seq_row0.data(), n_seq);
+    if (n_row_tree) std::memcpy(plan->staging.data() + off_row_tree, hp.row_tree.data(), n_row_tree);
+    if (n_trees) std::memcpy(plan->staging.data() + off_trees, hp.trees.data(), n_trees);
     for (size_t i = 0; i < n_wg; ++i) {
       msa::WgHead h{};
       const int32_t first = hp.wg_ptr[i], end = hp.wg_ptr[i + 1];
@@ -180,13 +202,13 @@ msa_status msa_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int
     const hipError_t gd = hipGetDevice(&plan->device);
     if (gd != hipSuccess) {
       delete plan;
-      return set_error(MSA_ERR_DEVICE, std::string("msa_plan: hipGetDevice failed: ") + hipGetErrorString(gd));
+      return set_error(MSA_ERR_DEVICE, w + ": hipGetDevice failed: " + hipGetErrorString(gd));
     }
     void* dev = nullptr;
     if (hipMalloc(&dev, bytes) != hipSuccess) {
       (void)hipGetLastError();
       delete plan;
-      return set_error(MSA_ERR_OUT_OF_MEMORY, "msa_plan: hipMalloc of the plan buffer failed");
+      return set_error(MSA_ERR_OUT_OF_MEMORY, w + ": hipMalloc of the plan buffer failed");
     }
     plan->dev = static_cast<char*>(dev);
     if (hipMemcpyAsync(dev, plan->staging.data(), bytes, hipMemcpyHostToDevice,
@@ -194,15 +216,46 @@ msa_status msa_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int
       (void)hipGetLastError();
       (void)hipFree(dev);
       delete plan;
-      return set_error(MSA_ERR_DEVICE, "msa_plan: upload of the plan buffer failed");
+      return set_error(MSA_ERR_DEVICE, w + ": upload of the plan buffer failed");
     }
     plan->d_row_pos = reinterpret_cast<const int32_t*>(plan->dev);
     plan->d_work = reinterpret_cast<const msa::WorkItem*>(plan->dev + off_work);
     plan->d_merge = reinterpret_cast<const msa::MergeItem*>(plan->dev + off_merge);
     plan->d_heads = reinterpret_cast<const msa::WgHead*>(plan->dev + off_heads);
     plan->d_append = reinterpret_cast<const msa::AppendItem*>(plan->dev + off_append);
+    plan->d_seq_row0 = reinterpret_cast<const int32_t*>(plan->dev + off_seq);
+    if (with_trees) plan->d_row_tree = reinterpret_cast<const msa::RowTree*>(plan->dev + off_row_tree);
+    plan->d_trees = reinterpret_cast<const msa::TreeSpan*>(plan->dev + off_trees);
   }
   *out = plan;
+  return MSA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+msa_status msa_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
+                    const int32_t* seg_start, const int32_t* seg_len, const msa_plan_opts* opts,
+                    void* hip_stream, msa_plan_t* out) {
+  return make_plan("msa_plan", shape, seq_kv_len, seg_indptr, seg_start, seg_len, false, nullptr, opts, hip_stream,
+                   out);
+}
+
+msa_status msa_plan_tree(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
+                         const int32_t* seg_start, const int32_t* seg_len, const int32_t* seg_tree,
+                         const msa_plan_opts* opts, void* hip_stream, msa_plan_t* out) {
+  return make_plan("msa_plan_tree", shape, seq_kv_len, seg_indptr, seg_start, seg_len, true, seg_tree, opts,
+                   hip_stream, out);
+}
+
+msa_status msa_plan_tree_info(msa_plan_t plan, msa_tree_info_t* info) {
+  if (!plan || !info) return set_error(MSA_ERR_INVALID_ARG, "msa_plan_tree_info: null argument");
+  const msa::HostPlan& hp = plan->hp;
+  info->num_trees = (int64_t)hp.trees.size();
+  info->tree_rows = hp.tree_rows;
+  info->max_slots = hp.max_slots;
+  info->mask_words = (hp.max_slots + 63) / 64;
   return MSA_OK;
 }
 

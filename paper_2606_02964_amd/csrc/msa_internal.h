@@ -63,8 +63,23 @@ static_assert(sizeof(MergeItem) == 32, "MergeItem is exported as 8 int32");
 // divided by its own softmax sum), then lse [tile_rows] fp32 (natural log).
 inline int64_t slot_floats(int head_dim, int tile_rows) { return (int64_t)tile_rows * (head_dim + 1); }
 
+// What a row of a plan with trees sees besides its causal limit.
+struct RowTree {
+  int32_t start;     // first slot (position) of the row's tree; a causal row: its own position + 1
+  int32_t mask_row;  // the row's mask among the trees' rows; -1 for a causal row
+};
+
+// One tree of a plan: slots 0 .. n-1 at positions start .. of sequence seq.
+struct TreeSpan {
+  int32_t seq;
+  int32_t start;
+  int32_t row0;  // mask row (row among the trees' rows) of slot 0
+  int32_t n;
+};
+
 // Arguments of the attention kernel.
 struct AttnParams {
+  static constexpr bool kTree = false;
   const uint16_t* q;
   const uint16_t* k;
   const uint16_t* v;
@@ -85,6 +100,13 @@ struct AttnParams {
   int32_t slot_rows; // rows of a workspace slot
   float scale_log2;  // scale * log2(e)
   int32_t precise;   // nonzero: every step carries hi + lo weights (MSA_PLAN_PRECISE_WEIGHTS)
+};
+
+struct TreeAttnParams : AttnParams {
+  static constexpr bool kTree = true;
+  const RowTree* row_tree;  // [rows]
+  const uint64_t* mask;     // [tree rows][mask_stride]
+  int64_t mask_stride;      // words
 };
 
 struct MergeParams {

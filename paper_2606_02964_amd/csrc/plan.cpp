@@ -36,6 +36,8 @@
 //      workgroup past the mean load is cut there.
 #include "plan.h"
 
+#include "msa_tree.h"
+
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -93,7 +95,7 @@ struct Unit {
 
 msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
                       const int32_t* seg_start, const int32_t* seg_len, const msa_plan_opts* opts,
-                      HostPlan* out, std::string* err) {
+                      bool with_trees, const int32_t* seg_tree, HostPlan* out, std::string* err) {
   if (!shape || !out) return fail(err, MSA_ERR_INVALID_ARG, "shape and out must be non-null");
   const msa_shape& s = *shape;
   msa_plan_opts o{};
@@ -178,6 +180,12 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
       if (st + n > L)
         return fail(err, MSA_ERR_INVALID_ARG,
                     "segment " + std::to_string(k) + " extends past seq_kv_len");
+      if (with_trees && seg_tree && seg_tree[k] != 0 && seg_tree[k] != 1)
+        return fail(err, MSA_ERR_INVALID_ARG, "seg_tree[" + std::to_string(k) + "] is neither 0 nor 1");
+      if (with_trees && (!seg_tree || seg_tree[k]) && n > MSA_TREE_MAX_SLOTS)
+        return fail(err, MSA_ERR_UNSUPPORTED,
+                    "segment " + std::to_string(k) + " is a tree of more than " +
+                        std::to_string(MSA_TREE_MAX_SLOTS) + " slots");
       total += n;
       if (total >= ((int64_t)1 << 31)) return fail(err, MSA_ERR_INVALID_ARG, "total_q >= 2^31");
       prev_end = st + n;
@@ -194,6 +202,21 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
     for (int32_t b = 0; b < B; ++b)
       for (int32_t k = seg_indptr[b]; k < seg_indptr[b + 1]; ++k)
         for (int32_t t = 0; t < seg_len[k]; ++t) P.row_pos[(size_t)r++] = seg_start[k] + t;
+  }
+  P.seq_row0.assign(seq_row0.begin(), seq_row0.end());
+  P.has_trees = with_trees;
+  if (with_trees) {
+    P.row_tree.reserve((size_t)total);
+    for (int32_t b = 0; b < B; ++b)
+      for (int32_t k = seg_indptr[b]; k < seg_indptr[b + 1]; ++k) {
+        const bool tree = !seg_tree || seg_tree[k];
+        if (tree) {
+          P.trees.push_back(TreeSpan{b, seg_start[k], P.tree_rows, seg_len[k]});
+          P.max_slots = std::max(P.max_slots, seg_len[k]);
+        }
+        for (int32_t t = 0; t < seg_len[k]; ++t)
+          P.row_tree.push_back(tree ? RowTree{seg_start[k], P.tree_rows++} : RowTree{seg_start[k] + t + 1, -1});
+      }
   }
   // 2. tiles of up to `tt` consecutive tokens of one sequence, packed
   // across segment gaps while the keys masked for the earlier rows stay a

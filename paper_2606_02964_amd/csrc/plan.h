@@ -24,18 +24,26 @@ struct HostPlan {
   std::vector<int32_t> wg_ptr;    // [num_workgroups + 1]; workgroup i runs on XCD i % 8
   std::vector<MergeItem> merge;
   std::vector<AppendItem> append; // one per (segment, cache block) slice
+  std::vector<int32_t> seq_row0;  // [num_seqs + 1] first packed row of each sequence
+  bool has_trees = false;         // built by msa_plan_tree (it may hold no tree all the same)
+  std::vector<RowTree> row_tree;  // [total_q] if has_trees
+  std::vector<TreeSpan> trees;    // one per tree segment
+  int32_t tree_rows = 0;          // rows of all trees
+  int32_t max_slots = 0;          // rows of the largest one
   int64_t num_tiles = 0;          // tiles x kv heads before splitting
   int64_t max_splits = 1;
   int32_t max_merge_rows = 0;     // rows (tokens x G) of the largest split tile
   int64_t num_slots = 0;          // workspace partial slots
   int64_t workspace_bytes = 0;
+  int num_workgroups() const { return wg_ptr.empty() ? 0 : (int)wg_ptr.size() - 1; }
   double useful_flops = 0, tile_flops = 0, planned_bytes = 0, min_bytes = 0;
 };
 
 // Validates the inputs and fills *out.  On error returns the status and a
-// message in *err; *out is then unspecified.
+// message in *err; *out is then unspecified.  with_trees: a plan of
+// msa_plan_tree, seg_tree as there (null: every segment is a tree).
 msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
                       const int32_t* seg_start, const int32_t* seg_len, const msa_plan_opts* opts,
-                      HostPlan* out, std::string* err);
+                      bool with_trees, const int32_t* seg_tree, HostPlan* out, std::string* err);
 
 }  // namespace msa
