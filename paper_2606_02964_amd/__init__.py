@@ -395,3 +395,5 @@ class Evictor:
 # the entry points of msa_tree.h and msa_cache.h
 from .tree import *  # noqa: E402,F401,F403
 from .tree import EXPORTED_TREE  # noqa: E402,F401
+from .cache import *  # noqa: E402,F401,F403
+from .cache import EXPORTED_CACHE  # noqa: E402,F401

@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libmsa.so")
 SOURCES = ["plan.cpp", "api.cpp", "evictor.cpp", "attn.hip", "append.hip", "noalloc.hip",
-           "tree.hip", "verify.hip"]
+           "tree.hip", "verify.hip", "weights.hip", "select.hip", "compact.hip"]
 ARCH = "gfx950"
 
 

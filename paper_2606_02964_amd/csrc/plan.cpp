@@ -93,6 +93,30 @@ struct Unit {
 
 }  // namespace
 
+msa_status check_shape(const msa_shape& s, std::string* err) {
+  if (s.num_seqs < 0) return fail(err, MSA_ERR_INVALID_ARG, "num_seqs < 0");
+  if (s.num_q_heads < 1 || s.num_kv_heads < 1)
+    return fail(err, MSA_ERR_INVALID_ARG, "head counts must be >= 1");
+  if (s.num_q_heads % s.num_kv_heads != 0)
+    return fail(err, MSA_ERR_INVALID_ARG, "num_q_heads must be a multiple of num_kv_heads");
+  if (s.num_q_heads / s.num_kv_heads > kTileRowsWide) return fail(err, MSA_ERR_UNSUPPORTED, "num_q_heads / num_kv_heads > 256");
+  if (s.head_dim <= 0) return fail(err, MSA_ERR_INVALID_ARG, "head_dim <= 0");
+  if (s.head_dim != 64 && s.head_dim != 128)
+    return fail(err, MSA_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  if (s.block_size <= 0) return fail(err, MSA_ERR_INVALID_ARG, "block_size <= 0");
+  if (s.block_size != kBlockSize) return fail(err, MSA_ERR_UNSUPPORTED, "block_size must be 16");
+  if (s.max_blocks_per_seq < 0 || s.num_blocks < 0)
+    return fail(err, MSA_ERR_INVALID_ARG, "max_blocks_per_seq and num_blocks must be >= 0");
+  if (!std::isfinite(s.scale) || !(s.scale > 0.0f))
+    return fail(err, MSA_ERR_INVALID_ARG, "scale must be finite and > 0");
+  if (!aligned8(s.q_stride_tok) || !aligned8(s.q_stride_head) || !aligned8(s.o_stride_tok) ||
+      !aligned8(s.o_stride_head) || !aligned8(s.k_stride_block) || !aligned8(s.k_stride_head) ||
+      !aligned8(s.k_stride_tok) || !aligned8(s.v_stride_block) || !aligned8(s.v_stride_head) ||
+      !aligned8(s.v_stride_dim))
+    return fail(err, MSA_ERR_INVALID_ARG, "strides must be positive multiples of 8 elements");
+  return MSA_OK;
+}
+
 msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
                       const int32_t* seg_start, const int32_t* seg_len, const msa_plan_opts* opts,
                       bool with_trees, const int32_t* seg_tree, HostPlan* out, std::string* err) {
@@ -113,31 +137,15 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
       return fail(err, MSA_ERR_INVALID_ARG, "MSA_PLAN_TILE_ROWS_32, _128 and _256 are exclusive");
   }
 
-  if (s.num_seqs < 0) return fail(err, MSA_ERR_INVALID_ARG, "num_seqs < 0");
-  if (s.num_q_heads < 1 || s.num_kv_heads < 1)
-    return fail(err, MSA_ERR_INVALID_ARG, "head counts must be >= 1");
-  if (s.num_q_heads % s.num_kv_heads != 0)
-    return fail(err, MSA_ERR_INVALID_ARG, "num_q_heads must be a multiple of num_kv_heads");
+  {
+    const msa_status st = check_shape(s, err);
+    if (st != MSA_OK) return st;
+  }
   const int32_t G = s.num_q_heads / s.num_kv_heads;
-  if (G > kTileRowsWide) return fail(err, MSA_ERR_UNSUPPORTED, "num_q_heads / num_kv_heads > 256");
   if (G > kTileRowsNarrow && (o.flags & MSA_PLAN_TILE_ROWS_128))
     return fail(err, MSA_ERR_UNSUPPORTED, "128-row tiles need num_q_heads / num_kv_heads <= 128");
   if (G > kTileRowsDecode && (o.flags & MSA_PLAN_TILE_ROWS_32))
     return fail(err, MSA_ERR_UNSUPPORTED, "32-row tiles need num_q_heads / num_kv_heads <= 32");
-  if (s.head_dim <= 0) return fail(err, MSA_ERR_INVALID_ARG, "head_dim <= 0");
-  if (s.head_dim != 64 && s.head_dim != 128)
-    return fail(err, MSA_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
-  if (s.block_size <= 0) return fail(err, MSA_ERR_INVALID_ARG, "block_size <= 0");
-  if (s.block_size != kBlockSize) return fail(err, MSA_ERR_UNSUPPORTED, "block_size must be 16");
-  if (s.max_blocks_per_seq < 0 || s.num_blocks < 0)
-    return fail(err, MSA_ERR_INVALID_ARG, "max_blocks_per_seq and num_blocks must be >= 0");
-  if (!std::isfinite(s.scale) || !(s.scale > 0.0f))
-    return fail(err, MSA_ERR_INVALID_ARG, "scale must be finite and > 0");
-  if (!aligned8(s.q_stride_tok) || !aligned8(s.q_stride_head) || !aligned8(s.o_stride_tok) ||
-      !aligned8(s.o_stride_head) || !aligned8(s.k_stride_block) || !aligned8(s.k_stride_head) ||
-      !aligned8(s.k_stride_tok) || !aligned8(s.v_stride_block) || !aligned8(s.v_stride_head) ||
-      !aligned8(s.v_stride_dim))
-    return fail(err, MSA_ERR_INVALID_ARG, "strides must be positive multiples of 8 elements");
   if (o.q_tile_tokens < 0 || o.q_tile_tokens > kTileRowsWide / G)
     return fail(err, MSA_ERR_INVALID_ARG, "q_tile_tokens must be in [0, tile_rows / (Hq/Hkv)]");
   if (o.kv_split_tokens < 0 || o.kv_split_tokens % kKvStep != 0)

@@ -39,6 +39,9 @@ struct HostPlan {
   double useful_flops = 0, tile_flops = 0, planned_bytes = 0, min_bytes = 0;
 };
 
+// The checks of a shape alone; a message in *err where it is refused.
+msa_status check_shape(const msa_shape& shape, std::string* err);
+
 // Validates the inputs and fills *out.  On error returns the status and a
 // message in *err; *out is then unspecified.  with_trees: a plan of
 // msa_plan_tree, seg_tree as there (null: every segment is a tree).
