@@ -134,7 +134,7 @@ msa_status msa_tree_forward(msa_plan_t plan, const void *q, const void *k_cache,
  * equal results.
  *
  *   prob_type      MSA_PROB_F32, _BF16 or _F16: type of target and draft
- *   vocab          entries of a row, >= 1
+ *   vocab          entries of a row, 1 .. 2^31 - 2^16
  *   target         device [tree_rows][target_stride]: row t's probabilities of
  *                  the token that follows slot t
  *   draft          device [tree_rows][draft_stride]: row t's probabilities that

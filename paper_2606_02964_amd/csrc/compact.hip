@@ -4,13 +4,25 @@
 // Position base + i of a sequence takes the K and V of position base + index[i],
 // index strictly ascending, hence index[i] >= i: a source lies at or behind
 // its destination and, for a run of moves, behind every destination of the moves
-// before it.  One workgroup per (sequence, KV head, K or V) therefore goes through
-// the list in runs: it reads a run's sources into registers, and writes
-// them once every read of the run has arrived.  Runs need no further order: what a
-// run writes lies before everything later runs read.
-// A run is 64 moves.  K rows are copied in 16-byte pieces; the V of 8
-// consecutive destination tokens of a channel is one 16-byte piece of the cache,
-// gathered from 8 places and written whole where all 8 are moved to.
+// before it.  One workgroup per (sequence, KV head, 64 channels of K or of V)
+// therefore goes through the list in runs of 128 moves, in order: what a run writes
+// lies before everything that later runs read, so later runs' reads may be under way
+// already, and the only wait is for the run's own reads, of all waves, before
+// its writes (one barrier a run).
+// The places of the moves (index, then two block-table entries) are looked up four
+// runs ahead and the reads are issued two runs ahead, so that no run waits for a
+// chain of reads.
+//   K: rows of 128 bytes, in 16-byte pieces from register to register.
+//   V: a block holds the 16 tokens of a channel side by side, and kept tokens
+//   change their place in it.  The channel rows (32 bytes) of each source block
+//   are read once, whole, and its kept tokens go to their place in a staging
+//   buffer in LDS, from where full pieces of 8 tokens are written.  (Gathered
+//   token by token in 2-byte reads, half of 16 x 16K tokens, 8 heads, d = 128, took
+//   955 us; a 2-byte read of a wave touches 16 lines for 128 bytes.)
+// Lists of up to 64 entries (a tree's path) take one workgroup per (sequence, KV
+// head), which holds all of their K and V in LDS between reading and writing.
+// Bound by HBM: each moved byte is read and written once, and whole blocks of V are
+// read where half of their tokens stay.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -24,8 +36,12 @@
 namespace msa {
 namespace {
 
-constexpr int kRun = 64;
-constexpr int kCompactThreads = 256;
+constexpr int kRun = 128;  // moves of a run: two waves' lanes hold one each
+constexpr int kSlice = 64;   // channels of a workgroup
+constexpr int kCompactThreads = 512;
+constexpr int kRing = 5;     // runs whose places are held: the one written, three ahead, one that slow waves still write
+constexpr int kAhead = 3;    // V blocks of a run that a wave reads ahead
+constexpr int kShort = 64;   // entries of a list that one workgroup holds
 
 struct CompactParams {
   const int32_t* base;  // may be null
@@ -39,94 +55,323 @@ struct CompactParams {
   int32_t num_kv_heads, max_blocks, num_blocks, max_count;
 };
 
-// Where the elements of a run's moves lie in the cache; -1: no such move.
-struct RunPlaces {
-  int64_t src[kRun], dst[kRun];
+// Where a run's moves lead, as element offsets in the head's cache.
+struct PlacesK {
+  int64_t src[kRun];
+  int64_t dst[kRun];  // -1: no move
+};
+struct __attribute__((aligned(16))) PlacesV {
+  // the distinct source blocks of each 64 moves, in order
+  int64_t block[2][64];
+  // by block and token: the run's move that takes it, kNoMove for none
+  uint8_t slot[2][64][kBlockSize];
+  // by 8 neighbouring moves: where their piece lies, and which of its tokens are moved to
+  int64_t piece[kRun / 8];
+  uint8_t moved[kRun / 8];
+  int32_t blocks[2];
+};
+constexpr int kNoMove = kRun;  // a column of the staging buffer that is not written out
+
+// The list's positions, and where they are in the cache.
+struct Moves {
+  const int32_t* index;
+  const int32_t* table;
+  int64_t base, end, sb, st;
+  int n, lead, num_blocks;
+
+  // the move at entry i (of the list's entries shifted by lead): index[i], or -1
+  __device__ __forceinline__ int32_t from(int i) const { return i >= 0 && i < n ? index[i] : -1; }
+  __device__ __forceinline__ int32_t block_at(int64_t pos) const {
+    const int32_t blk = pos >= 0 && pos < end ? table[pos / kBlockSize] : -1;
+    return blk < num_blocks ? blk : -1;
+  }
 };
 
-// every wave's reads have arrived (the barrier alone would not wait for them)
-__device__ __forceinline__ void reads_arrived() { asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory"); }
+// What lane m of waves 0 and 1 knows of move m of a run on the way to its places.
+struct Lookup {
+  int32_t from = -1, src_blk = -1, dst_blk = -1;
+};
+
+__device__ __forceinline__ bool is_move(const Moves& mv, int i, const Lookup& l) {
+  return l.from > i && l.src_blk >= 0 && l.dst_blk >= 0;  // (a place kept where it is needs no move)
+}
+__device__ __forceinline__ void enter_places(PlacesK& at, const Moves& mv, int i, const Lookup& l) {
+  const int m = threadIdx.x;
+  const bool moves = is_move(mv, i, l);
+  const int src_tok = (int)((mv.base + l.from) & (kBlockSize - 1)), dst_tok = (int)((mv.base + i) & (kBlockSize - 1));
+  at.src[m] = moves ? l.src_blk * mv.sb + src_tok * mv.st : 0;  // (what is read where nothing moves is not used)
+  at.dst[m] = moves ? l.dst_blk * mv.sb + dst_tok * mv.st : -1;
+}
+__device__ __forceinline__ void enter_places(PlacesV& at, const Moves& mv, int i, const Lookup& l) {
+  const int m = threadIdx.x, lane = m & 63, half = m >> 6;
+  const bool moves = is_move(mv, i, l);
+  const int src_tok = (int)((mv.base + l.from) & (kBlockSize - 1)), dst_tok = (int)((mv.base + i) & (kBlockSize - 1));
+  const int32_t blk = moves ? l.src_blk : -1;
+  const int32_t below = __shfl_up(blk, 1);  // (by all lanes: one that does not take part would read as block 0)
+  const bool leads = moves && (lane == 0 || blk != below);
+  const uint64_t leaders = __ballot(leads), movers = __ballot(moves);
+  const int g = __popcll(leaders & (~0ull >> (63 - lane))) - 1, blocks = __popcll(leaders);
+  if (lane >= blocks) at.block[half][lane] = 0;
+  if (leads) {
+    at.block[half][g] = blk * mv.sb;
+    *reinterpret_cast<uint4*>(at.slot[half][g]) = make_uint4(0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u);
+  }
+  if (moves) at.slot[half][g][src_tok] = (uint8_t)m;  // (a wave's LDS writes stay in order)
+  if (lane % 8 == 0) {  // (runs start at block borders: dst_tok is 0 or 8)
+    at.piece[m / 8] = l.dst_blk * mv.sb + dst_tok;
+    at.moved[m / 8] = (uint8_t)(movers >> lane);
+  }
+  if (lane == 0) at.blocks[half] = blocks;
+}
+static_assert(kNoMove == 0x80, "the empty slot");
+
+// The lookups, by waves 0 and 1: each call enters one more run's places and issues
+// the reads of the runs behind it, which arrive until the next call.
+struct Lookups {
+  Lookup held;       // of run `next`
+  int32_t from = -1; // index entry, of run next + 1
+  int next = 0;
+  __device__ __forceinline__ int entry(const Moves& mv, int run) const { return run * kRun - mv.lead + (int)threadIdx.x; }
+  __device__ __forceinline__ void start(const Moves& mv) {
+    held.from = mv.from(entry(mv, 0));
+    from = mv.from(entry(mv, 1));
+    blocks(mv, 0);
+  }
+  __device__ __forceinline__ void blocks(const Moves& mv, int run) {
+    held.src_blk = held.from >= 0 ? mv.block_at(mv.base + held.from) : -1;
+    held.dst_blk = mv.block_at(mv.base + entry(mv, run));
+  }
+  template <class P>
+  __device__ __forceinline__ void step(const Moves& mv, P (&ring)[kRing], int runs) {
+    if (threadIdx.x >= kRun || next >= runs) return;
+    enter_places(ring[next % kRing], mv, entry(mv, next), held);
+    ++next;
+    held.from = from;
+    blocks(mv, next);
+    from = mv.from(entry(mv, next + 1));
+  }
+};
+
+// the barrier that follows each run's reads: LDS writes of every wave are done
+// (the reads have arrived: their registers were used before it)
+__device__ __forceinline__ void run_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ __forceinline__ void compact_k(uint16_t* cache, const Moves& mv, PlacesK (&ring)[kRing],
+                                          Lookups& look, int runs) {
+  constexpr int kPieces = kSlice / 8, kEach = kRun * kPieces / kCompactThreads;
+  const int tid = threadIdx.x;
+  uint4 x[2][kEach];
+  auto read = [&](uint4 (&y)[kEach], int r) __attribute__((always_inline)) {
+    const PlacesK& at = ring[r % kRing];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e)
+      y[e] = *reinterpret_cast<const uint4*>(cache + at.src[(e * kCompactThreads + tid) / kPieces] + tid % kPieces * 8);
+  };
+  auto step = [&](uint4 (&now)[kEach], int r) __attribute__((always_inline)) {
+    look.step(mv, ring, runs);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) asm volatile("" : "+v"(now[e].x), "+v"(now[e].y), "+v"(now[e].z), "+v"(now[e].w));
+    run_barrier();
+    const PlacesK& at = ring[r % kRing];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int64_t dst = at.dst[(e * kCompactThreads + tid) / kPieces];
+      if (dst >= 0) *reinterpret_cast<uint4*>(cache + dst + tid % kPieces * 8) = now[e];
+    }
+    read(now, min(r + 2, runs - 1));  // (unconditional, so that the wait for the run before it can leave it out)
+  };
+  read(x[0], 0);
+  read(x[1], min(1, runs - 1));
+  for (int r = 0; r < runs; r += 2) {
+    step(x[0], r);
+    if (r + 1 < runs) step(x[1], r + 1);
+  }
+}
+
+// Staged tokens of a run: [channel][move], rows of a multiple of 16 bytes, some
+// columns for what does not stay
+constexpr int kStagePitch = kRun + 8;
+
+__device__ __forceinline__ void compact_v(uint16_t* cache, int64_t v_sd, const Moves& mv, PlacesV (&ring)[kRing],
+                                          Lookups& look, uint16_t (&stage)[2][kSlice][kStagePitch], int runs) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = wave & 1, first_block = wave >> 1;  // four waves share a half run's blocks
+  // a lane holds 8 tokens of one channel, and of the channel 32 further on
+  const int c = lane >> 1, side = lane & 1;
+  const uint16_t* from = cache + c * v_sd + side * 8;
+  uint4 x[2][kAhead][2];
+  auto read_block = [&](uint4 (&y)[2], int64_t block) __attribute__((always_inline)) {
+    y[0] = *reinterpret_cast<const uint4*>(from + block);
+    y[1] = *reinterpret_cast<const uint4*>(from + block + 32 * v_sd);
+  };
+  auto read = [&](uint4 (&y)[kAhead][2], int r) __attribute__((always_inline)) {
+    const PlacesV& at = ring[r % kRing];
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a) read_block(y[a], at.block[half][first_block + 4 * a]);
+  };
+  auto step = [&](uint4 (&now)[kAhead][2], int r) __attribute__((always_inline)) {
+    const PlacesV& at = ring[r % kRing];
+    const int blocks = __builtin_amdgcn_readfirstlane(at.blocks[half]);
+    uint16_t(&to)[kSlice][kStagePitch] = stage[r & 1];
+    // each of a lane's tokens to the column of its move (most hold one), or to the spare one
+    auto put = [&](const uint4 a, const uint4 b, int g) __attribute__((always_inline)) {
+      const uint2 slot = *reinterpret_cast<const uint2*>(&at.slot[half][g][side * 8]);
+      const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int m = (int)((t < 4 ? slot.x : slot.y) >> (t % 4 * 8) & 0xff);
+        to[c][m] = (uint16_t)(wa[t / 2] >> (t % 2 * 16));
+        to[c + 32][m] = (uint16_t)(wb[t / 2] >> (t % 2 * 16));
+      }
+    };
+    look.step(mv, ring, runs);
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a)
+      if (first_block + 4 * a < blocks) put(now[a][0], now[a][1], first_block + 4 * a);
+    for (int g = first_block + 4 * kAhead; g < blocks; g += 4) {  // kept tokens far apart
+      uint4 y[2];
+      read_block(y, at.block[half][g]);
+      put(y[0], y[1], g);
+    }
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) asm volatile("" : "+v"(now[a][h].x), "+v"(now[a][h].y), "+v"(now[a][h].z), "+v"(now[a][h].w));
+    run_barrier();
+#pragma unroll
+    for (int e = 0; e < kSlice * (kRun / 8) / kCompactThreads; ++e) {
+      // 32 channels of one destination block a wave
+      const int unit = e * (kCompactThreads / 64) + wave;  // (block of the run, channel half)
+      const int piece = (unit >> 1) * 2 + side, ch = (unit & 1) * 32 + c;
+      const int moved = at.moved[piece];
+      if (moved == 0) continue;
+      const uint4 y = *reinterpret_cast<const uint4*>(&to[ch][piece * 8]);
+      uint16_t* dst = cache + at.piece[piece] + ch * v_sd;
+      if (moved == 0xff) {
+        *reinterpret_cast<uint4*>(dst) = y;
+      } else {
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if (moved >> t & 1) dst[t] = (uint16_t)(w[t / 2] >> (t % 2 * 16));
+      }
+    }
+    read(now, min(r + 2, runs - 1));  // (unconditional, so that the wait for the run before it can leave it out)
+  };
+  read(x[0], 0);
+  read(x[1], min(1, runs - 1));
+  for (int r = 0; r < runs; r += 2) {
+    step(x[0], r);
+    if (r + 1 < runs) step(x[1], r + 1);
+  }
+}
 
 template <int D>
-__global__ __launch_bounds__(kCompactThreads) void msa_kv_compact_kernel(CompactParams p) {
-  __shared__ RunPlaces at;
-  const int head = blockIdx.x % p.num_kv_heads, rest = blockIdx.x / p.num_kv_heads;
-  const bool is_v = rest & 1;
-  const int seq = rest >> 1, tid = threadIdx.x;
-  const int n = max(0, min(p.count[seq], p.max_count));
-  const int64_t base = p.base ? p.base[seq] : 0;
-  const int32_t* index = p.index + (int64_t)seq * p.i_sb + (int64_t)head * p.i_sh;
-  const int32_t* table = p.block_table + (int64_t)seq * p.max_blocks;
-  const int64_t end = (int64_t)p.max_blocks * kBlockSize;
-  uint16_t* cache = is_v ? p.v + (int64_t)head * p.v_sh : p.k + (int64_t)head * p.k_sh;
-  const int64_t sb = is_v ? p.v_sb : p.k_sb, st = is_v ? 1 : p.k_st;
-  auto place = [&](int64_t pos) -> int64_t {
-    if (pos < 0 || pos >= end) return -1;
-    const int32_t blk = table[pos / kBlockSize];
-    return blk < 0 || blk >= p.num_blocks ? -1 : blk * sb + pos % kBlockSize * st;
-  };
-  // runs end at multiples of 8 destination positions, so that V's 16-byte pieces lie in one run
-  const int lead = (int)((base % 8 + 8) % 8);
-  for (int i0 = -lead; i0 < n; i0 += kRun) {
-    if (tid < kRun) {
-      const int i = i0 + tid;
-      int64_t src = -1, dst = -1;
-      if (i >= 0 && i < n) {
-        const int64_t from = index[i];
-        if (from > i) {  // (a place kept where it is needs no move)
-          src = place(base + from);
-          dst = place(base + i);
-        }
-      }
-      at.src[tid] = src >= 0 && dst >= 0 ? src : -1;
-      at.dst[tid] = src >= 0 && dst >= 0 ? dst : -1;
-    }
+__global__ __launch_bounds__(kCompactThreads, 4) void msa_kv_compact_kernel(CompactParams p) {
+  __shared__ union {
+    PlacesK k[kRing];
+    PlacesV v[kRing];
+  } ring;
+  __shared__ __attribute__((aligned(16))) uint16_t stage[2][kSlice][kStagePitch];
+  constexpr int kParts = 2 * D / kSlice;  // K slices, then V slices
+  const int part = blockIdx.x % kParts, rest = blockIdx.x / kParts;
+  const int seq = rest / p.num_kv_heads, head = rest - seq * p.num_kv_heads, tid = threadIdx.x;
+  const bool is_v = part >= kParts / 2;
+  const int slice = is_v ? part - kParts / 2 : part;
+  Moves mv;
+  // (entries past the table's positions are no moves: index[i] >= i)
+  mv.end = (int64_t)p.max_blocks * kBlockSize;
+  mv.n = (int)max((int64_t)0, min(min((int64_t)p.count[seq], (int64_t)p.max_count), min(mv.end, (int64_t)0x7ffff000)));
+  if (mv.n == 0) return;
+  mv.base = p.base ? p.base[seq] : 0;
+  mv.index = p.index + (int64_t)seq * p.i_sb + (int64_t)head * p.i_sh;
+  mv.table = p.block_table + (int64_t)seq * p.max_blocks;
+  mv.num_blocks = p.num_blocks;
+  mv.sb = is_v ? p.v_sb : p.k_sb;
+  mv.st = is_v ? 1 : p.k_st;
+  mv.lead = (int)(mv.base & (kBlockSize - 1));  // runs end at block borders of the destination
+  const int runs = (int)(((int64_t)mv.lead + mv.n + kRun - 1) / kRun);
+  Lookups look;
+  if (tid < kRun) look.start(mv);
+  if (is_v) {
+    for (int r = 0; r < 3; ++r) look.step(mv, ring.v, runs);
     __syncthreads();
-    if (!is_v) {
-      constexpr int kPieces = D / 8, kEach = kRun * kPieces / kCompactThreads;
-      uint4 x[kEach];
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int m = (e * kCompactThreads + tid) / kPieces, c = tid % kPieces;
-        if (at.src[m] >= 0) x[e] = *reinterpret_cast<const uint4*>(cache + at.src[m] + c * 8);
-      }
-      reads_arrived();
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int m = (e * kCompactThreads + tid) / kPieces, c = tid % kPieces;
-        if (at.dst[m] >= 0) *reinterpret_cast<uint4*>(cache + at.dst[m] + c * 8) = x[e];
-      }
-    } else {
-      constexpr int kEach = D * (kRun / 8) / kCompactThreads;
-      uint32_t x[kEach][4];  // two tokens each
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int c = (e * kCompactThreads + tid) % D, m = (e * kCompactThreads + tid) / D * 8;
-#pragma unroll
-        for (int t = 0; t < 8; t += 2) {
-          const uint32_t a = at.src[m + t] >= 0 ? cache[at.src[m + t] + c * p.v_sd] : 0;
-          const uint32_t b = at.src[m + t + 1] >= 0 ? cache[at.src[m + t + 1] + c * p.v_sd] : 0;
-          x[e][t / 2] = a | b << 16;
-        }
-      }
-      reads_arrived();
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int c = (e * kCompactThreads + tid) % D, m = (e * kCompactThreads + tid) / D * 8;
-        bool whole = true;
-#pragma unroll
-        for (int t = 0; t < 8; ++t) whole &= at.dst[m + t] >= 0;
-        if (whole) {
-          *reinterpret_cast<uint4*>(cache + at.dst[m] + c * p.v_sd) = make_uint4(x[e][0], x[e][1], x[e][2], x[e][3]);
-        } else {
-#pragma unroll
-          for (int t = 0; t < 8; ++t)
-            if (at.dst[m + t] >= 0) cache[at.dst[m + t] + c * p.v_sd] = (uint16_t)(x[e][t / 2] >> (t % 2 * 16));
-        }
-      }
-    }
-    __syncthreads();  // the places are read
+    compact_v(p.v + (int64_t)head * p.v_sh + slice * kSlice * p.v_sd, p.v_sd, mv, ring.v, look, stage, runs);
+  } else {
+    for (int r = 0; r < 3; ++r) look.step(mv, ring.k, runs);
+    __syncthreads();
+    compact_k(p.k + (int64_t)head * p.k_sh + slice * kSlice, mv, ring.k, look, runs);
   }
+}
+
+// Lists of up to kShort entries: everything is read before anything is written.
+template <int D>
+__global__ __launch_bounds__(256) void msa_kv_compact_short_kernel(CompactParams p) {
+  __shared__ __attribute__((aligned(16))) uint16_t s_k[kShort][D], s_v[kShort][D];
+  __shared__ int64_t k_src[kShort], k_dst[kShort], v_src[kShort], v_dst[kShort];
+  const int seq = blockIdx.x / p.num_kv_heads, head = blockIdx.x - seq * p.num_kv_heads, tid = threadIdx.x;
+  const int n = max(0, min(min(p.count[seq], p.max_count), kShort));
+  if (n == 0) return;
+  Moves mv;
+  mv.n = n;
+  mv.base = p.base ? p.base[seq] : 0;
+  mv.index = p.index + (int64_t)seq * p.i_sb + (int64_t)head * p.i_sh;
+  mv.table = p.block_table + (int64_t)seq * p.max_blocks;
+  mv.end = (int64_t)p.max_blocks * kBlockSize;
+  mv.num_blocks = p.num_blocks;
+  if (tid < n) {
+    const int32_t from = mv.index[tid];
+    const int64_t src = mv.base + from, dst = mv.base + tid;
+    const int32_t sb = from > tid ? mv.block_at(src) : -1, db = mv.block_at(dst);
+    const bool moves = sb >= 0 && db >= 0;
+    const int st = (int)(src & (kBlockSize - 1)), dt = (int)(dst & (kBlockSize - 1));
+    k_src[tid] = moves ? sb * p.k_sb + st * p.k_st : 0;  // (what is read where nothing moves is not used)
+    v_src[tid] = moves ? sb * p.v_sb + st : 0;
+    k_dst[tid] = moves ? db * p.k_sb + dt * p.k_st : -1;
+    v_dst[tid] = moves ? db * p.v_sb + dt : -1;
+  }
+  __syncthreads();
+  uint16_t* k = p.k + (int64_t)head * p.k_sh;
+  uint16_t* v = p.v + (int64_t)head * p.v_sh;
+  constexpr int kPieces = D / 8, kBatch = 8;  // reads of a thread under way together
+  const int pieces = n * kPieces, tokens = n * D;
+  for (int e0 = tid; e0 < tokens; e0 += 256 * kBatch) {
+    uint16_t x[kBatch];
+    uint4 y;
+    const int ek = (e0 - tid) / kBatch + tid;  // a piece of K for 8 tokens of V
+    if (ek < pieces) y = *reinterpret_cast<const uint4*>(k + k_src[ek / kPieces] + ek % kPieces * 8);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int e = min(e0 + i * 256, tokens - 1);
+      x[i] = v[v_src[e / D] + e % D * p.v_sd];
+    }
+    if (ek < pieces) *reinterpret_cast<uint4*>(&s_k[ek / kPieces][ek % kPieces * 8]) = y;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int e = min(e0 + i * 256, tokens - 1);
+      s_v[e / D][e % D] = x[i];
+    }
+  }
+  __syncthreads();
+  for (int e = tid; e < pieces; e += 256) {
+    const int64_t dst = k_dst[e / kPieces];
+    if (dst >= 0) *reinterpret_cast<uint4*>(k + dst + e % kPieces * 8) = *reinterpret_cast<const uint4*>(&s_k[e / kPieces][e % kPieces * 8]);
+  }
+  for (int e = tid; e < tokens; e += 256) {
+    const int64_t dst = v_dst[e / D];
+    if (dst >= 0) v[dst + e % D * p.v_sd] = s_v[e / D][e % D];
+  }
+}
+
+template <int D>
+int launch_compact(const CompactParams& p, int64_t heads, hipStream_t s) {
+  if (p.max_count <= kShort)
+    hipLaunchKernelGGL(msa_kv_compact_short_kernel<D>, dim3((uint32_t)heads), dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL(msa_kv_compact_kernel<D>, dim3((uint32_t)heads * (2 * D / kSlice)), dim3(kCompactThreads), 0, s,
+                       p);
+  return (int)hipGetLastError();
 }
 
 msa_status fail(msa_status st, const std::string& msg) {
@@ -150,14 +395,13 @@ extern "C" msa_status msa_kv_compact(const msa_shape* shape, const int32_t* base
   const msa_shape& s = *shape;
   if (max_count < 0 || index_stride_seq < 0 || index_stride_head < 0)
     return msa::fail(MSA_ERR_INVALID_ARG, "max_count and the index strides must be >= 0");
-  if (s.num_seqs == 0 || max_count == 0) return MSA_OK;
+  if (s.num_seqs == 0 || max_count == 0 || s.num_blocks == 0) return MSA_OK;
   if (!index || !count || !block_table || !k_cache || !v_cache)
     return msa::fail(MSA_ERR_INVALID_ARG, "index, count, block_table, k_cache, v_cache must be non-null");
   if (!msa::aligned(k_cache, 16) || !msa::aligned(v_cache, 16) || !msa::aligned(base, 4) || !msa::aligned(index, 4) ||
       !msa::aligned(count, 4) || !msa::aligned(block_table, 4))
     return msa::fail(MSA_ERR_INVALID_ARG, "caches must be 16-byte, the others 4-byte aligned");
-  const int64_t groups = (int64_t)s.num_seqs * s.num_kv_heads * 2;
-  if (groups >= ((int64_t)1 << 31)) return msa::fail(MSA_ERR_UNSUPPORTED, "too many heads for one launch");
+  if ((int64_t)s.num_seqs * s.num_kv_heads >= ((int64_t)1 << 29)) return msa::fail(MSA_ERR_UNSUPPORTED, "too many heads for one launch");
   msa::CompactParams p{};
   p.base = base;
   p.index = index;
@@ -178,9 +422,7 @@ extern "C" msa_status msa_kv_compact(const msa_shape* shape, const int32_t* base
   p.num_blocks = s.num_blocks;
   p.max_count = max_count;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  if (s.head_dim == 128)
-    hipLaunchKernelGGL(msa::msa_kv_compact_kernel<128>, dim3((uint32_t)groups), dim3(msa::kCompactThreads), 0, stream, p);
-  else
-    hipLaunchKernelGGL(msa::msa_kv_compact_kernel<64>, dim3((uint32_t)groups), dim3(msa::kCompactThreads), 0, stream, p);
-  return msa::launched("msa_kv_compact", "compaction", (int)hipGetLastError());
+  const int64_t heads = (int64_t)s.num_seqs * s.num_kv_heads;
+  const int rc = s.head_dim == 128 ? msa::launch_compact<128>(p, heads, stream) : msa::launch_compact<64>(p, heads, stream);
+  return msa::launched("msa_kv_compact", "compaction", rc);
 }

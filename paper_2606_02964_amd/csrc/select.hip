@@ -1,13 +1,22 @@
 // select.hip -- the positions that a reduced cache keeps (msa_kv_select).
 //
-// One workgroup per list.  The kept positions outside the first and the latest
-// ones are those of the largest scores: the bits of a float, flipped so that they
-// order as unsigned numbers, are fixed from the top, some bits a pass, by
-// counting (a histogram in LDS of the values that share the bits found so far).
-// The last pass leaves the smallest kept value T and how many of the values equal to
-// T stay; those of the lowest positions do.  One more pass over the positions
-// in order writes the list.  Counts are whole numbers, so the result does not
-// depend on the order of the LDS atomics.
+// One workgroup per list.  Every position gets a 32-bit key that orders as its
+// score does; the first and the latest positions, which stay whatever their
+// score, get the largest key there is.  The k-th largest key T is found from
+// its top bits down, 11 bits a pass, by counting (a histogram in LDS of the keys
+// that share the bits found so far); with it comes how many of the keys equal to T
+// stay, those of the lowest positions.  Each of the 16 waves holds a run of
+// neighbouring positions: it counts what it keeps, learns from the other
+// waves' counts where its own begin, and writes them in order.
+// A list of up to 64K scores is read once, into registers (up to 64 keys a
+// thread); longer ones are read again by every pass.  Reading is the smaller part:
+// one instruction for each of 16K keys takes a CU 256 cycles (16 waves, 16 keys a
+// lane), so time goes by instructions per key.  (With the window and the list's end
+// tested by position in every loop, and lanes that share a bin added up first, a
+// list of 9001 took 13.7 us; ranking the values that share T's first 11 bits one
+// against the other 19.6 us.)
+// Counts are whole numbers, so the result does not depend on the order of
+// the LDS atomics.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -16,6 +25,7 @@
 #include "errors.h"
 #include "forward.h"
 #include "msa_cache.h"
+#include "wave_ops.h"
 
 namespace msa {
 namespace {
@@ -36,19 +46,32 @@ struct SelectParams {
   int32_t num_lists, max_len, max_keep, first, recent;
 };
 
-// larger scores have larger keys; NaN as -inf, -0 as +0
+constexpr uint32_t kStays = 0xffffffffu;  // above every score's key
+
+// larger scores have larger keys; NaN as -inf, -0 as +0.  No score's key is 0 or kStays.
 __device__ __forceinline__ uint32_t order_key(float x) {
   if (x != x) x = -__builtin_inff();
-  const uint32_t u = x == 0.0f ? 0u : __float_as_uint(x);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  const int32_t u = __float_as_int(x + 0.0f);  // (-0 + 0 is +0)
+  return (uint32_t)u ^ ((uint32_t)(u >> 31) | 0x80000000u);
 }
 
+// sum of the entries before `wave`'s
+__device__ __forceinline__ int sum_before(const int (&x)[kSelectWaves], int wave) {
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < kSelectWaves; ++i) before += i < wave ? x[i] : 0;
+  return before;
+}
+
+// kEach: positions of a thread that registers hold, 0 where they do not
+template <int kEach>
 __global__ __launch_bounds__(kSelectThreads) void msa_kv_select_kernel(SelectParams p) {
-  __shared__ int hist[kBins];
-  __shared__ int s_wave[2][kSelectWaves];
-  __shared__ int s_bin, s_above;
+  __shared__ __attribute__((aligned(16))) int hist[kBins];
+  __shared__ __attribute__((aligned(16))) int s_bins[kSelectWaves], s_stay[kSelectWaves], s_tie[kSelectWaves];
+  __shared__ int s_bin, s_above, s_in;
   const int seq = blockIdx.x / p.num_lists, list = blockIdx.x - seq * p.num_lists;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = max(0, min(p.seq_len[seq], p.max_len));
   const int k = max(0, min(min(p.keep[seq], p.max_keep), n));
   if (list == 0 && tid == 0) p.count[seq] = k;
@@ -56,85 +79,118 @@ __global__ __launch_bounds__(kSelectThreads) void msa_kv_select_kernel(SelectPar
   const float* scores = p.scores + (int64_t)seq * p.s_sb + (int64_t)list * p.s_sl;
   int32_t* out = p.index + (int64_t)seq * p.i_sb + (int64_t)list * p.i_sl;
   const int recent = min(p.recent, k), first = min(p.first, k - recent);
-  const int lo = first, hi = n - recent;  // positions chosen by score lie in [lo, hi)
-  int want = k - recent - first;          // of them stay
+  const uint32_t lo = (uint32_t)first, hi = (uint32_t)(n - recent);  // by score: [lo, hi); with k = n all stay
 
-  // the key T of the last one that stays, and how many equal to it do
-  uint32_t found = 0, known = 0;  // T's bits found so far, their mask
-  int shift = 32, ties = 0;
-  const bool all = want == hi - lo;
-  if (!all && want > 0) {
-    while (shift > 0) {
-      const int bits = min(kRadixBits, shift);
-      shift -= bits;
-      for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
-      __syncthreads();
-      for (int j = lo + tid; j < hi; j += kSelectThreads) {
-        const uint32_t key = order_key(scores[j]);
-        if ((key & known) == found) atomicAdd(&hist[key >> shift & ((1u << bits) - 1)], 1);
-      }
-      __syncthreads();
-      // the bin, from the top, in which the want-th value lies: each thread has two bins
-      const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
-      const int c1 = hist[b1], c0 = hist[b0];
-      int run = c0 + c1;
+  // the wave's elements: element e of a lane is position first_of + 64 e
+  const int each = (int)(((int64_t)n + kSelectThreads - 1) / kSelectThreads);
+  const uint32_t first_of = (uint32_t)wave * (uint32_t)each * 64u + (uint32_t)lane;
+  auto key_at = [&](uint32_t j) -> uint32_t {
+    if (j >= (uint32_t)n) return 0u;
+    if (j - lo >= hi - lo || k == n) return kStays;
+    return order_key(scores[j]);
+  };
+  uint32_t held[kEach > 0 ? kEach : 1];
+  if constexpr (kEach > 0) {
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(run, d);
-        if (lane >= d) run += y;
-      }
-      if (lane == 63) s_wave[0][wave] = run;
-      __syncthreads();
-      for (int i = 0; i < wave; ++i) run += s_wave[0][i];
-      const int before = run - c0 - c1;
-      if (before < want && want <= run) {
-        const bool upper = want <= before + c1;
-        s_bin = upper ? b1 : b0;
-        s_above = before + (upper ? 0 : c1);
-      }
-      __syncthreads();
-      found |= (uint32_t)s_bin << shift;
-      known |= ((1u << bits) - 1) << shift;
-      want -= s_above;
-      __syncthreads();
+    for (int e = 0; e < kEach; ++e) held[e] = e < each ? key_at(first_of + (uint32_t)e * 64u) : 0u;
+  }
+  // f(position, key) for the wave's elements, in order
+  auto for_each = [&](auto&& f) __attribute__((always_inline)) {
+    uint32_t start = first_of;
+    asm volatile("" : "+v"(start));  // (positions are not kept from one loop to the next)
+    if constexpr (kEach > 0) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (e < each) f(start + (uint32_t)e * 64u, held[e]);
+    } else {
+      for (int e = 0; e < each; ++e) f(start + (uint32_t)e * 64u, key_at(start + (uint32_t)e * 64u));
     }
+  };
+
+  // Keys above `found` stay, and the first `ties` of those equal to it.
+  uint32_t found = 0;
+  int ties = 0;
+  if (k < n) {
+    int want = k, shift = 32, bits = 0;
+    for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
+    __syncthreads();
+    do {
+      const int above_bits = shift;  // bits of a key from here up are found
+      bits = min(kRadixBits, shift);
+      shift -= bits;
+      if (above_bits == 32) {
+        for_each([&](uint32_t, uint32_t key) { atomicAdd(&hist[key >> (32 - kRadixBits)], 1); });
+      } else {
+        const uint32_t share = found >> above_bits;
+        for_each([&](uint32_t, uint32_t key) {
+          if (key >> above_bits == share) atomicAdd(&hist[__builtin_amdgcn_ubfe(key, (uint32_t)shift, (uint32_t)bits)], 1);
+        });
+      }
+      __syncthreads();
+      // the bin, from the top, in which the want-th key lies: each thread has two bins
+      const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
+      const int2 c = *reinterpret_cast<const int2*>(&hist[b0]);
+      *reinterpret_cast<int2*>(&hist[b0]) = make_int2(0, 0);
+      int run = wave_scan(c.x + c.y);
+      if (lane == 63) s_bins[wave] = run;
+      __syncthreads();
+      run += sum_before(s_bins, wave);
+      const int before = run - c.x - c.y;
+      if (before < want && want <= run) {
+        const bool upper = want <= before + c.y;
+        s_bin = upper ? b1 : b0;
+        s_above = before + (upper ? 0 : c.y);
+        s_in = upper ? c.y : c.x;
+      }
+      __syncthreads();
+      found |= (uint32_t)__builtin_amdgcn_readfirstlane(s_bin) << shift;
+      want -= __builtin_amdgcn_readfirstlane(s_above);
+      if (__builtin_amdgcn_readfirstlane(s_in) == want) {  // all that share the bits found so far stay
+        found -= 1;                                        // (their bin is not 0: key 0 is no position's)
+        want = 0;
+      }
+    } while (shift > 0 && want > 0);
     ties = want;
   }
 
-  // positions in order, one per thread at a time
-  int placed = 0, equal = 0;  // before this round
-  for (int base = 0; base < n; base += kSelectThreads) {
-    const int j = base + tid;
-    bool stays = j < n && (j < lo || j >= hi), tie = false;
-    if (j >= lo && j < hi) {
-      if (all) {
-        stays = true;
-      } else if (ties > 0) {
-        const uint32_t key = order_key(scores[j]);
-        stays = key > found;
-        tie = key == found;
-      }
-    }
-    const uint64_t below = (1ull << lane) - 1;
-    const uint64_t tie_lanes = __ballot(tie);
-    if (lane == 0) s_wave[0][wave] = __popcll(tie_lanes);
-    __syncthreads();
-    int eq = equal;
-    for (int i = 0; i < kSelectWaves; ++i) {
-      eq += i < wave ? s_wave[0][i] : 0;
-      equal += s_wave[0][i];
-    }
-    if (tie && eq + __popcll(tie_lanes & below) < ties) stays = true;
-    const uint64_t stay_lanes = __ballot(stays);
-    if (lane == 0) s_wave[1][wave] = __popcll(stay_lanes);
-    __syncthreads();
-    int at = placed;
-    for (int i = 0; i < kSelectWaves; ++i) {
-      at += i < wave ? s_wave[1][i] : 0;
-      placed += s_wave[1][i];
-    }
-    if (stays) out[at + __popcll(stay_lanes & below)] = j;
+  // what each wave keeps
+  int stay = 0, tie = 0;
+  for_each([&](uint32_t, uint32_t key) {
+    stay += key > found;
+    tie += key == found;
+  });
+  stay = wave_sum(stay);
+  tie = ties > 0 ? wave_sum(tie) : 0;
+  if (lane == 0) {
+    s_stay[wave] = stay;
+    s_tie[wave] = tie;
   }
+  __syncthreads();
+  int equal = sum_before(s_tie, wave);
+  int32_t* at = out + sum_before(s_stay, wave) + min(equal, ties);
+  if (tie == 0 || equal >= ties) {  // (uniform over the wave)
+    for_each([&](uint32_t j, uint32_t key) {
+      const uint64_t lanes = __ballot(key > found);
+      if (key > found)
+        at[__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0))] = (int32_t)j;
+      at += __popcll(lanes);
+    });
+  } else {
+    const uint64_t below = (1ull << lane) - 1;
+    for_each([&](uint32_t j, uint32_t key) {
+      const uint64_t tie_lanes = __ballot(key == found);
+      const bool stays = key > found || (key == found && equal + __popcll(tie_lanes & below) < ties);
+      const uint64_t lanes = __ballot(stays);
+      if (stays) at[__popcll(lanes & below)] = (int32_t)j;
+      equal += __popcll(tie_lanes);
+      at += __popcll(lanes);
+    });
+  }
+}
+
+template <int kEach>
+void launch_select(const SelectParams& p, int64_t lists, hipStream_t s) {
+  hipLaunchKernelGGL(msa_kv_select_kernel<kEach>, dim3((uint32_t)lists), dim3(kSelectThreads), 0, s, p);
 }
 
 msa_status fail(msa_status st, const std::string& msg) {
@@ -179,7 +235,18 @@ extern "C" msa_status msa_kv_select(int32_t num_seqs, int32_t num_lists, const f
   p.max_keep = max_keep;
   p.first = first;
   p.recent = recent;
-  hipLaunchKernelGGL(msa::msa_kv_select_kernel, dim3((uint32_t)lists), dim3(msa::kSelectThreads), 0,
-                     static_cast<hipStream_t>(hip_stream), p);
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  // the fewest registers that hold the longest list
+  const int64_t each = ((int64_t)max_len + msa::kSelectThreads - 1) / msa::kSelectThreads;
+  if (each <= 8)
+    msa::launch_select<8>(p, lists, st);
+  else if (each <= 16)
+    msa::launch_select<16>(p, lists, st);
+  else if (each <= 32)
+    msa::launch_select<32>(p, lists, st);
+  else if (each <= 64)
+    msa::launch_select<64>(p, lists, st);
+  else
+    msa::launch_select<0>(p, lists, st);
   return msa::launched("msa_kv_select", "selection", (int)hipGetLastError());
 }

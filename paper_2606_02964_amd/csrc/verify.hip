@@ -1,7 +1,7 @@
 // verify.hip -- verification of trees of drafted tokens against the target's
 // probabilities (msa_tree_verify; the rule is in include/msa_tree.h).
 //
-// Two launches.
+// Three launches.
 // msa_verify_walk, one workgroup per tree: the walk reads two numbers a slot
 // (p and q of the slot's token in its parent's row), all at once, and then
 // takes one decision after the other in registers.  Where a node's children
@@ -9,9 +9,13 @@
 // two scalars a and b (max(max(x, 0) / P - q, 0) = max(x / P - q, 0), as q >= 0),
 // so nothing of the vocabulary's length is stored; a second or later child's test
 // needs that residual's mass, for which the workgroup reads the node's two rows.
-// msa_verify_sample, chunks of the vocabulary x trees: sums r over its chunk;
-// the last chunk of a tree to finish finds the chunk, then the entry, at which the
-// running sum passes u T.
+// msa_verify_sums: the sum of r over each cell of 2048 entries of the vocabulary.
+// msa_verify_pick, one workgroup per tree: the cell, then the entry, at which the
+// running sum passes u T; a thread holds 8 neighbouring entries of the cell.
+// Bound by reading one or two rows of the vocabulary per tree, and for few trees by
+// the chains of dependent reads in walk and pick.  (The pick used to be done by
+// the last workgroup of the sums to finish: the fences that this takes write
+// back the whole L2 of an XCD, for every workgroup.)
 // Sums are in 64 bits: with 10^5 tokens the borders between neighbouring tokens
 // are about 10^-5 of the mass apart and a 32-bit running sum would pick a
 // neighbour once in some hundred draws; and the tests' products (24 + 24 bits)
@@ -28,6 +32,7 @@
 #include "forward.h"
 #include "msa_tree.h"
 #include "plan_handle.h"
+#include "wave_ops.h"
 
 #pragma clang fp contract(off)  // a p - b q is 0 where both products are equal
 
@@ -35,9 +40,9 @@ namespace msa {
 namespace {
 
 constexpr int kWalkThreads = 1024;
-constexpr int kSampleThreads = 256;
-constexpr int kChunkMin = 2048;   // entries of a sample workgroup, at least
-constexpr int kChunkMax = 32768;  // and at most (its bitmap of failed tokens is in LDS)
+constexpr int kCellThreads = 256;
+constexpr int kEach = 8;                        // neighbouring entries of a thread
+constexpr int kCell = kCellThreads * kEach;     // entries of a cell
 constexpr int kWave = 64;
 
 // How the next token's weights follow from the last node's row(s).
@@ -48,7 +53,7 @@ struct WalkResult {
   int32_t tree_row;  // of the last node
   int32_t node;      // its slot
   int32_t rest;
-  int32_t arrived;   // chunks summed so far (msa_verify_sample)
+  int32_t pad;
 };
 
 struct VerifyParams {
@@ -65,8 +70,10 @@ struct VerifyParams {
   int32_t* next_token;
   const TreeSpan* trees;
   WalkResult* walk;  // [trees]
-  double* sums;      // [trees][chunks][2]: r, p
-  int32_t vocab, max_slots, chunk, chunks;
+  double* sums;      // [trees][cells]
+  int32_t vocab, max_slots;
+  int32_t cells;     // of a row
+  int32_t groups;    // sums: workgroups of a tree
 };
 
 __device__ __forceinline__ float clean(float x) { return x > 0.0f && x < __builtin_inff() ? x : 0.0f; }
@@ -85,19 +92,16 @@ __device__ __forceinline__ void load4(const T* src, float (&x)[4]) {
   for (int i = 0; i < 4; ++i) x[i] = clean(to_float(r.v[i]));
 }
 
-__device__ __forceinline__ double wave_sum(double x) {
+template <class T>
+__device__ __forceinline__ void load8(const T* src, float (&x)[8]) {
+  float lo[4], hi[4];
+  load4(src, lo);
+  load4(src + 4, hi);
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-  return x;
-}
-// inclusive running sum over the wave
-__device__ __forceinline__ double wave_scan(double x, int lane) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const double y = __shfl_up(x, d);
-    if (lane >= d) x += y;
+  for (int i = 0; i < 4; ++i) {
+    x[i] = lo[i];
+    x[i + 4] = hi[i];
   }
-  return x;
 }
 
 // sum over the workgroup of max(a p - b q, 0) over the vocabulary
@@ -216,165 +220,173 @@ __global__ __launch_bounds__(kWalkThreads) void msa_verify_walk_kernel(VerifyPar
   }
 }
 
-// The weights of the next token: entry t of a row is weight(t).
+// The last node's weights, a cell at a time.
 template <class T>
-struct Weights {
+struct Rows {
   const T *p, *q;
   double a, b;
-  int rest, lo;
-  const uint32_t* gone;  // bit t - lo: token t failed under the last node
-  __device__ __forceinline__ double of(float x, float y, int t) const {
-    if (rest == kResidual) return fmax(a * (double)x - b * (double)y, 0.0);
-    if (rest == kWithout && (gone[(t - lo) >> 5] >> ((t - lo) & 31) & 1)) return 0.0;
-    return (double)x;
+  int rest, vocab;
+  const TreeSpan tree;
+  int node;
+  const int32_t *tokens, *parents;
+
+  __device__ __forceinline__ Rows(const VerifyParams& v, int tree_id)
+      : vocab(v.vocab), tree(v.trees[tree_id]), tokens(v.tokens + tree.row0), parents(v.parents + tree.row0) {
+    const WalkResult r = v.walk[tree_id];
+    p = static_cast<const T*>(v.target) + (int64_t)r.tree_row * v.target_stride;
+    q = static_cast<const T*>(v.draft) + (int64_t)r.tree_row * v.draft_stride;
+    a = r.a;
+    b = r.b;
+    rest = r.rest;
+    node = r.node;
   }
-  __device__ __forceinline__ double at(int t) const {
-    return of(clean(to_float(p[t])), rest == kResidual ? clean(to_float(q[t])) : 0.0f, t);
+
+  // the thread's 8 entries of a cell, 0 behind the row's end; `gone` (LDS) takes a bit for
+  // each of the cell's tokens that failed under the last node
+  __device__ __forceinline__ void load(int cell, uint32_t* gone, double (&w)[kEach]) const {
+    const int tid = threadIdx.x, lo = cell * kCell, t0 = lo + tid * kEach;
+    float x[kEach], y[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) x[i] = y[i] = 0.0f;
+    if (t0 + kEach <= vocab) {
+      load8(p + t0, x);
+      if (rest == kResidual) load8(q + t0, y);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        if (t0 + i < vocab) {
+          x[i] = clean(to_float(p[t0 + i]));
+          if (rest == kResidual) y[i] = clean(to_float(q[t0 + i]));
+        }
+    }
+    uint32_t out = 0;
+    if (rest == kWithout) {
+      __syncthreads();
+      if (tid < kCell / 32) gone[tid] = 0;
+      __syncthreads();
+      for (int i = node + 1 + tid; i < tree.n; i += kCellThreads) {
+        const int32_t t = tokens[i];
+        if (parents[i] == node && t >= lo && t - lo < kCell) atomicOr(&gone[(t - lo) >> 5], 1u << ((t - lo) & 31));
+      }
+      __syncthreads();
+      out = gone[tid * kEach >> 5] >> (tid * kEach & 31);
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      w[i] = rest == kResidual ? fmax(a * (double)x[i] - b * (double)y[i], 0.0) : out >> i & 1 ? 0.0 : (double)x[i];
   }
 };
 
-// marks the failed children's tokens inside [lo, hi) in `gone`
-template <class T>
-__device__ void mark_failed(const VerifyParams& v, const TreeSpan& tree, const WalkResult& r, int lo, int hi,
-                            uint32_t* gone) {
-  const int tid = threadIdx.x;
+__device__ __forceinline__ double sum_of(const double (&w)[kEach]) {
+  return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+}
+
+// sum over the workgroup, for every thread
+__device__ __forceinline__ double group_sum(double x, double* part) {
+  x = wave_sum(x);
   __syncthreads();
-  for (int i = tid; i < kChunkMax / 32; i += kSampleThreads) gone[i] = 0;
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
   __syncthreads();
-  for (int i = r.node + 1 + tid; i < tree.n; i += kSampleThreads) {
-    const int32_t t = v.tokens[tree.row0 + i];
-    if (v.parents[tree.row0 + i] == r.node && t >= lo && t < hi)
-      atomicOr(&gone[(t - lo) >> 5], 1u << ((t - lo) & 31));
-  }
-  __syncthreads();
+  return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
 template <class T>
-__global__ __launch_bounds__(kSampleThreads) void msa_verify_sample_kernel(VerifyParams v) {
-  __shared__ uint32_t gone[kChunkMax / 32];
-  __shared__ double part[2][kSampleThreads / kWave];
-  __shared__ int s_last, s_found;
-  const int tree_id = blockIdx.x / v.chunks, chunk = blockIdx.x - tree_id * v.chunks;
-  const TreeSpan tree = v.trees[tree_id];
-  const WalkResult r = v.walk[tree_id];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  Weights<T> w;
-  w.p = static_cast<const T*>(v.target) + (int64_t)r.tree_row * v.target_stride;
-  w.q = r.rest == kResidual ? static_cast<const T*>(v.draft) + (int64_t)r.tree_row * v.draft_stride : nullptr;
-  w.a = r.a;
-  w.b = r.b;
-  w.rest = r.rest;
-  w.gone = gone;
-  {
-    const int lo = chunk * v.chunk, hi = min(lo + v.chunk, v.vocab);
-    w.lo = lo;
-    if (r.rest == kWithout) mark_failed<T>(v, tree, r, lo, hi, gone);
-    double sr = 0.0, sp = 0.0;
-    const int whole = lo + ((hi - lo) & ~3);
-    for (int t = lo + tid * 4; t < whole; t += kSampleThreads * 4) {
-      float x[4], y[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      load4(w.p + t, x);
-      if (r.rest == kResidual) load4(w.q + t, y);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        sr += w.of(x[i], y[i], t + i);
-        sp += (double)x[i];
-      }
-    }
-    for (int t = whole + tid; t < hi; t += kSampleThreads) {
-      sr += w.at(t);
-      sp += (double)clean(to_float(w.p[t]));
-    }
-    sr = wave_sum(sr);
-    sp = wave_sum(sp);
-    if (lane == 0) {
-      part[0][wave] = sr;
-      part[1][wave] = sp;
-    }
-    __syncthreads();
-    if (tid == 0) {
-      double* out = v.sums + ((int64_t)tree_id * v.chunks + chunk) * 2;
-      out[0] = part[0][0] + part[0][1] + part[0][2] + part[0][3];
-      out[1] = part[1][0] + part[1][1] + part[1][2] + part[1][3];
-      __threadfence();  // the sums are seen on every XCD before the arrival is
-      s_last = atomicAdd(&v.walk[tree_id].arrived, 1) == v.chunks - 1;
-    }
-    __syncthreads();
-    if (!s_last) return;
-    __threadfence();
+__global__ __launch_bounds__(kCellThreads) void msa_verify_sums_kernel(VerifyParams v) {
+  __shared__ uint32_t gone[kCell / 32];
+  __shared__ double part[kCellThreads / kWave];
+  const int tree_id = blockIdx.x / v.groups, group = blockIdx.x - tree_id * v.groups;
+  const Rows<T> rows(v, tree_id);
+  for (int cell = group; cell < v.cells; cell += v.groups) {
+    double w[kEach];
+    rows.load(cell, gone, w);
+    const double sum = group_sum(sum_of(w), part);
+    if (threadIdx.x == 0) v.sums[(int64_t)tree_id * v.cells + cell] = sum;
   }
+}
 
-  // The tree's last workgroup: total, chunk, entry.
-  const volatile double* sums = v.sums + (int64_t)tree_id * v.chunks * 2;
-  double total[2] = {0.0, 0.0};
-  for (int c0 = 0; c0 < v.chunks; c0 += kWave) {
-    const int c = c0 + lane;
-    total[0] += __shfl(wave_scan(c < v.chunks ? sums[2 * c] : 0.0, lane), kWave - 1);
-    total[1] += __shfl(wave_scan(c < v.chunks ? sums[2 * c + 1] : 0.0, lane), kWave - 1);
+template <class T>
+__global__ __launch_bounds__(kCellThreads) void msa_verify_pick_kernel(VerifyParams v) {
+  __shared__ uint32_t gone[kCell / 32];
+  __shared__ double part[kCellThreads / kWave];
+  __shared__ int s_found, s_last;
+  const int tree_id = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const double* sums = v.sums + (int64_t)tree_id * v.cells;
+  const double u = (double)fminf(fmaxf(v.u_sample[tree_id], 0.0f), 0x1.fffffep-1f);  // (fmaxf of NaN and 0 is 0)
+  Rows<T> rows(v, tree_id);
+  double w[kEach], total = 0.0;
+  for (int c0 = 0; c0 < v.cells; c0 += kWave) total += wave_sum(c0 + lane < v.cells ? sums[c0 + lane] : 0.0);
+  const bool again = !(total > 0.0);  // nothing is left: the row itself, summed here (it hardly ever is)
+  if (again) {
+    rows.rest = kAsIs;
+    total = 0.0;
+    for (int c = 0; c < v.cells; ++c) {
+      rows.load(c, gone, w);
+      total += group_sum(sum_of(w), part);
+    }
+    if (!(total > 0.0)) {  // (uniform over the workgroup)
+      if (tid == 0) v.next_token[tree_id] = -1;
+      return;
+    }
   }
-  const int which = total[0] > 0.0 ? 0 : 1;  // nothing left: the row itself
-  if (!(total[which] > 0.0)) {               // uniform over the workgroup
-    if (tid == 0) v.next_token[tree_id] = -1;
-    return;
-  }
-  if (which == 1) w.rest = kAsIs;
-  const float u = fminf(fmaxf(v.u_sample[tree_id], 0.0f), 0x1.fffffep-1f);  // (fmaxf of NaN and 0 is 0)
-  const double x = (double)u * total[which];
-  // the first chunk whose running sum passes x; where rounding leaves none, the
+  const double x = u * total;
+  // the first cell whose running sum passes x; where rounding leaves none, the
   // last one that holds any weight
-  double before = 0.0, carry = 0.0;
   int found = -1, holds = 0;
-  double holds_before = 0.0;
-  for (int c0 = 0; c0 < v.chunks && found < 0; c0 += kWave) {
-    const int c = c0 + lane;
-    const double s = c < v.chunks ? sums[2 * c + which] : 0.0;
-    const double run = carry + wave_scan(s, lane);
+  double before = 0.0, holds_before = 0.0, carry = 0.0;
+  if (again) {
+    for (int c = 0; c < v.cells && found < 0; ++c) {
+      rows.load(c, gone, w);
+      const double s = group_sum(sum_of(w), part);
+      if (carry + s > x) {
+        found = c;
+        before = carry;
+      } else if (s > 0.0) {
+        holds = c;
+        holds_before = carry;
+      }
+      carry += s;
+    }
+  }
+  for (int c0 = 0; c0 < v.cells && found < 0 && !again; c0 += kWave) {
+    const double s = c0 + lane < v.cells ? sums[c0 + lane] : 0.0;
+    const double run = carry + wave_scan(s);
     const uint64_t past = __ballot(run > x), some = __ballot(s > 0.0);
-    double prev = __shfl_up(run, 1);
-    if (lane == 0) prev = carry;
+    const double prev = lane_below(run, carry);
     if (past) {
       const int l = __builtin_ctzll(past);
       found = c0 + l;
-      before = __shfl(prev, l);
+      before = lane_value(prev, l);
     } else if (some) {
       const int l = 63 - __builtin_clzll(some);
       holds = c0 + l;
-      holds_before = __shfl(prev, l);
+      holds_before = lane_value(prev, l);
     }
-    carry = __shfl(run, kWave - 1);
+    carry = lane_value(run, kWave - 1);
   }
   if (found < 0) {
     found = holds;
     before = holds_before;
   }
-  const int lo = found * v.chunk, hi = min(lo + v.chunk, v.vocab);
-  w.lo = lo;
-  if (w.rest == kWithout) mark_failed<T>(v, tree, r, lo, hi, gone);
-  // inside it, each thread takes a run of entries
-  const int each = (hi - lo + kSampleThreads - 1) / kSampleThreads;
-  const int t0 = min(lo + tid * each, hi), t1 = min(t0 + each, hi);
-  double own = 0.0;
-  for (int t = t0; t < t1; ++t) own += w.at(t);
-  const double run = wave_scan(own, lane);
+  rows.load(found, gone, w);
+  const double own = sum_of(w), run = wave_scan(own);
   __syncthreads();
-  if (lane == kWave - 1) part[0][wave] = run;
+  if (lane == kWave - 1) part[wave] = run;
   if (tid == 0) s_found = 0x7fffffff, s_last = -1;
   __syncthreads();
   double at = before;
-  for (int i = 0; i < wave; ++i) at += part[0][i];
-  double prev = __shfl_up(run, 1);
-  at += lane == 0 ? 0.0 : prev;
-  for (int t = t0; t < t1; ++t) {
-    const double y = w.at(t);
-    at += y;
-    if (y > 0.0) {
-      if (at > x) {
-        atomicMin(&s_found, t);
-        break;
-      }
-      atomicMax(&s_last, t);
+  for (int i = 0; i < wave; ++i) at += part[i];
+  at += lane_below(run, 0.0);
+  int first = 0x7fffffff, last = -1;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    at += w[i];
+    if (w[i] > 0.0) {
+      last = found * kCell + tid * kEach + i;
+      if (at > x && first == 0x7fffffff) first = last;
     }
   }
+  if (first != 0x7fffffff) atomicMin(&s_found, first);
+  if (last >= 0) atomicMax(&s_last, last);
   __syncthreads();
   if (tid == 0) v.next_token[tree_id] = s_found != 0x7fffffff ? s_found : s_last;
 }
@@ -382,26 +394,20 @@ __global__ __launch_bounds__(kSampleThreads) void msa_verify_sample_kernel(Verif
 template <class T>
 int launch_verify(const VerifyParams& v, int trees, hipStream_t s) {
   hipLaunchKernelGGL(msa_verify_walk_kernel<T>, dim3(trees), dim3(kWalkThreads), 0, s, v);
-  const int rc = (int)hipGetLastError();
+  int rc = (int)hipGetLastError();
   if (rc != 0) return rc;
-  hipLaunchKernelGGL(msa_verify_sample_kernel<T>, dim3((uint32_t)trees * (uint32_t)v.chunks), dim3(kSampleThreads),
-                     0, s, v);
+  hipLaunchKernelGGL(msa_verify_sums_kernel<T>, dim3((uint32_t)trees * (uint32_t)v.groups), dim3(kCellThreads), 0, s,
+                     v);
+  rc = (int)hipGetLastError();
+  if (rc != 0) return rc;
+  hipLaunchKernelGGL(msa_verify_pick_kernel<T>, dim3(trees), dim3(kCellThreads), 0, s, v);
   return (int)hipGetLastError();
 }
 
-// entries of a chunk: some 1024 workgroups in all, as the chunk's bounds allow
-int chunk_of(int64_t trees, int64_t vocab) {
-  const int64_t per_tree = std::max<int64_t>(1, 1024 / trees);
-  const int64_t c = ((vocab + per_tree - 1) / per_tree + 1023) / 1024 * 1024;
-  return (int)std::min<int64_t>(kChunkMax, std::max<int64_t>(kChunkMin, c));
-}
-int64_t chunks_of(int64_t trees, int64_t vocab) {
-  const int64_t c = chunk_of(trees, vocab);
-  return (vocab + c - 1) / c;
-}
+int64_t cells_of(int64_t vocab) { return (vocab + kCell - 1) / kCell; }
 size_t walk_bytes(int64_t trees) { return ((size_t)trees * sizeof(WalkResult) + 255) / 256 * 256; }
 size_t workspace_of(int64_t trees, int64_t vocab) {
-  return trees == 0 ? 0 : walk_bytes(trees) + (size_t)(trees * chunks_of(trees, vocab)) * 2 * sizeof(double);
+  return trees == 0 ? 0 : walk_bytes(trees) + (size_t)(trees * cells_of(vocab)) * sizeof(double);
 }
 
 msa_status fail(const char* who, msa_status st, const std::string& msg) {
@@ -434,6 +440,7 @@ extern "C" msa_status msa_tree_verify(msa_plan_t plan, int32_t prob_type, int32_
   if (prob_type != MSA_PROB_F32 && prob_type != MSA_PROB_BF16 && prob_type != MSA_PROB_F16)
     return invalid("prob_type must be MSA_PROB_F32, MSA_PROB_BF16 or MSA_PROB_F16");
   if (vocab < 1) return invalid("vocab < 1");
+  if (vocab > 0x7fff0000) return msa::fail(who, MSA_ERR_UNSUPPORTED, "vocab > 2^31 - 2^16");
   if (plan->host_only) return invalid("plan was built with MSA_PLAN_HOST_ONLY");
   const msa::HostPlan& hp = plan->hp;
   const int64_t trees = (int64_t)hp.trees.size();
@@ -451,9 +458,6 @@ extern "C" msa_status msa_tree_verify(msa_plan_t plan, int32_t prob_type, int32_
   const size_t need = msa::workspace_of(trees, vocab);
   if (!workspace || !msa::aligned(workspace, 16) || workspace_bytes < need)
     return invalid("workspace must be 16-byte aligned and hold " + std::to_string(need) + " bytes");
-  const int64_t chunks = msa::chunks_of(trees, vocab);
-  if (trees * chunks >= ((int64_t)1 << 31))
-    return msa::fail(who, MSA_ERR_UNSUPPORTED, "trees x vocab too large for one launch");
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev != plan->device)
     return invalid("current device differs from the plan's device");
@@ -475,8 +479,9 @@ extern "C" msa_status msa_tree_verify(msa_plan_t plan, int32_t prob_type, int32_
   v.sums = reinterpret_cast<double*>(static_cast<char*>(workspace) + msa::walk_bytes(trees));
   v.vocab = vocab;
   v.max_slots = hp.max_slots;
-  v.chunk = msa::chunk_of(trees, vocab);
-  v.chunks = (int32_t)chunks;
+  v.cells = (int32_t)msa::cells_of(vocab);
+  // a workgroup per cell, up to some 8192 of them
+  v.groups = (int32_t)std::min<int64_t>(v.cells, std::max<int64_t>(1, 8192 / trees));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int rc = prob_type == MSA_PROB_F32    ? msa::launch_verify<float>(v, (int)trees, s)
                  : prob_type == MSA_PROB_BF16 ? msa::launch_verify<__hip_bfloat16>(v, (int)trees, s)

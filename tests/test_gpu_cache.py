@@ -259,10 +259,15 @@ def compact_ref(k, v, table, base, lists, counts, cap):
     return k, v
 
 
-def check_compact(lens, base, counts, lists, heads=(2, 128), shared=False, spoil=(), seed=1, strides=False):
+def check_compact(lens, base, counts, lists, heads=(2, 128), shared=False, spoil=(), seed=1, strides=False,
+                  swap=()):
     hkv, d = heads
     table, k, v = paged(lens, hkv, d, seed)
     for b, i, blk in spoil:
+        table[b, i] = blk
+    for b, i, blk in swap:  # physical block blk at logical block i, its owner gets the other one
+        old = table[b, i].clone()
+        table[table == blk] = old
         table[b, i] = blk
     kw = {}
     if strides:  # heads outermost in the block, padded rows
@@ -332,6 +337,18 @@ def test_compact_long():
     lens = [9000, 5000]
     counts = [4500, 4999]
     check_compact(lens, [0, 0], counts, [[pick(r, n, c) for _ in range(2)] for n, c in zip(lens, counts)], (2, 64))
+
+
+def test_compact_with_any_block_anywhere():
+    """Physical block 0 (and every other) as a source behind kept places and behind skipped moves, at every block of a
+    sequence."""
+    r = random.Random(10)
+    for at in range(12):
+        lens = [192, 192]
+        idx = list(range(5)) + pick(r, 187, 150)
+        idx = sorted(set(x + 5 if i >= 5 else x for i, x in enumerate(idx)))
+        table_order = [(0, at, 0)]
+        check_compact(lens, [0, 3], [len(idx)] * 2, [[idx, idx]] * 2, shared=True, swap=table_order)
 
 
 def test_compact_skips_what_lies_outside():
