@@ -5,8 +5,8 @@
 //          head's group, of exp(scale q_rh k_j - lse_rh)
 //
 // The softmax's statistics are known (msa_forward's lse), so a key's sum needs
-// one pass over the rows and no other key.  A wave takes 64 keys of one KV head
-// and goes through the rows of their sequence, 32 (row, head) pairs at a time:
+// one pass over the rows and no other key.  Rows are taken 32 (row, head) pairs of a
+// KV head at a time:
 //   - S = Q K^T on v_mfma_f32_32x32x16_bf16 with Q as the A operand: each lane
 //     then holds 16 rows of ONE key (a column of S), so a key's sum stays in its
 //     lane; the lane pair (l, l + 32) of a key is joined once at the end;
@@ -16,12 +16,25 @@
 //     exp2 of that times scale * log2(e).  A row that is to give no weight (no such
 //     row, or lse = -inf) has -inf there, and costs nothing further;
 //   - the causal limit is applied only on the tiles that hold a row before the
-//     wave's last key.  Rows ascend in position, so the walk starts at the last
-//     row and ends at the first tile whose rows all lie before the wave's keys.
+//     wave's last key.
+// Two kernels, by the pairs of a sequence's rows and a KV head's group:
+//   msa_kv_weights_stream, up to 32 pairs (decoding): the rows stay in registers
+//   and each wave streams a run of keys, the next 32 on their way while it
+//   computes.  Bound by reading K.
+//   msa_kv_weights_tiles, more: a workgroup holds 256 keys in registers, 64 a wave,
+//   and streams the pairs' Q, lse and positions through a ring of four tiles in
+//   LDS, filled by direct copies that run three tiles ahead (each wave its share,
+//   one barrier a tile).  Read by every wave for itself, Q took four times the reads,
+//   each over 32 cache lines.  Rows ascend in position: the first tile is the one
+//   that holds the first row to see the workgroup's keys.  Where a launch would
+//   hold few workgroups, each one's tiles are split; the parts' sums go through
+//   the workspace and are added in order.  Bound by MFMAs (18 of 32 cycles a tile
+//   of 32 x 64) and exponentials (32 of 16 cycles) about equally.
 // Sums are in fp32, 16 rows of a tile added pairwise and then to the running sum;
 // no atomics, so equal calls give equal bits.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <string>
 
@@ -36,8 +49,13 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+constexpr int kPairs = 32;                 // (row, head) pairs of a tile
 constexpr int kWaveKeys = 64;
-constexpr int kGroupKeys = 4 * kWaveKeys;  // keys of a workgroup
+constexpr int kGroupKeys = 4 * kWaveKeys;  // keys of a workgroup (tiles)
+constexpr int kRing = 4;                   // tiles in LDS
+constexpr int kMostParts = 16;
 
 struct WeightsParams {
   const uint16_t* q;
@@ -47,9 +65,13 @@ struct WeightsParams {
   const int32_t* seq_row0;
   const float* lse;
   float* weights;
+  float* sums;  // [parts][sequences][KV heads][span], parts > 1
   int64_t q_st, q_sh, k_sb, k_sh, k_st, w_sb, w_sh;
+  int64_t span;
   int32_t num_seqs, num_q_heads, num_kv_heads, max_blocks, group;
-  uint32_t group_inv;  // ceil(2^20 / G): r / G = r * group_inv >> 20 for r < 288
+  int32_t parts;      // of a workgroup's tiles
+  int32_t wave_keys;  // stream: keys of a wave, a multiple of 32, at most 1024
+  uint32_t group_inv; // ceil(2^20 / G): r / G = r * group_inv >> 20 for r < 288
   float inv_scale, scale_log2;
   int32_t accumulate;
 };
@@ -68,24 +90,148 @@ __device__ __forceinline__ bf16x8 three_terms(float x, bool here) {
   return v;
 }
 
+__device__ __forceinline__ bf16x8 all_of(float x) {
+  bf16x8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (__bf16)x;
+  return v;
+}
+
+// the sum of a lane's 16 weights of one key; pos: position of pair `lane % 32` of the tile
+__device__ __forceinline__ float key_sum(const f32x16& s, float scale_log2, bool masked, int pos, int key, int hl) {
+  float w[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(s[i] * scale_log2);
+  if (masked) {
+    // register i of a lane: pair (i/4)*8 + hl*4 + i%4
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = __shfl(pos, (i >> 2) * 8 + hl * 4 + (i & 3)) >= key ? w[i] : 0.0f;
+  }
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < d; ++i) w[i] += w[i + d];
+  return w[0];
+}
+
+// ---- up to 32 pairs ----
+
 template <int D>
-__global__ __launch_bounds__(256, 2) void msa_kv_weights_kernel(WeightsParams p) {
+__global__ __launch_bounds__(256, 3) void msa_kv_weights_stream_kernel(WeightsParams p) {
   const int per_chunk = p.num_seqs * p.num_kv_heads;
   const int chunk = blockIdx.x / per_chunk, rest = blockIdx.x - chunk * per_chunk;
   const int seq = rest / p.num_kv_heads, kv_head = rest - seq * p.num_kv_heads;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, hl = lane >> 5, ln = lane & 31;
   const int row0 = p.seq_row0[seq], nrows = p.seq_row0[seq + 1] - row0;
-  if (nrows == 0) return;
+  const int G = p.group, n = nrows * G;
+  if (n == 0 || n > kPairs) return;
   const int last = p.row_pos[row0 + nrows - 1];
-  const int k0 = chunk * kGroupKeys + wave * kWaveKeys;
-  if (k0 > last) return;
-  const int G = p.group;
+  const int64_t begin = ((int64_t)chunk * 4 + wave) * p.wave_keys;
+  if (begin > last) return;
+  const int k0 = (int)begin, k1 = min(k0 + p.wave_keys, last + 1);
 
-  // B operand: key k0 + kt*32 + ln, channels kk*16 + hl*8 .. +8
-  bf16x8 kf[2][D / 16], ones;
+  // the wave's block ids, one a lane
+  const int32_t* table = p.block_table + (int64_t)seq * p.max_blocks + (k0 >> 4);
+  const int32_t ids = k0 + lane * kBlockSize < k1 ? table[lane] : 0;
+
+  const int dt = (int)((uint32_t)ln * p.group_inv >> 20);
+  const bool valid = ln < n;
+  const int tok = row0 + (valid ? dt : 0), head = kv_head * G + (valid ? ln - dt * G : 0);
+  const int pos = p.row_pos[tok];
+  bf16x8 qf[D / 16];
+  const uint16_t* src = p.q + (int64_t)tok * p.q_st + (int64_t)head * p.q_sh + hl * 8;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.0f;
+  for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
+  float l = p.lse[(int64_t)tok * p.num_q_heads + head];
+  if (!valid || l == -__builtin_inff()) l = __builtin_inff();
+  const bf16x8 lf = three_terms(-l * p.inv_scale, hl == 0), ones = all_of(1.0f);
+  if (!valid) {  // (its scores are -inf whatever Q holds, but for NaN)
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) qf[kk] = all_of(0.0f);
+  }
+  const int first_pos = __builtin_amdgcn_readfirstlane(pos);
+  float* out = p.weights + (int64_t)seq * p.w_sb + (int64_t)kv_head * p.w_sh;
+
+  // B operand: key base + ln, channels kk*16 + hl*8 .. +8 (a key behind the last one reads the last one's row)
+  const uint16_t* kbase = p.k + (int64_t)kv_head * p.k_sh + hl * 8;
+  auto load = [&](bf16x8 (&kf)[D / 16], float& old, int base) __attribute__((always_inline)) {
+    const int key = min(base + ln, k1 - 1);
+    const int b = (base - k0) >> 4;
+    const int32_t id0 = __builtin_amdgcn_readlane(ids, b), id1 = __builtin_amdgcn_readlane(ids, min(b + 1, 63));
+    const int32_t blk = (key - base) >> 4 ? id1 : id0;
+    const uint16_t* at = kbase + (int64_t)blk * p.k_sb + (int64_t)(key & 15) * p.k_st;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) kf[kk] = *reinterpret_cast<const bf16x8*>(at + kk * 16);
+    old = p.accumulate ? out[key] : 0.0f;
+  };
+  bf16x8 kf[2][D / 16];
+  float old[2];
+  auto tile = [&](bf16x8 (&now)[D / 16], float was, bf16x8 (&then)[D / 16], float& next, int base)
+      __attribute__((always_inline)) {
+    if (base + 32 < k1) load(then, next, base + 32);
+    f32x16 s = {};
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lf, ones, s, 0, 0, 0);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[kk], now[kk], s, 0, 0, 0);
+    float sum = key_sum(s, p.scale_log2, first_pos < base + 31, pos, base + ln, hl);
+    sum += __shfl_xor(sum, 32);
+    if (hl == 0 && base + ln < k1) out[base + ln] = was + sum;
+  };
+  load(kf[0], old[0], k0);
+  for (int base = k0; base < k1; base += 64) {
+    tile(kf[0], old[0], kf[1], old[1], base);
+    if (base + 32 < k1) tile(kf[1], old[1], kf[0], old[0], base + 32);
+  }
+}
+
+// ---- more ----
+
+// 16 or 4 bytes a lane from global memory straight into LDS at lds + 16 (4) * lane
+// (M0 holds the wave's base); completion is tracked by vmcnt, which the
+// kernel waits for itself
+__device__ __forceinline__ void copy16(const void* src, void* lds) {
+  const uint32_t l = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(l) : "memory");
+}
+__device__ __forceinline__ void copy4(const void* src, void* lds) {
+  const uint32_t l = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "{m0}"(l) : "memory");
+}
+
+// s_waitcnt's operand: at most n loads or copies outstanding
+constexpr int wait_loads(int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); }
+
+template <int D>
+struct QRing {
+  static constexpr int kTile = kPairs * D * 2;
+  char q[kRing][kTile];             // [pair][D], 16-byte chunks XOR-swizzled
+  uint32_t more[kRing][4][64];      // for each wave: 32 lse, 32 positions
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 3) void msa_kv_weights_tiles_kernel(WeightsParams p) {
+  __shared__ __attribute__((aligned(1024))) QRing<D> ring;
+  const int per_chunk = p.num_seqs * p.num_kv_heads * p.parts;
+  const int chunk = blockIdx.x / per_chunk;
+  int rest = blockIdx.x - chunk * per_chunk;
+  const int part = rest / (p.num_seqs * p.num_kv_heads);
+  rest -= part * (p.num_seqs * p.num_kv_heads);
+  const int seq = rest / p.num_kv_heads, kv_head = rest - seq * p.num_kv_heads;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, hl = lane >> 5, ln = lane & 31;
+  const int row0 = p.seq_row0[seq], nrows = p.seq_row0[seq + 1] - row0;
+  const int G = p.group, n = nrows * G;
+  if (n <= kPairs) return;
+  const int32_t* row_pos = p.row_pos + row0;
+  const int last = row_pos[nrows - 1];
+  const int group0 = chunk * kGroupKeys;
+  if (group0 > last) return;
+  const int k0 = group0 + wave * kWaveKeys;
+
+  // B operand: key k0 + kt*32 + ln, channels kk*16 + hl*8 .. +8; keys behind the last one are 0
+  bf16x8 kf[2][D / 16];
+  const bf16x8 ones = all_of(1.0f);
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt) {
     const int key = k0 + kt * 32 + ln;
@@ -93,77 +239,173 @@ __global__ __launch_bounds__(256, 2) void msa_kv_weights_kernel(WeightsParams p)
     const uint16_t* src = p.k + (int64_t)blk * p.k_sb + (int64_t)kv_head * p.k_sh + (int64_t)(key & 15) * p.k_st + hl * 8;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
-      if (key <= last) {
-        kf[kt][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) kf[kt][kk][j] = (__bf16)0.0f;
-      }
+      kf[kt][kk] = all_of(0.0f);
+      if (key <= last) kf[kt][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
     }
   }
 
-  const int n = nrows * G;  // (row, head) pairs
-  float sum[2] = {0.0f, 0.0f};
-  for (int base = (n - 1) / 32 * 32; base >= 0; base -= 32) {
-    const int t0 = base / G;  // uniform
-    const uint32_t off = (uint32_t)(base - t0 * G + ln);
-    const int dt = (int)(off * p.group_inv >> 20);
-    const bool valid = base + ln < n;
-    const int tok = row0 + t0 + dt, head = kv_head * G + (int)off - dt * G;
-    const int pos = valid ? p.row_pos[tok] : 0x7fffffff;
-    const int nvalid = n - base < 32 ? n - base : 32;
-    if (__builtin_amdgcn_readlane(pos, nvalid - 1) < k0) break;
-    bf16x8 qf[D / 16];
-    float l = __builtin_inff();
-    if (valid) {
-      const uint16_t* src = p.q + (int64_t)tok * p.q_st + (int64_t)head * p.q_sh + hl * 8;
-#pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
-      l = p.lse[(int64_t)tok * p.num_q_heads + head];
-      if (l == -__builtin_inff()) l = __builtin_inff();
+  // the first row that sees the workgroup's first key: 64 rows probed at once
+  int lo = 0, hi = nrows - 1;  // it is in [lo, hi]
+  while (lo < hi) {
+    const int step = (hi - lo + 63) / 64;
+    const int at = lo + lane * step;  // the probes cut [lo, hi) into runs of `step`
+    const int before = __popcll(__ballot(at < hi && row_pos[at < hi ? at : hi] < group0));
+    if (before == 0) {
+      hi = lo;
     } else {
+      const int from = lo + (before - 1) * step + 1;
+      hi = min(hi, lo + before * step);
+      lo = from;
+    }
+  }
+  const int tiles_all = (n + kPairs - 1) / kPairs, tile0 = lo * G / kPairs;
+  const int t_begin = tile0 + (int)((int64_t)(tiles_all - tile0) * part / p.parts);
+  const int t_end = tile0 + (int)((int64_t)(tiles_all - tile0) * (part + 1) / p.parts);
+
+  // Copies: a wave's share of a tile is 8 pairs (two copies, or one at d = 64, of 16 bytes a
+  // lane), and lse and position of all 32.  Pairs behind the last one read the last one's.
+  constexpr int kChunks = D / 8;           // 16-byte chunks of a pair
+  constexpr int kPerCopy = 64 / kChunks;   // pairs of a copy
+  constexpr int kCopies = 8 / kPerCopy;
+  auto swizzle = [](int r) { return (D == 128 ? r : r >> 1) & (kChunks - 1); };
+  // the next tile to copy: its first pair, as a row and a place in the group (a division once, here)
+  const int step_rows = kPairs / G, step_heads = kPairs - step_rows * G;
+  int next = t_begin, next_row = t_begin * kPairs / G, next_head = t_begin * kPairs - next_row * G;
+  auto copy = [&]() __attribute__((always_inline)) {
+    const int slot = next & (kRing - 1);
+    const int most = n - 1 - min(next, t_end - 1) * kPairs;  // the tile's last pair, if not 31
+    auto pair_at = [&](int r, int& tok, int& head) __attribute__((always_inline)) {
+      const uint32_t off = (uint32_t)(next_head + min(r, most));
+      const int dt = (int)(off * p.group_inv >> 20);
+      tok = next_row + dt;
+      head = kv_head * G + (int)off - dt * G;
+    };
+    int tok, head;
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) {
+      const int r0 = wave * 8 + c * kPerCopy, r = r0 + lane / kChunks;
+      pair_at(r, tok, head);
+      copy16(p.q + (int64_t)(row0 + tok) * p.q_st + (int64_t)head * p.q_sh + ((lane % kChunks) ^ swizzle(r)) * 8,
+             ring.q[__builtin_amdgcn_readfirstlane(slot)] + r0 * D * 2);
+    }
+    pair_at(ln, tok, head);
+    const void* lse = p.lse + (int64_t)(row0 + tok) * p.num_q_heads + head;
+    const void* pos = row_pos + tok;
+    copy4(hl ? pos : lse, ring.more[__builtin_amdgcn_readfirstlane(slot)][wave]);
+    ++next;
+    if (next < t_end) {  // (behind the last tile it is copied again, so that each step waits for as many)
+      next_row += step_rows;
+      next_head += step_heads;
+      if (next_head >= G) {
+        next_head -= G;
+        ++next_row;
+      }
+    }
+  };
+  constexpr int kEach = kCopies + 1;  // copies of a wave and tile
+
+  float sum[2] = {0.0f, 0.0f};
+  if (t_begin < t_end) {
+    __builtin_amdgcn_s_waitcnt(wait_loads(0));  // K has arrived (the compiler would wait for it, and for all copies, in the loop)
+    copy();
+    copy();
+    copy();
+    for (int t = t_begin; t < t_end; ++t) {
+      // tile t has arrived once no more than the copies of two tiles are outstanding; behind the
+      // barrier every wave's share has, and tile t - 1 is read
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kEach) : "memory");
+      copy();
+      const int slot = t & (kRing - 1);
+      const uint32_t* more = ring.more[slot][wave];
+      float l = __uint_as_float(more[ln]);
+      const int pos = (int)more[32 + ln];
+      if (t * kPairs + ln >= n || l == -__builtin_inff()) l = __builtin_inff();
+      const int first_pos = __builtin_amdgcn_readfirstlane(pos);
+      if (__builtin_amdgcn_readlane(pos, 31) < k0) continue;  // all of the tile's rows lie before the wave's keys
+      const bf16x8 lf = three_terms(-l * p.inv_scale, hl == 0);
+      bf16x8 qf[D / 16];
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk)
+        qf[kk] = *reinterpret_cast<const bf16x8*>(ring.q[slot] + ln * D * 2 + (((kk * 2 + hl) ^ swizzle(ln)) * 16));
+      const bool masked = first_pos < k0 + kWaveKeys - 1;
+      f32x16 s[2] = {};
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lf, ones, s[kt], 0, 0, 0);
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) qf[kk][j] = (__bf16)0.0f;
+        for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[kk], kf[kt][kk], s[kt], 0, 0, 0);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) sum[kt] += key_sum(s[kt], p.scale_log2, masked, pos, k0 + kt * 32 + ln, hl);
     }
-    const bf16x8 lf = three_terms(-l * p.inv_scale, hl == 0);
-    const bool masked = __builtin_amdgcn_readfirstlane(pos) < k0 + kWaveKeys - 1;
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      f32x16 s = {};
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lf, ones, s, 0, 0, 0);
-#pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[kk], kf[kt][kk], s, 0, 0, 0);
-      // register i of a lane: pair base + (i/4)*8 + hl*4 + i%4, key k0 + kt*32 + ln
-      float w[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(s[i] * p.scale_log2);
-      if (masked) {
-        const int key = k0 + kt * 32 + ln;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = __shfl(pos, (i >> 2) * 8 + hl * 4 + (i & 3));
-          w[i] = at >= key ? w[i] : 0.0f;
-        }
-      }
-#pragma unroll
-      for (int d = 8; d > 0; d >>= 1)
-#pragma unroll
-        for (int i = 0; i < d; ++i) w[i] += w[i + d];
-      sum[kt] += w[0];
-    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // copies under way end before the workgroup's LDS does
   }
-  // the two lanes of a key
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt) {
     const float total = sum[kt] + __shfl_xor(sum[kt], 32);
     const int key = k0 + kt * 32 + ln;
-    if (hl == 0 && key <= last) {
+    if (hl != 0 || key > last) continue;
+    if (p.parts == 1) {
       float* out = p.weights + (int64_t)seq * p.w_sb + (int64_t)kv_head * p.w_sh + key;
       *out = p.accumulate ? *out + total : total;
+    } else {
+      p.sums[(((int64_t)part * p.num_seqs + seq) * p.num_kv_heads + kv_head) * p.span + key] = total;
     }
   }
+}
+
+// adds up the parts' sums, in order
+__global__ __launch_bounds__(256) void msa_kv_weights_join_kernel(WeightsParams p) {
+  const int per_chunk = p.num_seqs * p.num_kv_heads;
+  const int chunk = blockIdx.x / per_chunk, rest = blockIdx.x - chunk * per_chunk;
+  const int seq = rest / p.num_kv_heads, kv_head = rest - seq * p.num_kv_heads;
+  const int row0 = p.seq_row0[seq], nrows = p.seq_row0[seq + 1] - row0;
+  if (nrows * p.group <= kPairs) return;
+  const int key = chunk * 256 + (int)threadIdx.x;
+  if (key > p.row_pos[row0 + nrows - 1]) return;
+  float* out = p.weights + (int64_t)seq * p.w_sb + (int64_t)kv_head * p.w_sh + key;
+  const float old = p.accumulate ? *out : 0.0f;
+  const float* src = p.sums + ((int64_t)seq * p.num_kv_heads + kv_head) * p.span + key;
+  float x[kMostParts], total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kMostParts; ++i)
+    x[i] = i < p.parts ? src[(int64_t)i * p.num_seqs * p.num_kv_heads * p.span] : 0.0f;
+#pragma unroll
+  for (int i = 0; i < kMostParts; ++i) total += x[i];
+  *out = old + total;
+}
+
+// What a plan's call launches.
+struct Shape {
+  int64_t stream_keys = 0;  // keys x KV heads of sequences of up to 32 pairs
+  int64_t longest_stream = 0, longest_tiles = 0;  // keys
+  int64_t parts = 1, span = 0;
+};
+Shape shape_of(const HostPlan& hp) {
+  Shape s;
+  int64_t groups = 0, most_tiles = 0;
+  for (size_t b = 0; b < hp.seq_blocks.size(); ++b) {
+    const int64_t pairs = (int64_t)(hp.seq_row0[b + 1] - hp.seq_row0[b]) * hp.group;
+    const int64_t keys = (int64_t)hp.seq_blocks[b] * kBlockSize;
+    if (pairs == 0) continue;
+    if (pairs <= kPairs) {
+      s.stream_keys += keys * hp.shape.num_kv_heads;
+      s.longest_stream = std::max(s.longest_stream, keys);
+    } else {
+      s.longest_tiles = std::max(s.longest_tiles, keys);
+      groups += (keys + kGroupKeys - 1) / kGroupKeys * hp.shape.num_kv_heads;
+      most_tiles = std::max(most_tiles, (pairs + kPairs - 1) / kPairs);
+    }
+  }
+  if (groups > 0) {
+    // some 2048 workgroups, with 16 tiles in a part
+    s.parts = std::min({(2048 + groups - 1) / groups, std::max<int64_t>(1, most_tiles / 16), (int64_t)kMostParts});
+    s.span = (s.longest_tiles + kGroupKeys - 1) / kGroupKeys * kGroupKeys;
+  }
+  return s;
+}
+size_t workspace_of(const HostPlan& hp, const Shape& s) {
+  return s.parts == 1 ? 0 : (size_t)(s.parts * hp.shape.num_seqs * hp.shape.num_kv_heads * s.span) * sizeof(float);
 }
 
 msa_status fail(const char* who, msa_status st, const std::string& msg) {
@@ -178,7 +420,7 @@ bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p)
 
 extern "C" msa_status msa_kv_weights_workspace(msa_plan_t plan, size_t* bytes) {
   if (!plan || !bytes) return msa::fail("msa_kv_weights_workspace", MSA_ERR_INVALID_ARG, "null argument");
-  *bytes = 0;
+  *bytes = plan->hp.total_q == 0 ? 0 : msa::workspace_of(plan->hp, msa::shape_of(plan->hp));
   return MSA_OK;
 }
 
@@ -187,7 +429,6 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
                                      int32_t accumulate, void* workspace, size_t workspace_bytes, void* hip_stream) {
   const char* who = "msa_kv_weights";
   const auto invalid = [&](const std::string& msg) { return msa::fail(who, MSA_ERR_INVALID_ARG, msg); };
-  (void)workspace, (void)workspace_bytes;
   if (!plan) return invalid("null plan");
   if (plan->hp.has_trees) return msa::fail(who, MSA_ERR_UNSUPPORTED, "the plan was built by msa_plan_tree");
   if (stride_seq < 0 || stride_head < 0) return invalid("strides must be >= 0");
@@ -201,11 +442,18 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
       !msa::aligned(weights, 4))
     return invalid("q and k_cache must be 16-byte, the others 4-byte aligned");
   const msa_shape& s = hp.shape;
-  int64_t longest = 0;
-  for (int32_t nb : hp.seq_blocks) longest = longest < nb ? nb : longest;
-  const int64_t chunks = (longest * msa::kBlockSize + msa::kGroupKeys - 1) / msa::kGroupKeys;
-  const int64_t groups = chunks * s.num_seqs * s.num_kv_heads;
-  if (hp.total_q * hp.group >= ((int64_t)1 << 31) || groups >= ((int64_t)1 << 31))
+  const msa::Shape launch = msa::shape_of(hp);
+  const size_t need = msa::workspace_of(hp, launch);
+  if (need > workspace_bytes || (need > 0 && (!workspace || !msa::aligned(workspace, 16))))
+    return invalid("workspace must be 16-byte aligned and hold " + std::to_string(need) + " bytes");
+  // stream: two rounds of the waves that the card holds (12 a CU), 64 to 1024 keys each
+  int64_t wave_keys = launch.stream_keys / (2 * 12 * msa::kCUs) / 64 * 64;
+  wave_keys = wave_keys < 64 ? 64 : wave_keys > 1024 ? 1024 : wave_keys;
+  const int64_t heads = (int64_t)s.num_seqs * s.num_kv_heads;
+  const int64_t stream_groups = (launch.longest_stream + 4 * wave_keys - 1) / (4 * wave_keys) * heads;
+  const int64_t chunks = (launch.longest_tiles + msa::kGroupKeys - 1) / msa::kGroupKeys;
+  if (hp.total_q * hp.group >= ((int64_t)1 << 31) - 64 || stream_groups >= ((int64_t)1 << 31) ||
+      chunks * heads * launch.parts >= ((int64_t)1 << 31))
     return msa::fail(who, MSA_ERR_UNSUPPORTED, "too many rows or keys for one launch");
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev != plan->device)
@@ -234,10 +482,33 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
   p.inv_scale = 1.0f / s.scale;
   p.scale_log2 = s.scale * 1.4426950408889634f;
   p.accumulate = accumulate;
+  p.wave_keys = (int32_t)wave_keys;
+  p.parts = (int32_t)launch.parts;
+  p.span = launch.span;
+  p.sums = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  if (s.head_dim == 128)
-    hipLaunchKernelGGL(msa::msa_kv_weights_kernel<128>, dim3((uint32_t)groups), dim3(256), 0, st, p);
-  else
-    hipLaunchKernelGGL(msa::msa_kv_weights_kernel<64>, dim3((uint32_t)groups), dim3(256), 0, st, p);
-  return msa::launched(who, "weights", (int)hipGetLastError());
+  const bool d128 = s.head_dim == 128;
+  if (stream_groups > 0) {
+    const dim3 grid((uint32_t)stream_groups);
+    if (d128)
+      hipLaunchKernelGGL(msa::msa_kv_weights_stream_kernel<128>, grid, dim3(256), 0, st, p);
+    else
+      hipLaunchKernelGGL(msa::msa_kv_weights_stream_kernel<64>, grid, dim3(256), 0, st, p);
+    const msa_status rc = msa::launched(who, "stream", (int)hipGetLastError());
+    if (rc != MSA_OK) return rc;
+  }
+  if (chunks > 0) {
+    const dim3 grid((uint32_t)(chunks * heads * launch.parts));
+    if (d128)
+      hipLaunchKernelGGL(msa::msa_kv_weights_tiles_kernel<128>, grid, dim3(256), 0, st, p);
+    else
+      hipLaunchKernelGGL(msa::msa_kv_weights_tiles_kernel<64>, grid, dim3(256), 0, st, p);
+    const msa_status rc = msa::launched(who, "tiles", (int)hipGetLastError());
+    if (rc != MSA_OK) return rc;
+  }
+  if (launch.parts > 1) {
+    hipLaunchKernelGGL(msa::msa_kv_weights_join_kernel, dim3((uint32_t)(chunks * heads)), dim3(256), 0, st, p);
+    return msa::launched(who, "join", (int)hipGetLastError());
+  }
+  return MSA_OK;
 }
