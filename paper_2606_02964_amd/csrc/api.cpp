@@ -177,7 +177,11 @@ msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq
     const size_t off_seq = off_heads + align_up(n_wg * sizeof(msa::WgHead), 256);
     const size_t off_row_tree = off_seq + align_up(n_seq, 256);
     const size_t off_trees = off_row_tree + align_up(n_row_tree, 256);
-    const size_t bytes = std::max<size_t>(off_trees + n_trees, 256);
+    const size_t n_weights = hp.weights.size() * sizeof(msa::WeightsItem);
+    const size_t n_joins = hp.weight_joins.size() * sizeof(msa::WeightsJoin);
+    const size_t off_weights = off_trees + align_up(n_trees, 256);
+    const size_t off_joins = off_weights + align_up(n_weights, 256);
+    const size_t bytes = std::max<size_t>(off_joins + n_joins, 256);
     try {
       plan->staging.assign(bytes, 0);
     } catch (const std::bad_alloc&) {
@@ -191,6 +195,8 @@ msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq
     if (n_seq) std::memcpy(plan->staging.data() + off_seq, hp.seq_row0.data(), n_seq);
     if (n_row_tree) std::memcpy(plan->staging.data() + off_row_tree, hp.row_tree.data(), n_row_tree);
     if (n_trees) std::memcpy(plan->staging.data() + off_trees, hp.trees.data(), n_trees);
+    if (n_weights) std::memcpy(plan->staging.data() + off_weights, hp.weights.data(), n_weights);
+    if (n_joins) std::memcpy(plan->staging.data() + off_joins, hp.weight_joins.data(), n_joins);
     for (size_t i = 0; i < n_wg; ++i) {
       msa::WgHead h{};
       const int32_t first = hp.wg_ptr[i], end = hp.wg_ptr[i + 1];
@@ -226,6 +232,8 @@ msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq
     plan->d_seq_row0 = reinterpret_cast<const int32_t*>(plan->dev + off_seq);
     if (with_trees) plan->d_row_tree = reinterpret_cast<const msa::RowTree*>(plan->dev + off_row_tree);
     plan->d_trees = reinterpret_cast<const msa::TreeSpan*>(plan->dev + off_trees);
+    plan->d_weights = reinterpret_cast<const msa::WeightsItem*>(plan->dev + off_weights);
+    plan->d_weight_joins = reinterpret_cast<const msa::WeightsJoin*>(plan->dev + off_joins);
   }
   *out = plan;
   return MSA_OK;

@@ -91,6 +91,96 @@ struct Unit {
   int32_t seq, kv_head, row0, nrows, kv_hi;
 };
 
+// Key weights: the tiles of 32 (row, head) pairs that see each 256 keys of a
+// sequence, cut into items of up to `part` tiles.  An item costs some 5 us besides
+// its tiles (about 1 us each, two workgroups on a CU).  A launch of few rounds of
+// workgroups takes as long as that many of the longest items, one of many rounds a
+// CU's share of all items and half an item, as it ends unevenly.  The part is the
+// one of least such cost, among lengths a third apart and the shortest that need one,
+// two or three rounds (8 KV heads: one prompt of 4096 93 us in one round, 105 us in
+// items of 24 tiles; of 8192 356 us in two full rounds, 395 us in items of 160;
+// 8 prompts of 2048 217 us in items of 32, 260 us in one round, whose longest item is
+// twice the mean).  Items in the order of their first tile: workgroups that run
+// together read the same Q, from their XCD's L2, which they would not in long items
+// (one prompt of 16384 1166 us in items of 150 tiles, 1484 us in one round of
+// 1057): kMost tiles at most.
+void plan_weights(HostPlan* plan) {
+  constexpr int64_t kShortest = 8, kMost = 160, kSlots = 2 * kCUs, kItemTiles = 5, kRounds = 3;
+  HostPlan& P = *plan;
+  const int64_t G = P.group, B = P.shape.num_seqs, heads = P.shape.num_kv_heads;
+  struct Chunk {
+    int32_t seq, key0, first, tiles, last;
+  };
+  std::vector<Chunk> chunks;
+  int64_t work = 0, longest = kShortest;  // tiles in all, of a chunk at most
+  for (int64_t b = 0; b < B; ++b) {
+    const int32_t lo = P.seq_row0[(size_t)b], hi = P.seq_row0[(size_t)b + 1];
+    const int64_t pairs = (int64_t)(hi - lo) * G;
+    if (pairs == 0) continue;
+    const int32_t last = P.row_pos[(size_t)hi - 1];
+    if (pairs <= kPairs) {
+      P.stream_keys += last + 1;
+      P.longest_stream = std::max<int64_t>(P.longest_stream, last + 1);
+      continue;
+    }
+    if (pairs >= (int64_t)1 << 31) continue;  // (such a call is refused)
+    auto row = P.row_pos.begin() + lo;
+    for (int64_t key0 = 0; key0 <= last; key0 += kGroupKeys) {
+      row = std::lower_bound(row, P.row_pos.begin() + hi, (int32_t)key0);
+      const int64_t first = (int64_t)(row - P.row_pos.begin() - lo) * G / kPairs;
+      const int64_t tiles = (pairs + kPairs - 1) / kPairs;
+      chunks.push_back(Chunk{(int32_t)b, (int32_t)key0, (int32_t)first, (int32_t)tiles, last});
+      work += (tiles - first) * heads;
+      longest = std::max(longest, tiles - first);
+    }
+  }
+  if (chunks.empty()) return;
+  auto items_of = [&](int64_t len) {
+    int64_t items = 0;
+    for (const Chunk& c : chunks) items += (c.tiles - c.first + len - 1) / len * heads;
+    return items;
+  };
+  auto cost_of = [&](int64_t len) {
+    const int64_t items = items_of(len), rounds = (items + kSlots - 1) / kSlots;
+    return rounds <= kRounds ? (double)(rounds * (len + kItemTiles))
+                             : (double)(work + items * kItemTiles) / kSlots + 0.5 * (double)(len + kItemTiles);
+  };
+  int64_t part = std::min(longest, kMost);
+  double least = cost_of(part);
+  auto consider = [&](int64_t len) {
+    const double cost = cost_of(len);
+    if (cost < least) {
+      least = cost;
+      part = len;
+    }
+  };
+  for (int64_t rounds = 1; rounds <= kRounds; ++rounds) {  // the shortest that needs no more rounds
+    int64_t len = kShortest;
+    for (int64_t most = std::min(longest, kMost); len < most;) {
+      const int64_t mid = (len + most) / 2;
+      if (items_of(mid) <= rounds * kSlots) most = mid; else len = mid + 1;
+    }
+    consider(len);
+  }
+  for (int64_t len = kShortest; len < std::min(longest, kMost); len += len / 3) consider(len);
+  for (const Chunk& c : chunks) {
+    const int64_t len = c.tiles - c.first, parts = (len + part - 1) / part;
+    const int32_t slot0 = P.weight_slots;
+    if (parts > 1) {
+      P.weight_joins.push_back(WeightsJoin{c.seq, c.key0, slot0, (int32_t)parts});
+      P.weight_slots += (int32_t)parts;
+    }
+    for (int64_t i = 0; i < parts; ++i)
+      P.weights.push_back(WeightsItem{c.seq, c.key0, P.seq_row0[(size_t)c.seq],
+                                      P.seq_row0[(size_t)c.seq + 1] - P.seq_row0[(size_t)c.seq],
+                                      (int32_t)(c.first + len * i / parts), (int32_t)(c.first + len * (i + 1) / parts),
+                                      parts > 1 ? (int32_t)(slot0 + i) : -1, c.last});
+  }
+  std::stable_sort(P.weights.begin(), P.weights.end(), [](const WeightsItem& a, const WeightsItem& b) {
+    return a.seq != b.seq ? a.seq < b.seq : a.tile0 < b.tile0;
+  });
+}
+
 }  // namespace
 
 msa_status check_shape(const msa_shape& s, std::string* err) {
@@ -661,6 +751,8 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
           WorkItem{u.seq, u.kv_head, u.row0, u.nrows, p.lo, p.hi, slot, p.wg};
     }
   }
+
+  if (!with_trees) plan_weights(&P);
 
   // figures
   const double hq = s.num_q_heads;

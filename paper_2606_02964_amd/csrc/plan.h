@@ -7,6 +7,7 @@
 #include "append.h"
 #include "msa.h"
 #include "msa_internal.h"
+#include "weights.h"
 
 namespace msa {
 
@@ -25,6 +26,10 @@ struct HostPlan {
   std::vector<MergeItem> merge;
   std::vector<AppendItem> append; // one per (segment, cache block) slice
   std::vector<int32_t> seq_row0;  // [num_seqs + 1] first packed row of each sequence
+  std::vector<WeightsItem> weights;      // key weights of sequences of more than kPairs pairs
+  std::vector<WeightsJoin> weight_joins;
+  int32_t weight_slots = 0;
+  int64_t stream_keys = 0, longest_stream = 0;  // key weights of the others: keys in all, of the longest
   bool has_trees = false;         // built by msa_plan_tree (it may hold no tree all the same)
   std::vector<RowTree> row_tree;  // [total_q] if has_trees
   std::vector<TreeSpan> trees;    // one per tree segment

@@ -25,11 +25,11 @@
 //   and streams the pairs' Q, lse and positions through a ring of four tiles in
 //   LDS, filled by direct copies that run three tiles ahead (each wave its share,
 //   one barrier a tile).  Read by every wave for itself, Q took four times the reads,
-//   each over 32 cache lines.  Rows ascend in position: the first tile is the one
-//   that holds the first row to see the workgroup's keys.  Where a launch would
-//   hold few workgroups, each one's tiles are split; the parts' sums go through
-//   the workspace and are added in order.  Bound by MFMAs (18 of 32 cycles a tile
-//   of 32 x 64) and exponentials (32 of 16 cycles) about equally.
+//   each over 32 cache lines.  The plan deals out the tiles (see plan_weights); where
+//   keys have several items, their sums go through the workspace and are added in
+//   order.  Bound by vector instructions and MFMAs: a tile of 32 pairs x 64 keys
+//   takes a wave 17 MFMAs of 32 cycles and about 150 vector instructions, 32 of them
+//   exponentials of 8 cycles, beside them.
 // Sums are in fp32, 16 rows of a tile added pairwise and then to the running sum;
 // no atomics, so equal calls give equal bits.
 #include <hip/hip_runtime.h>
@@ -51,11 +51,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 typedef __attribute__((address_space(3))) void lds_void_t;
 
-constexpr int kPairs = 32;                 // (row, head) pairs of a tile
-constexpr int kWaveKeys = 64;
-constexpr int kGroupKeys = 4 * kWaveKeys;  // keys of a workgroup (tiles)
-constexpr int kRing = 4;                   // tiles in LDS
-constexpr int kMostParts = 16;
+constexpr int kWaveKeys = kGroupKeys / 4;
+constexpr int kRing = 4;  // tiles in LDS
 
 struct WeightsParams {
   const uint16_t* q;
@@ -65,11 +62,11 @@ struct WeightsParams {
   const int32_t* seq_row0;
   const float* lse;
   float* weights;
-  float* sums;  // [parts][sequences][KV heads][span], parts > 1
+  float* sums;  // [slots][KV heads][kGroupKeys]
+  const WeightsItem* items;
+  const WeightsJoin* joins;
   int64_t q_st, q_sh, k_sb, k_sh, k_st, w_sb, w_sh;
-  int64_t span;
   int32_t num_seqs, num_q_heads, num_kv_heads, max_blocks, group;
-  int32_t parts;      // of a workgroup's tiles
   int32_t wave_keys;  // stream: keys of a wave, a multiple of 32, at most 1024
   uint32_t group_inv; // ceil(2^20 / G): r / G = r * group_inv >> 20 for r < 288
   float inv_scale, scale_log2;
@@ -210,57 +207,17 @@ struct QRing {
 };
 
 template <int D>
-__global__ __launch_bounds__(256, 3) void msa_kv_weights_tiles_kernel(WeightsParams p) {
+__global__ __launch_bounds__(256, 2) void msa_kv_weights_tiles_kernel(WeightsParams p) {
   __shared__ __attribute__((aligned(1024))) QRing<D> ring;
-  const int per_chunk = p.num_seqs * p.num_kv_heads * p.parts;
-  const int chunk = blockIdx.x / per_chunk;
-  int rest = blockIdx.x - chunk * per_chunk;
-  const int part = rest / (p.num_seqs * p.num_kv_heads);
-  rest -= part * (p.num_seqs * p.num_kv_heads);
-  const int seq = rest / p.num_kv_heads, kv_head = rest - seq * p.num_kv_heads;
+  const uint32_t item = blockIdx.x / (uint32_t)p.num_kv_heads;
+  const int kv_head = (int)(blockIdx.x - item * (uint32_t)p.num_kv_heads);
+  const WeightsItem it = p.items[item];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, hl = lane >> 5, ln = lane & 31;
-  const int row0 = p.seq_row0[seq], nrows = p.seq_row0[seq + 1] - row0;
-  const int G = p.group, n = nrows * G;
-  if (n <= kPairs) return;
+  const int row0 = it.row0, last = it.last, t_begin = it.tile0, t_end = it.tile1;
+  const int G = p.group, n = it.nrows * G, tiles_all = (n + kPairs - 1) / kPairs;
   const int32_t* row_pos = p.row_pos + row0;
-  const int last = row_pos[nrows - 1];
-  const int group0 = chunk * kGroupKeys;
-  if (group0 > last) return;
-  const int k0 = group0 + wave * kWaveKeys;
-
-  // B operand: key k0 + kt*32 + ln, channels kk*16 + hl*8 .. +8; keys behind the last one are 0
-  bf16x8 kf[2][D / 16];
-  const bf16x8 ones = all_of(1.0f);
-#pragma unroll
-  for (int kt = 0; kt < 2; ++kt) {
-    const int key = k0 + kt * 32 + ln;
-    const int32_t blk = key <= last ? p.block_table[(int64_t)seq * p.max_blocks + (key >> 4)] : 0;
-    const uint16_t* src = p.k + (int64_t)blk * p.k_sb + (int64_t)kv_head * p.k_sh + (int64_t)(key & 15) * p.k_st + hl * 8;
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) {
-      kf[kt][kk] = all_of(0.0f);
-      if (key <= last) kf[kt][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
-    }
-  }
-
-  // the first row that sees the workgroup's first key: 64 rows probed at once
-  int lo = 0, hi = nrows - 1;  // it is in [lo, hi]
-  while (lo < hi) {
-    const int step = (hi - lo + 63) / 64;
-    const int at = lo + lane * step;  // the probes cut [lo, hi) into runs of `step`
-    const int before = __popcll(__ballot(at < hi && row_pos[at < hi ? at : hi] < group0));
-    if (before == 0) {
-      hi = lo;
-    } else {
-      const int from = lo + (before - 1) * step + 1;
-      hi = min(hi, lo + before * step);
-      lo = from;
-    }
-  }
-  const int tiles_all = (n + kPairs - 1) / kPairs, tile0 = lo * G / kPairs;
-  const int t_begin = tile0 + (int)((int64_t)(tiles_all - tile0) * part / p.parts);
-  const int t_end = tile0 + (int)((int64_t)(tiles_all - tile0) * (part + 1) / p.parts);
+  const int k0 = it.key0 + wave * kWaveKeys;
 
   // Copies: a wave's share of a tile is 8 pairs (two copies, or one at d = 64, of 16 bytes a
   // lane), and lse and position of all 32.  Pairs behind the last one read the last one's.
@@ -268,75 +225,181 @@ __global__ __launch_bounds__(256, 3) void msa_kv_weights_tiles_kernel(WeightsPar
   constexpr int kPerCopy = 64 / kChunks;   // pairs of a copy
   constexpr int kCopies = 8 / kPerCopy;
   auto swizzle = [](int r) { return (D == 128 ? r : r >> 1) & (kChunks - 1); };
-  // the next tile to copy: its first pair, as a row and a place in the group (a division once, here)
+  // Sources of the lane's copies from the next tile.  From tile to tile each moves on by 32 pairs,
+  // that is step_rows rows and step_heads heads, and by one more row where the heads pass G.
   const int step_rows = kPairs / G, step_heads = kPairs - step_rows * G;
-  int next = t_begin, next_row = t_begin * kPairs / G, next_head = t_begin * kPairs - next_row * G;
-  auto copy = [&]() __attribute__((always_inline)) {
-    const int slot = next & (kRing - 1);
-    const int most = n - 1 - min(next, t_end - 1) * kPairs;  // the tile's last pair, if not 31
-    auto pair_at = [&](int r, int& tok, int& head) __attribute__((always_inline)) {
-      const uint32_t off = (uint32_t)(next_head + min(r, most));
-      const int dt = (int)(off * p.group_inv >> 20);
-      tok = next_row + dt;
-      head = kv_head * G + (int)off - dt * G;
-    };
-    int tok, head;
+  int next = t_begin;
+  const char* from[kCopies + 1];
+  int head_at[kCopies + 1];
+  const int64_t q_step = (step_rows * p.q_st + step_heads * p.q_sh) * 2, q_wrap = (p.q_st - G * p.q_sh) * 2;
+  const int64_t l_step = hl ? step_rows * 4 : ((int64_t)step_rows * p.num_q_heads + step_heads) * 4;
+  const int64_t l_wrap = hl ? 4 : ((int64_t)p.num_q_heads - G) * 4;
+  auto aim = [&](int t, int most) __attribute__((always_inline)) {  // at tile t, pairs behind `most` at that one
 #pragma unroll
-    for (int c = 0; c < kCopies; ++c) {
-      const int r0 = wave * 8 + c * kPerCopy, r = r0 + lane / kChunks;
-      pair_at(r, tok, head);
-      copy16(p.q + (int64_t)(row0 + tok) * p.q_st + (int64_t)head * p.q_sh + ((lane % kChunks) ^ swizzle(r)) * 8,
-             ring.q[__builtin_amdgcn_readfirstlane(slot)] + r0 * D * 2);
+    for (int c = 0; c <= kCopies; ++c) {
+      const int r = c < kCopies ? wave * 8 + c * kPerCopy + lane / kChunks : ln;
+      const int first_row = t * kPairs / G, off = t * kPairs - first_row * G + min(r, most);
+      const int dt = (int)((uint32_t)off * p.group_inv >> 20), tok = first_row + dt;
+      head_at[c] = off - dt * G;
+      const int head = kv_head * G + head_at[c];
+      if (c < kCopies)
+        from[c] = reinterpret_cast<const char*>(p.q + (int64_t)(row0 + tok) * p.q_st + (int64_t)head * p.q_sh +
+                                                ((lane % kChunks) ^ swizzle(r)) * 8);
+      else
+        from[c] = hl ? reinterpret_cast<const char*>(row_pos + tok)
+                     : reinterpret_cast<const char*>(p.lse + (int64_t)(row0 + tok) * p.num_q_heads + head);
     }
-    pair_at(ln, tok, head);
-    const void* lse = p.lse + (int64_t)(row0 + tok) * p.num_q_heads + head;
-    const void* pos = row_pos + tok;
-    copy4(hl ? pos : lse, ring.more[__builtin_amdgcn_readfirstlane(slot)][wave]);
+  };
+  auto copy = [&]() __attribute__((always_inline)) {
+    const int slot = __builtin_amdgcn_readfirstlane(next & (kRing - 1));
+    if (next == tiles_all - 1) aim(next, n - 1 - next * kPairs);  // the sequence's last tile may be short
+#pragma unroll
+    for (int c = 0; c < kCopies; ++c) copy16(from[c], ring.q[slot] + (wave * 8 + c * kPerCopy) * D * 2);
+    copy4(from[kCopies], ring.more[slot][wave]);
     ++next;
-    if (next < t_end) {  // (behind the last tile it is copied again, so that each step waits for as many)
-      next_row += step_rows;
-      next_head += step_heads;
-      if (next_head >= G) {
-        next_head -= G;
-        ++next_row;
+    if (next >= t_end) return;  // (behind the last tile it is copied again, so that each step waits for as many)
+#pragma unroll
+    for (int c = 0; c <= kCopies; ++c) from[c] += c < kCopies ? q_step : l_step;
+    if (step_heads != 0) {
+#pragma unroll
+      for (int c = 0; c <= kCopies; ++c) {
+        head_at[c] += step_heads;
+        const bool wraps = head_at[c] >= G;
+        head_at[c] -= wraps ? G : 0;
+        from[c] += wraps ? (c < kCopies ? q_wrap : l_wrap) : 0;
       }
     }
   };
   constexpr int kEach = kCopies + 1;  // copies of a wave and tile
 
+  aim(t_begin, kPairs - 1);
+  copy();
+  copy();
+  copy();
+
+  // B operand: key k0 + kt*32 + ln, channels kk*16 + hl*8 .. +8 (behind the last one: that one, not written)
+  bf16x8 kf[2][D / 16];
+  const bf16x8 ones = all_of(1.0f);
+  int32_t blk[2];
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt)
+    blk[kt] = p.block_table[(int64_t)it.seq * p.max_blocks + (min(k0 + kt * 32 + ln, last) >> 4)];
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt) {
+    const uint16_t* src = p.k + (int64_t)blk[kt] * p.k_sb + (int64_t)kv_head * p.k_sh +
+                          (int64_t)(min(k0 + kt * 32 + ln, last) & 15) * p.k_st + hl * 8;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) kf[kt][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
+  }
   float sum[2] = {0.0f, 0.0f};
-  if (t_begin < t_end) {
-    __builtin_amdgcn_s_waitcnt(wait_loads(0));  // K has arrived (the compiler would wait for it, and for all copies, in the loop)
-    copy();
-    copy();
-    copy();
-    for (int t = t_begin; t < t_end; ++t) {
-      // tile t has arrived once no more than the copies of two tiles are outstanding; behind the
-      // barrier every wave's share has, and tile t - 1 is read
+  __builtin_amdgcn_s_waitcnt(wait_loads(0));  // K has arrived (the compiler would wait for it, and for all copies, in the loop)
+  {
+    // Tile t has arrived once no more than the copies of two tiles are outstanding; behind the
+    // barrier every wave's share has, and tile t - 1 is read.
+    auto advance = [&]() __attribute__((always_inline)) {
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kEach) : "memory");
       copy();
+    };
+    // the operands of tile t, -lse / scale and Q; and the positions of the lane's 16 score rows,
+    // where some may not see all of the wave's keys
+    int pos[16];
+    auto read = [&](int t, bool masked, bf16x8& lf, bf16x8 (&qf)[D / 16]) __attribute__((always_inline)) {
       const int slot = t & (kRing - 1);
-      const uint32_t* more = ring.more[slot][wave];
-      float l = __uint_as_float(more[ln]);
-      const int pos = (int)more[32 + ln];
+      float l = __uint_as_float(ring.more[slot][wave][ln]);
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {  // register i of a lane: pair (i/4)*8 + hl*4 + i%4
+          const uint4 x = *reinterpret_cast<const uint4*>(&ring.more[slot][wave][32 + i * 2 + hl * 4]);
+          pos[i] = (int)x.x;
+          pos[i + 1] = (int)x.y;
+          pos[i + 2] = (int)x.z;
+          pos[i + 3] = (int)x.w;
+        }
+      }
       if (t * kPairs + ln >= n || l == -__builtin_inff()) l = __builtin_inff();
-      const int first_pos = __builtin_amdgcn_readfirstlane(pos);
-      if (__builtin_amdgcn_readlane(pos, 31) < k0) continue;  // all of the tile's rows lie before the wave's keys
-      const bf16x8 lf = three_terms(-l * p.inv_scale, hl == 0);
-      bf16x8 qf[D / 16];
+      lf = three_terms(-l * p.inv_scale, hl == 0);
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk)
         qf[kk] = *reinterpret_cast<const bf16x8*>(ring.q[slot] + ln * D * 2 + (((kk * 2 + hl) ^ swizzle(ln)) * 16));
-      const bool masked = first_pos < k0 + kWaveKeys - 1;
-      f32x16 s[2] = {};
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lf, ones, s[kt], 0, 0, 0);
+    };
+    auto position = [&](int t, int pair) {  // uniform
+      return __builtin_amdgcn_readfirstlane((int)ring.more[t & (kRing - 1)][wave][32 + pair]);
+    };
+    auto is_masked = [&](int t) { return position(t, 0) < k0 + kWaveKeys - 1; };
+    bf16x8 lf, qf[D / 16];
+    f32x16 s[2][2];
+    constexpr int kEl = 16 / (D / 16);  // scores of a key tile beside each pair of MFMAs
+    float part_sum[2][4] = {};
+    auto scores = [&](f32x16 (&to)[2], auto&& beside) __attribute__((always_inline)) {
+      const f32x16 zero = {};
+      to[0] = to[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lf, ones, zero, 0, 0, 0);
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[kk], kf[kt][kk], s[kt], 0, 0, 0);
+        for (int kt = 0; kt < 2; ++kt) {
+          to[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[kk], kf[kt][kk], to[kt], 0, 0, 0);
+          beside(kt, kk);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto weights = [&](const f32x16 (&of)[2], int kt, int kk) __attribute__((always_inline)) {
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) sum[kt] += key_sum(s[kt], p.scale_log2, masked, pos, k0 + kt * 32 + ln, hl);
+      for (int e = kk * kEl; e < (kk + 1) * kEl; e += 2) {
+        part_sum[kt][e / 2 % 4] +=
+            __builtin_amdgcn_exp2f(of[kt][e] * p.scale_log2) + __builtin_amdgcn_exp2f(of[kt][e + 1] * p.scale_log2);
+        asm volatile("" : "+v"(part_sum[kt][e / 2 % 4]));  // (the compiler would move it all behind the MFMAs)
+      }
+    };
+    auto hide = [&](f32x16 (&of)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) of[kt][e] = pos[e] >= k0 + kt * 32 + ln ? of[kt][e] : -__builtin_inff();
+    };
+    int t = t_begin;
+    for (; t < t_end; ++t) {  // tiles of which no row sees any of the wave's keys
+      advance();
+      if (position(t, 31) >= k0) break;
+    }
+    // The MFMAs of tile t + 1 run beside the exponentials of tile t, two scores a key tile and MFMA
+    // pair.  The first tiles are those whose rows do not all see all of the wave's keys.
+    if (t < t_end) {
+      bool masked = is_masked(t);
+      read(t, masked, lf, qf);
+      scores(s[0], [](int, int) {});
+      ++t;
+      while (t < t_end && masked) {
+        hide(s[0]);
+        advance();
+        masked = is_masked(t);
+        read(t, masked, lf, qf);
+        scores(s[1], [&](int kt, int kk) __attribute__((always_inline)) { weights(s[0], kt, kk); });
+        s[0][0] = s[1][0];
+        s[0][1] = s[1][1];
+        ++t;
+      }
+      auto step = [&](f32x16 (&now)[2], f32x16 (&then)[2]) __attribute__((always_inline)) {
+        advance();
+        read(t, false, lf, qf);
+        scores(then, [&](int kt, int kk) __attribute__((always_inline)) { weights(now, kt, kk); });
+        ++t;
+      };
+      while (t + 1 < t_end) {
+        step(s[0], s[1]);
+        step(s[1], s[0]);
+      }
+      if (t < t_end) {
+        step(s[0], s[1]);
+        s[0][0] = s[1][0];
+        s[0][1] = s[1][1];
+      }
+      if (masked) hide(s[0]);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) weights(s[0], kt, kk);
+        sum[kt] = (part_sum[kt][0] + part_sum[kt][1]) + (part_sum[kt][2] + part_sum[kt][3]);
+      }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // copies under way end before the workgroup's LDS does
   }
@@ -345,67 +408,41 @@ __global__ __launch_bounds__(256, 3) void msa_kv_weights_tiles_kernel(WeightsPar
     const float total = sum[kt] + __shfl_xor(sum[kt], 32);
     const int key = k0 + kt * 32 + ln;
     if (hl != 0 || key > last) continue;
-    if (p.parts == 1) {
-      float* out = p.weights + (int64_t)seq * p.w_sb + (int64_t)kv_head * p.w_sh + key;
+    if (it.slot < 0) {
+      float* out = p.weights + (int64_t)it.seq * p.w_sb + (int64_t)kv_head * p.w_sh + key;
       *out = p.accumulate ? *out + total : total;
     } else {
-      p.sums[(((int64_t)part * p.num_seqs + seq) * p.num_kv_heads + kv_head) * p.span + key] = total;
+      p.sums[((int64_t)it.slot * p.num_kv_heads + kv_head) * kGroupKeys + (key - it.key0)] = total;
     }
   }
 }
 
-// adds up the parts' sums, in order
-__global__ __launch_bounds__(256) void msa_kv_weights_join_kernel(WeightsParams p) {
-  const int per_chunk = p.num_seqs * p.num_kv_heads;
-  const int chunk = blockIdx.x / per_chunk, rest = blockIdx.x - chunk * per_chunk;
-  const int seq = rest / p.num_kv_heads, kv_head = rest - seq * p.num_kv_heads;
-  const int row0 = p.seq_row0[seq], nrows = p.seq_row0[seq + 1] - row0;
-  if (nrows * p.group <= kPairs) return;
-  const int key = chunk * 256 + (int)threadIdx.x;
-  if (key > p.row_pos[row0 + nrows - 1]) return;
-  float* out = p.weights + (int64_t)seq * p.w_sb + (int64_t)kv_head * p.w_sh + key;
+// adds up the sums of keys with several items, in order
+__global__ __launch_bounds__(kGroupKeys) void msa_kv_weights_join_kernel(WeightsParams p) {
+  const uint32_t item = blockIdx.x / (uint32_t)p.num_kv_heads;
+  const int kv_head = (int)(blockIdx.x - item * (uint32_t)p.num_kv_heads);
+  const WeightsJoin it = p.joins[item];
+  const int key = it.key0 + (int)threadIdx.x;
+  const int last = p.row_pos[p.seq_row0[it.seq + 1] - 1];
+  if (key > last) return;
+  float* out = p.weights + (int64_t)it.seq * p.w_sb + (int64_t)kv_head * p.w_sh + key;
   const float old = p.accumulate ? *out : 0.0f;
-  const float* src = p.sums + ((int64_t)seq * p.num_kv_heads + kv_head) * p.span + key;
-  float x[kMostParts], total = 0.0f;
+  const int64_t stride = (int64_t)p.num_kv_heads * kGroupKeys;
+  const float* src = p.sums + (int64_t)it.slot0 * stride + (int64_t)kv_head * kGroupKeys + threadIdx.x;
+  constexpr int kBatch = 16;
+  float total = 0.0f;
+  for (int i0 = 0; i0 < it.parts; i0 += kBatch) {
+    float x[kBatch];
 #pragma unroll
-  for (int i = 0; i < kMostParts; ++i)
-    x[i] = i < p.parts ? src[(int64_t)i * p.num_seqs * p.num_kv_heads * p.span] : 0.0f;
+    for (int i = 0; i < kBatch; ++i) x[i] = src[min(i0 + i, it.parts - 1) * stride];
 #pragma unroll
-  for (int i = 0; i < kMostParts; ++i) total += x[i];
+    for (int i = 0; i < kBatch; ++i) total += i0 + i < it.parts ? x[i] : 0.0f;
+  }
   *out = old + total;
 }
 
-// What a plan's call launches.
-struct Shape {
-  int64_t stream_keys = 0;  // keys x KV heads of sequences of up to 32 pairs
-  int64_t longest_stream = 0, longest_tiles = 0;  // keys
-  int64_t parts = 1, span = 0;
-};
-Shape shape_of(const HostPlan& hp) {
-  Shape s;
-  int64_t groups = 0, most_tiles = 0;
-  for (size_t b = 0; b < hp.seq_blocks.size(); ++b) {
-    const int64_t pairs = (int64_t)(hp.seq_row0[b + 1] - hp.seq_row0[b]) * hp.group;
-    const int64_t keys = (int64_t)hp.seq_blocks[b] * kBlockSize;
-    if (pairs == 0) continue;
-    if (pairs <= kPairs) {
-      s.stream_keys += keys * hp.shape.num_kv_heads;
-      s.longest_stream = std::max(s.longest_stream, keys);
-    } else {
-      s.longest_tiles = std::max(s.longest_tiles, keys);
-      groups += (keys + kGroupKeys - 1) / kGroupKeys * hp.shape.num_kv_heads;
-      most_tiles = std::max(most_tiles, (pairs + kPairs - 1) / kPairs);
-    }
-  }
-  if (groups > 0) {
-    // some 2048 workgroups, with 16 tiles in a part
-    s.parts = std::min({(2048 + groups - 1) / groups, std::max<int64_t>(1, most_tiles / 16), (int64_t)kMostParts});
-    s.span = (s.longest_tiles + kGroupKeys - 1) / kGroupKeys * kGroupKeys;
-  }
-  return s;
-}
-size_t workspace_of(const HostPlan& hp, const Shape& s) {
-  return s.parts == 1 ? 0 : (size_t)(s.parts * hp.shape.num_seqs * hp.shape.num_kv_heads * s.span) * sizeof(float);
+size_t workspace_of(const HostPlan& hp) {
+  return (size_t)hp.weight_slots * (size_t)hp.shape.num_kv_heads * kGroupKeys * sizeof(float);
 }
 
 msa_status fail(const char* who, msa_status st, const std::string& msg) {
@@ -420,7 +457,7 @@ bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p)
 
 extern "C" msa_status msa_kv_weights_workspace(msa_plan_t plan, size_t* bytes) {
   if (!plan || !bytes) return msa::fail("msa_kv_weights_workspace", MSA_ERR_INVALID_ARG, "null argument");
-  *bytes = plan->hp.total_q == 0 ? 0 : msa::workspace_of(plan->hp, msa::shape_of(plan->hp));
+  *bytes = msa::workspace_of(plan->hp);
   return MSA_OK;
 }
 
@@ -442,18 +479,18 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
       !msa::aligned(weights, 4))
     return invalid("q and k_cache must be 16-byte, the others 4-byte aligned");
   const msa_shape& s = hp.shape;
-  const msa::Shape launch = msa::shape_of(hp);
-  const size_t need = msa::workspace_of(hp, launch);
+  const size_t need = msa::workspace_of(hp);
   if (need > workspace_bytes || (need > 0 && (!workspace || !msa::aligned(workspace, 16))))
     return invalid("workspace must be 16-byte aligned and hold " + std::to_string(need) + " bytes");
   // stream: two rounds of the waves that the card holds (12 a CU), 64 to 1024 keys each
-  int64_t wave_keys = launch.stream_keys / (2 * 12 * msa::kCUs) / 64 * 64;
+  int64_t wave_keys = hp.stream_keys * s.num_kv_heads / (2 * 12 * msa::kCUs) / 64 * 64;
   wave_keys = wave_keys < 64 ? 64 : wave_keys > 1024 ? 1024 : wave_keys;
-  const int64_t heads = (int64_t)s.num_seqs * s.num_kv_heads;
-  const int64_t stream_groups = (launch.longest_stream + 4 * wave_keys - 1) / (4 * wave_keys) * heads;
-  const int64_t chunks = (launch.longest_tiles + msa::kGroupKeys - 1) / msa::kGroupKeys;
+  const int64_t stream_groups =
+      (hp.longest_stream + 4 * wave_keys - 1) / (4 * wave_keys) * s.num_seqs * s.num_kv_heads;
+  const int64_t items = (int64_t)hp.weights.size() * s.num_kv_heads;
+  const int64_t joins = (int64_t)hp.weight_joins.size() * s.num_kv_heads;
   if (hp.total_q * hp.group >= ((int64_t)1 << 31) - 64 || stream_groups >= ((int64_t)1 << 31) ||
-      chunks * heads * launch.parts >= ((int64_t)1 << 31))
+      items >= ((int64_t)1 << 31))
     return msa::fail(who, MSA_ERR_UNSUPPORTED, "too many rows or keys for one launch");
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev != plan->device)
@@ -483,8 +520,8 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
   p.scale_log2 = s.scale * 1.4426950408889634f;
   p.accumulate = accumulate;
   p.wave_keys = (int32_t)wave_keys;
-  p.parts = (int32_t)launch.parts;
-  p.span = launch.span;
+  p.items = plan->d_weights;
+  p.joins = plan->d_weight_joins;
   p.sums = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const bool d128 = s.head_dim == 128;
@@ -497,8 +534,8 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
     const msa_status rc = msa::launched(who, "stream", (int)hipGetLastError());
     if (rc != MSA_OK) return rc;
   }
-  if (chunks > 0) {
-    const dim3 grid((uint32_t)(chunks * heads * launch.parts));
+  if (items > 0) {
+    const dim3 grid((uint32_t)items);
     if (d128)
       hipLaunchKernelGGL(msa::msa_kv_weights_tiles_kernel<128>, grid, dim3(256), 0, st, p);
     else
@@ -506,8 +543,8 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
     const msa_status rc = msa::launched(who, "tiles", (int)hipGetLastError());
     if (rc != MSA_OK) return rc;
   }
-  if (launch.parts > 1) {
-    hipLaunchKernelGGL(msa::msa_kv_weights_join_kernel, dim3((uint32_t)(chunks * heads)), dim3(256), 0, st, p);
+  if (joins > 0) {
+    hipLaunchKernelGGL(msa::msa_kv_weights_join_kernel, dim3((uint32_t)joins), dim3(msa::kGroupKeys), 0, st, p);
     return msa::launched(who, "join", (int)hipGetLastError());
   }
   return MSA_OK;
