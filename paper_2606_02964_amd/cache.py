@@ -15,7 +15,7 @@ except ImportError:  # the package itself does without
     torch = None
 
 from . import MSA_ERR_INVALID_ARG, MsaError, Plan, _addr, _bind, _check, _i32, _i64, _lib, _P, _stream, msa_shape
-from .tree import check_tensor
+from .tree import FLOAT32, INT32, check_tensor, size_of
 
 __all__ = ["msa_kv_weights", "msa_kv_weights_workspace", "msa_kv_select", "msa_kv_compact"]
 
@@ -31,20 +31,23 @@ def _refuse(who: str, what: str) -> None:
     raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {what}")
 
 
-def _lists(who: str, name: str, x, dtype: str, shape) -> None:
-    """A tensor [sequences, lists, entries] of at least ``shape``, its entries contiguous."""
-    if str(x.dtype)[6:] != dtype or not x.is_cuda:
-        _refuse(who, f"{name} is not a {dtype} tensor on a GPU")
-    if x.dim() != 3 or any(a < b for a, b in zip(x.shape, shape)):
-        _refuse(who, f"{name} has shape {tuple(x.shape)}, {tuple(shape)} is needed")
-    if x.shape[2] > 1 and x.stride(2) != 1:
-        _refuse(who, f"{name} is not contiguous along its last dimension")
+def _lists(who: str, name: str, x, dtypes, a: int, b: int, c: int) -> None:
+    """A tensor [sequences, lists, entries] of at least (a, b, c), its entries contiguous."""
+    have = x.shape
+    if x.dtype in dtypes and x.is_cuda and len(have) == 3 and have[0] >= a and have[1] >= b and have[2] >= c \
+            and (x.stride(2) == 1 or have[2] <= 1):
+        return
+    if x.dtype not in dtypes or not x.is_cuda:
+        _refuse(who, f"{name} is not a {dtypes[0]} tensor on a GPU")
+    if len(have) != 3 or have[0] < a or have[1] < b or have[2] < c:
+        _refuse(who, f"{name} has shape {tuple(have)}, {(a, b, c)} is needed")
+    _refuse(who, f"{name} is not contiguous along its last dimension")
 
 
 def _here(who: str, x) -> None:
     """Calls without a plan know no device of their own: their tensors are on the current one."""
-    if x.device.index != torch.cuda.current_device():
-        _refuse(who, f"tensors are on device {x.device.index}, the current device is {torch.cuda.current_device()}")
+    if x.get_device() != torch.cuda.current_device():
+        _refuse(who, f"tensors are on device {x.get_device()}, the current device is {torch.cuda.current_device()}")
 
 
 def msa_kv_weights_workspace(plan: Plan) -> int:
@@ -59,14 +62,14 @@ def msa_kv_weights(plan: Plan, q, k_cache, block_table, lse, weights, workspace=
     """Enqueue the sum of the plan's softmax weights by key into ``weights`` float32 [sequences, KV heads, positions];
     ``accumulate`` adds to what is there."""
     who, sh = "msa_kv_weights", plan.shape
-    need = getattr(plan, "_positions", None)
+    need = getattr(plan, "positions", None)
     if need is None:  # the most positions a sequence may have
-        need = plan._positions = sh.max_blocks_per_seq * sh.block_size
-    _lists(who, "weights", weights, "float32", (sh.num_seqs, sh.num_kv_heads, need))
-    size = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
+        need = plan.positions = sh.max_blocks_per_seq * sh.block_size
+        plan.heads = (sh.num_seqs, sh.num_kv_heads)
+    _lists(who, "weights", weights, FLOAT32, *plan.heads, need)
     _check(_lib.msa_kv_weights(plan.handle, _addr(q), _addr(k_cache), _addr(block_table), _addr(lse), _addr(weights),
-                               weights.stride(0), weights.stride(1), int(accumulate), _addr(workspace), size,
-                               _stream(stream)))
+                               weights.stride(0), weights.stride(1), int(accumulate), _addr(workspace),
+                               size_of(workspace), _stream(stream)))
 
 
 def msa_kv_select(scores, seq_len, keep, index, count, first: int = 0, recent: int = 0, stream=None) -> None:
@@ -77,10 +80,11 @@ def msa_kv_select(scores, seq_len, keep, index, count, first: int = 0, recent: i
     if getattr(scores, "dim", lambda: 0)() != 3:
         _refuse(who, "scores is not a tensor [sequences, lists, positions]")
     B, H, L = scores.shape
-    _lists(who, "scores", scores, "float32", (B, H, 0))
-    _lists(who, "index", index, "int32", (B, H, 0))
-    for name, x in (("seq_len", seq_len), ("keep", keep), ("count", count)):
-        check_tensor(who, name, x, ("int32",), B)
+    _lists(who, "scores", scores, FLOAT32, B, H, 0)
+    _lists(who, "index", index, INT32, B, H, 0)
+    check_tensor(who, "seq_len", seq_len, INT32, B)
+    check_tensor(who, "keep", keep, INT32, B)
+    check_tensor(who, "count", count, INT32, B)
     _here(who, scores)
     _check(_lib.msa_kv_select(B, H, _addr(scores), scores.stride(0), scores.stride(1), L, _addr(seq_len), _addr(keep),
                               int(first), int(recent), index.shape[2], _addr(index), index.stride(0), index.stride(1),
@@ -93,11 +97,13 @@ def msa_kv_compact(shape: msa_shape, base, index, count, block_table, k_cache, v
     0) and ``count`` int32 [sequences]."""
     who, B = "msa_kv_compact", shape.num_seqs
     if index.dim() == 2:
-        index = index[:, None].expand(-1, shape.num_kv_heads, -1)
-    _lists(who, "index", index, "int32", (B, shape.num_kv_heads, 0))
-    for name, x in (("base", base), ("count", count)):
-        check_tensor(who, name, x, ("int32",), B)
+        check_tensor(who, "index", index, INT32, index.shape[1], B)
+        entries, per_seq, per_head = index.shape[1], index.stride(0), 0
+    else:
+        _lists(who, "index", index, INT32, B, shape.num_kv_heads, 0)
+        entries, per_seq, per_head = index.shape[2], index.stride(0), index.stride(1)
+    check_tensor(who, "base", base, INT32, B)
+    check_tensor(who, "count", count, INT32, B)
     _here(who, index)
-    _check(_lib.msa_kv_compact(ctypes.byref(shape), _addr(base), _addr(index), index.stride(0), index.stride(1),
-                               index.shape[2], _addr(count), _addr(block_table), _addr(k_cache), _addr(v_cache),
-                               _stream(stream)))
+    _check(_lib.msa_kv_compact(ctypes.byref(shape), _addr(base), _addr(index), per_seq, per_head, entries, _addr(count),
+                               _addr(block_table), _addr(k_cache), _addr(v_cache), _stream(stream)))

@@ -96,7 +96,7 @@ struct Unit {
 // its tiles (about 1 us each, two workgroups on a CU).  A launch of few rounds of
 // workgroups takes as long as that many of the longest items, one of many rounds a
 // CU's share of all items and half an item, as it ends unevenly.  The part is the
-// one of least such cost, among lengths a third apart and the shortest that need one,
+// one of least such cost, among lengths a half apart and the shortest that need one,
 // two or three rounds (8 KV heads: one prompt of 4096 93 us in one round, 105 us in
 // items of 24 tiles; of 8192 356 us in two full rounds, 395 us in items of 160;
 // 8 prompts of 2048 217 us in items of 32, 260 us in one round, whose longest item is
@@ -105,7 +105,7 @@ struct Unit {
 // (one prompt of 16384 1166 us in items of 150 tiles, 1484 us in one round of
 // 1057): kMost tiles at most.
 void plan_weights(HostPlan* plan) {
-  constexpr int64_t kShortest = 8, kMost = 160, kSlots = 2 * kCUs, kItemTiles = 5, kRounds = 3;
+  constexpr int64_t kShortest = 8, kMost = 160, kSlots = 2 * kCUs, kItemTiles = 5, kRounds = 3, kStep = 4;
   HostPlan& P = *plan;
   const int64_t G = P.group, B = P.shape.num_seqs, heads = P.shape.num_kv_heads;
   struct Chunk {
@@ -137,8 +137,8 @@ void plan_weights(HostPlan* plan) {
   if (chunks.empty()) return;
   auto items_of = [&](int64_t len) {
     int64_t items = 0;
-    for (const Chunk& c : chunks) items += (c.tiles - c.first + len - 1) / len * heads;
-    return items;
+    for (const Chunk& c : chunks) items += (uint32_t)(c.tiles - c.first + len - 1) / (uint32_t)len;
+    return items * heads;
   };
   auto cost_of = [&](int64_t len) {
     const int64_t items = items_of(len), rounds = (items + kSlots - 1) / kSlots;
@@ -155,14 +155,14 @@ void plan_weights(HostPlan* plan) {
     }
   };
   for (int64_t rounds = 1; rounds <= kRounds; ++rounds) {  // the shortest that needs no more rounds
-    int64_t len = kShortest;
-    for (int64_t most = std::min(longest, kMost); len < most;) {
+    int64_t len = 1, most = (std::min(longest, kMost) + kStep - 1) / kStep;  // in steps of 4 tiles
+    while (len < most) {
       const int64_t mid = (len + most) / 2;
-      if (items_of(mid) <= rounds * kSlots) most = mid; else len = mid + 1;
+      if (items_of(mid * kStep) <= rounds * kSlots) most = mid; else len = mid + 1;
     }
-    consider(len);
+    consider(std::max(kShortest, len * kStep));
   }
-  for (int64_t len = kShortest; len < std::min(longest, kMost); len += len / 3) consider(len);
+  for (int64_t len = kShortest; len < std::min(longest, kMost); len += len / 2) consider(len);
   for (const Chunk& c : chunks) {
     const int64_t len = c.tiles - c.first, parts = (len + part - 1) / part;
     const int32_t slot0 = P.weight_slots;

@@ -10,6 +10,14 @@ from __future__ import annotations
 import ctypes
 from typing import Optional, Sequence
 
+try:
+    import torch
+    INT32, FLOAT32, MASK = (torch.int32,), (torch.float32,), (torch.int64, torch.uint64)
+    _PROB = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # MSA_PROB_*
+except ImportError:  # the package itself does without; then nothing here is a tensor
+    INT32 = FLOAT32 = MASK = ()
+    _PROB = {}
+
 from . import (MSA_ERR_INVALID_ARG, MSA_PLAN_HOST_ONLY, MsaError, Plan, _addr, _bind, _check, _host_i32, _i32, _i64,
                _lib, _P, _stream, msa_plan_opts, msa_shape)
 
@@ -37,40 +45,47 @@ _bind("msa_tree_verify", [_P, _i32, _i32, _P, _i64, _P, _i64, _P, _P, _P, _P, _P
 _bind("msa_tree_verify_workspace", [_P, _i32, ctypes.POINTER(ctypes.c_size_t)])
 
 
-def check_tensor(who: str, name: str, x, dtypes: Sequence[str], need: int, rows: Optional[int] = None) -> None:
+def check_tensor(who: str, name: str, x, dtypes, need: int, rows: Optional[int] = None) -> None:
     """Refuses a tensor of another type, on the host, not contiguous, or with fewer than ``need`` elements; with
-    ``rows``, a 2-D one (rows, need) whose last dimension is contiguous.  Other objects pass."""
-    if x is None or isinstance(x, int) or not hasattr(x, "stride"):
+    ``rows``, a 2-D one (rows, need) whose last dimension is contiguous.  Other objects pass.  (These checks run on
+    every call: the common case is a few attribute reads.)"""
+    if x is None or type(x) is int or not hasattr(x, "stride"):
         return
-    bad = None
-    if str(x.dtype)[6:] not in dtypes:
-        bad = f"has type {x.dtype}, not {' or '.join(dtypes)}"
+    if x.dtype in dtypes and x.is_cuda:
+        if rows is None:
+            if x.numel() >= need and x.is_contiguous():
+                return
+        elif x.dim() == 2:
+            have = x.shape
+            if have[0] >= rows and have[1] >= need and (need <= 1 or rows == 0 or x.stride(1) == 1):
+                return
+    if x.dtype not in dtypes:
+        bad = f"has type {x.dtype}, not {' or '.join(str(d) for d in dtypes)}"
     elif not x.is_cuda:
         bad = "is not on a GPU"
-    elif rows is None:
-        if not x.is_contiguous():
-            bad = "is not contiguous"
-        elif x.numel() < need:
-            bad = f"has {x.numel()} elements, {need} are needed"
-    elif x.dim() != 2 or x.shape[0] < rows or x.shape[1] < need:
+    elif rows is not None and (x.dim() != 2 or x.shape[0] < rows or x.shape[1] < need):
         bad = f"has shape {tuple(x.shape)}, ({rows}, {need}) is needed"
-    elif rows and x.stride(1) != 1 and need > 1:
+    elif rows is not None:
         bad = "is not contiguous along its last dimension"
-    if bad:
-        raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {name} {bad}")
+    elif x.numel() < need:
+        bad = f"has {x.numel()} elements, {need} are needed"
+    else:
+        bad = "is not contiguous"
+    raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {name} {bad}")
 
 
-def workspace_bytes(workspace, given: int) -> int:
+def size_of(workspace, given: int = 0) -> int:
+    """Bytes of a workspace tensor, or as given."""
     if workspace is None or given:
         return int(given)
-    return int(workspace.numel() * workspace.element_size())
+    return workspace.numel() * workspace.element_size()
 
 
 def _row_stride(x, given: Optional[int], width: int) -> int:
     if given is not None:
         return int(given)
     if hasattr(x, "stride") and x.dim() == 2:
-        return int(x.stride(0)) if x.shape[0] > 1 else max(int(x.shape[1]), width)
+        return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], width)
     return width
 
 
@@ -90,8 +105,8 @@ def msa_plan_tree(shape: msa_shape, seq_kv_len: Sequence[int], seg_indptr: Seque
                               None if flags & MSA_PLAN_HOST_ONLY else _stream(stream), ctypes.byref(handle)))
     plan = Plan(handle.value, shape)
     info = msa_plan_tree_info(plan)
-    plan.trees, plan.tree_rows = info["num_trees"], info["tree_rows"]
-    plan.max_slots, plan.mask_words = info["max_slots"], info["mask_words"]
+    plan.tree_rows, plan.max_slots, plan.mask_words = info["tree_rows"], info["max_slots"], info["mask_words"]
+    plan.tree_figures = (info["num_trees"], info["tree_rows"], info["max_slots"], info["mask_words"])
     return plan
 
 
@@ -104,16 +119,15 @@ def msa_plan_tree_info(plan: Plan) -> dict:
 def _figures(plan: Plan):
     """(trees, tree rows, slots of the largest, mask words); zeros for a plan without trees, whose calls the library
     refuses or answers without reading anything."""
-    return (getattr(plan, "trees", 0), getattr(plan, "tree_rows", 0), getattr(plan, "max_slots", 0),
-            getattr(plan, "mask_words", 0))
+    return getattr(plan, "tree_figures", (0, 0, 0, 0))
 
 
 def msa_tree_mask(plan: Plan, parents, mask, mask_stride: Optional[int] = None, stream=None) -> None:
     """Enqueue the trees' ancestor masks: ``parents`` int32 [tree_rows] to ``mask`` int64 or uint64
     [tree_rows, >= mask_words]."""
     _, rows, _, words = _figures(plan)
-    check_tensor("msa_tree_mask", "parents", parents, ("int32",), rows)
-    check_tensor("msa_tree_mask", "mask", mask, ("int64", "uint64"), words, rows)
+    check_tensor("msa_tree_mask", "parents", parents, INT32, rows)
+    check_tensor("msa_tree_mask", "mask", mask, MASK, words, rows)
     _check(_lib.msa_tree_mask(plan.handle, _addr(parents), _addr(mask), _row_stride(mask, mask_stride, words),
                               _stream(stream)))
 
@@ -123,12 +137,10 @@ def msa_tree_forward(plan: Plan, q, k_cache, v_cache, block_table, mask, o, lse=
     """Enqueue the attention of a plan with trees for one layer; ``mask`` as of ``msa_tree_mask`` (None if the plan
     has no tree), the rest as of ``msa_forward``."""
     _, rows, _, words = _figures(plan)
-    check_tensor("msa_tree_forward", "mask", mask, ("int64", "uint64"), words, rows)
-    if workspace is not None and not workspace_bytes:
-        workspace_bytes = int(workspace.numel() * workspace.element_size())
+    check_tensor("msa_tree_forward", "mask", mask, MASK, words, rows)
     _check(_lib.msa_tree_forward(plan.handle, _addr(q), _addr(k_cache), _addr(v_cache), _addr(block_table),
                                  _addr(mask), _row_stride(mask, mask_stride, words), _addr(o), _addr(lse),
-                                 _addr(workspace), int(workspace_bytes), _stream(stream)))
+                                 _addr(workspace), size_of(workspace, workspace_bytes), _stream(stream)))
 
 
 def msa_tree_verify_workspace(plan: Plan, vocab: int) -> int:
@@ -136,9 +148,6 @@ def msa_tree_verify_workspace(plan: Plan, vocab: int) -> int:
     out = ctypes.c_size_t()
     _check(_lib.msa_tree_verify_workspace(plan.handle, int(vocab), ctypes.byref(out)))
     return out.value
-
-
-_PROB = {"float32": MSA_PROB_F32, "bfloat16": MSA_PROB_BF16, "float16": MSA_PROB_F16}
 
 
 def msa_tree_verify(plan: Plan, target, tokens, parents, u_accept, u_sample, path, path_len, next_token, draft=None,
@@ -150,16 +159,19 @@ def msa_tree_verify(plan: Plan, target, tokens, parents, u_accept, u_sample, pat
     trees, rows, slots, _ = _figures(plan)
     if target is None or target.dim() != 2:
         raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: target is not a 2-D tensor")
-    vocab, kind = int(target.shape[1]), str(target.dtype)[6:]
-    check_tensor(who, "target", target, tuple(_PROB), vocab, rows)
-    check_tensor(who, "draft", draft, (kind,), vocab, rows)
-    for name, x, dtype, need in (("tokens", tokens, "int32", rows), ("parents", parents, "int32", rows),
-                                 ("u_accept", u_accept, "float32", rows), ("u_sample", u_sample, "float32", trees),
-                                 ("path_len", path_len, "int32", trees), ("next_token", next_token, "int32", trees)):
-        check_tensor(who, name, x, (dtype,), need)
-    check_tensor(who, "path", path, ("int32",), slots, trees)
+    vocab, kind = target.shape[1], target.dtype
+    check_tensor(who, "target", target, _PROB, vocab, rows)
+    if draft is not None:
+        check_tensor(who, "draft", draft, (kind,), vocab, rows)
+    check_tensor(who, "tokens", tokens, INT32, rows)
+    check_tensor(who, "parents", parents, INT32, rows)
+    check_tensor(who, "u_accept", u_accept, FLOAT32, rows)
+    check_tensor(who, "u_sample", u_sample, FLOAT32, trees)
+    check_tensor(who, "path", path, INT32, slots, trees)
+    check_tensor(who, "path_len", path_len, INT32, trees)
+    check_tensor(who, "next_token", next_token, INT32, trees)
     _check(_lib.msa_tree_verify(plan.handle, _PROB[kind], vocab, _addr(target), _row_stride(target, None, vocab),
                                 _addr(draft), 0 if draft is None else _row_stride(draft, None, vocab), _addr(tokens),
                                 _addr(parents), _addr(u_accept), _addr(u_sample), _addr(path),
                                 _row_stride(path, None, slots), _addr(path_len), _addr(next_token), _addr(workspace),
-                                workspace_bytes(workspace, 0), _stream(stream)))
+                                size_of(workspace), _stream(stream)))
