@@ -1,7 +1,9 @@
 // verify.hip -- verification of trees of drafted tokens against the target's
 // probabilities (msa_tree_verify; the rule is in include/msa_tree.h).
 //
-// Three launches.
+// A row of up to 32768 entries: one launch, a workgroup per tree that walks it and
+// then holds the last node's weights in registers (msa_verify_one).  Longer ones, whose
+// reading one CU would take too long over, in three:
 // msa_verify_walk, one workgroup per tree: the walk reads two numbers a slot
 // (p and q of the slot's token in its parent's row), all at once, and then
 // takes one decision after the other in registers.  Where a node's children
@@ -9,9 +11,10 @@
 // two scalars a and b (max(max(x, 0) / P - q, 0) = max(x / P - q, 0), as q >= 0),
 // so nothing of the vocabulary's length is stored; a second or later child's test
 // needs that residual's mass, for which the workgroup reads the node's two rows.
-// msa_verify_sums: the sum of r over each cell of 2048 entries of the vocabulary.
-// msa_verify_pick, one workgroup per tree: the cell, then the entry, at which the
-// running sum passes u T; a thread holds 8 neighbouring entries of the cell.
+// msa_verify_sums: the sum of r over each cell of 512 entries of the vocabulary, a wave
+// a cell, 8 neighbouring entries a lane.
+// msa_verify_pick, one wave per tree: the cell, then the lane, then the entry at which
+// the running sum passes u T.
 // Bound by reading one or two rows of the vocabulary per tree, and for few trees by
 // the chains of dependent reads in walk and pick.  (The pick used to be done by
 // the last workgroup of the sums to finish: the fences that this takes write
@@ -40,10 +43,10 @@ namespace msa {
 namespace {
 
 constexpr int kWalkThreads = 1024;
-constexpr int kCellThreads = 256;
-constexpr int kEach = 8;                        // neighbouring entries of a thread
-constexpr int kCell = kCellThreads * kEach;     // entries of a cell
 constexpr int kWave = 64;
+constexpr int kEach = 8;                // neighbouring entries of a lane
+constexpr int kCell = kWave * kEach;    // entries of a cell
+constexpr int kSumsThreads = 256;
 
 // How the next token's weights follow from the last node's row(s).
 enum Rest { kAsIs = 0, kResidual = 1, kWithout = 2 };
@@ -128,16 +131,18 @@ __device__ double residual_mass(const T* p, const T* q, double a, double b, int 
   return total;
 }
 
-// Every wave of the workgroup takes the walk's (uniform) decisions, so that
-// all of them meet in residual_mass.  Children lie behind their parent, so the
-// walk is one pass over the slots, 64 at a time.
+struct WalkLds {
+  int16_t parent[MSA_TREE_MAX_SLOTS];
+  int32_t token[MSA_TREE_MAX_SLOTS];
+  float p[MSA_TREE_MAX_SLOTS], q[MSA_TREE_MAX_SLOTS], u[MSA_TREE_MAX_SLOTS];
+  double part[kWalkThreads / kWave];
+};
+
+// The walk of a tree; path and path_len are written.  Every wave of the workgroup
+// takes the (uniform) decisions, so that all of them meet in residual_mass.
+// Children lie behind their parent, so the walk is one pass over the slots, 64 at a time.
 template <class T>
-__global__ __launch_bounds__(kWalkThreads) void msa_verify_walk_kernel(VerifyParams v) {
-  __shared__ int16_t s_parent[MSA_TREE_MAX_SLOTS];
-  __shared__ int32_t s_token[MSA_TREE_MAX_SLOTS];
-  __shared__ float s_p[MSA_TREE_MAX_SLOTS], s_q[MSA_TREE_MAX_SLOTS], s_u[MSA_TREE_MAX_SLOTS];
-  __shared__ double part[kWalkThreads / kWave];
-  const TreeSpan tree = v.trees[blockIdx.x];
+__device__ __forceinline__ WalkResult walk_tree(const VerifyParams& v, int tree_id, const TreeSpan& tree, WalkLds& s) {
   const T* target = static_cast<const T*>(v.target);
   const T* draft = static_cast<const T*>(v.draft);
   const int tid = threadIdx.x, lane = tid & 63;
@@ -148,43 +153,43 @@ __global__ __launch_bounds__(kWalkThreads) void msa_verify_walk_kernel(VerifyPar
     const int32_t token = v.tokens[row];
     const bool ok = up >= 0 && token >= 0 && token < v.vocab;
     const int64_t prow = (int64_t)tree.row0 + up;
-    s_parent[i] = (int16_t)up;
-    s_token[i] = token;
-    s_p[i] = ok ? clean(to_float(target[prow * v.target_stride + token])) : 0.0f;
-    s_q[i] = ok && draft ? clean(to_float(draft[prow * v.draft_stride + token])) : 0.0f;
-    s_u[i] = v.u_accept[row];
+    s.parent[i] = (int16_t)up;
+    s.token[i] = token;
+    s.p[i] = ok ? clean(to_float(target[prow * v.target_stride + token])) : 0.0f;
+    s.q[i] = ok && draft ? clean(to_float(draft[prow * v.draft_stride + token])) : 0.0f;
+    s.u[i] = v.u_accept[row];
   }
   __syncthreads();
 
-  int32_t* path = v.path + (int64_t)blockIdx.x * v.path_stride;
+  int32_t* path = v.path + (int64_t)tree_id * v.path_stride;
   int node = 0, len = 1;
   double a = 1.0, b = 0.0, mass = 1.0;
   bool known = true, dead = false, failed = false;  // mass known; no residual left; some child failed
   for (int base = 0; base < tree.n; base += kWave) {
     const int slot = base + lane;
     const bool in = slot < tree.n;
-    const int up = in ? s_parent[slot] : -1;
-    const int token = in ? s_token[slot] : -1;
+    const int up = in ? s.parent[slot] : -1;
+    const int token = in ? s.token[slot] : -1;
     uint64_t children = __ballot(in && up == node);
     while (children) {
       const int l = __builtin_ctzll(children), i = base + l;
       children &= children - 1;
-      double p = s_p[i], q = s_q[i];
-      const double u = s_u[i];
+      double p = s.p[i], q = s.q[i];
+      const double u = s.u[i];
       bool stays;
       if (draft) {
         if (!known && !dead) {
           mass = residual_mass(target + ((int64_t)tree.row0 + node) * v.target_stride,
-                               draft + ((int64_t)tree.row0 + node) * v.draft_stride, a, b, v.vocab, part);
+                               draft + ((int64_t)tree.row0 + node) * v.draft_stride, a, b, v.vocab, s.part);
           known = true;
           dead = !(mass > 0.0);
         }
         stays = !dead && u * q * mass < fmax(a * p - b * q, 0.0);
       } else {
         // a token that failed before under this node has nothing left
-        const int32_t x = s_token[i];
+        const int32_t x = s.token[i];
         bool twice = __any(in && up == node && slot < i && token == x);
-        for (int e = node + 1 + lane; e < base; e += kWave) twice |= s_parent[e] == node && s_token[e] == x;
+        for (int e = node + 1 + lane; e < base; e += kWave) twice |= s.parent[e] == node && s.token[e] == x;
         if (__any(twice)) p = 0.0;
         stays = u * mass < p;
         if (!stays) mass -= p;
@@ -209,18 +214,135 @@ __global__ __launch_bounds__(kWalkThreads) void msa_verify_walk_kernel(VerifyPar
   for (int i = len + tid; i < v.max_slots; i += kWalkThreads) path[i] = -1;
   if (tid == 0) {
     path[0] = 0;
-    v.path_len[blockIdx.x] = len;
-    WalkResult r{};
-    r.a = a;
-    r.b = b;
-    r.tree_row = tree.row0 + node;
-    r.node = node;
-    r.rest = !failed || dead ? kAsIs : draft ? kResidual : kWithout;
-    v.walk[blockIdx.x] = r;
+    v.path_len[tree_id] = len;
+  }
+  WalkResult r{};
+  r.a = a;
+  r.b = b;
+  r.tree_row = tree.row0 + node;
+  r.node = node;
+  r.rest = !failed || dead ? kAsIs : draft ? kResidual : kWithout;
+  return r;
+}
+
+template <class T>
+__global__ __launch_bounds__(kWalkThreads) void msa_verify_walk_kernel(VerifyParams v) {
+  __shared__ WalkLds s;
+  const WalkResult r = walk_tree<T>(v, (int)blockIdx.x, v.trees[blockIdx.x], s);
+  if (threadIdx.x == 0) v.walk[blockIdx.x] = r;
+}
+
+__device__ __forceinline__ double sum_of(const double (&w)[kEach]) {
+  return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+}
+
+// 8 entries of a row from t0, 0 behind its end
+template <class T>
+__device__ __forceinline__ void load_entries(const T* row, int t0, int vocab, float (&x)[kEach]) {
+  if (t0 + kEach <= vocab) {
+    load8(row + t0, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) x[i] = t0 + i < vocab ? clean(to_float(row[t0 + i])) : 0.0f;
   }
 }
 
-// The last node's weights, a cell at a time.
+// Walk, sums and pick of a row of up to kOneCells * kOneCell entries in one
+// workgroup.  A thread sums 8 neighbouring entries of each cell; the wave and cell, then the lane,
+// then the entry at which the running sum passes u T follow one from the other, the entry from
+// reading 8 of them again.
+constexpr int kOneCell = kWalkThreads * kEach;
+constexpr int kOneCells = 4;
+constexpr int kWaves = kWalkThreads / kWave;
+
+template <class T>
+__global__ __launch_bounds__(kWalkThreads) void msa_verify_one_kernel(VerifyParams v) {
+  __shared__ WalkLds s;
+  __shared__ uint32_t gone[kOneCells * kOneCell / 32];
+  __shared__ double part[kOneCells * kWaves];
+  const int tree_id = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const TreeSpan tree = v.trees[tree_id];
+  const double u = (double)fminf(fmaxf(v.u_sample[tree_id], 0.0f), 0x1.fffffep-1f);  // (fmaxf of NaN and 0 is 0)
+  const WalkResult r = walk_tree<T>(v, tree_id, tree, s);
+  const T* p = static_cast<const T*>(v.target) + (int64_t)r.tree_row * v.target_stride;
+  const T* q = static_cast<const T*>(v.draft) + (int64_t)r.tree_row * v.draft_stride;
+  if (r.rest == kWithout) {
+    for (int i = tid; i < kOneCells * kOneCell / 32; i += kWalkThreads) gone[i] = 0;
+    __syncthreads();
+    for (int i = r.node + 1 + tid; i < tree.n; i += kWalkThreads) {
+      const int32_t t = s.token[i];
+      if (s.parent[i] == r.node && t >= 0 && t < v.vocab) atomicOr(&gone[t >> 5], 1u << (t & 31));
+    }
+    __syncthreads();
+  }
+  // the thread's entries of a cell
+  auto load = [&](int c, int rest, double (&w)[kEach]) __attribute__((always_inline)) {
+    const int t0 = c * kOneCell + tid * kEach;
+    float x[kEach], y[kEach];
+    load_entries(p, t0, v.vocab, x);
+    if (rest == kResidual) load_entries(q, t0, v.vocab, y);
+    const uint32_t out = rest == kWithout ? gone[t0 >> 5] >> (t0 & 31) : 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      w[i] = rest == kResidual ? fmax(r.a * (double)x[i] - r.b * (double)y[i], 0.0) : out >> i & 1 ? 0.0 : (double)x[i];
+  };
+  int rest = r.rest;
+  double run[kOneCells], running, total;
+  for (;;) {
+#pragma unroll 2
+    for (int c = 0; c < kOneCells; ++c) {
+      run[c] = 0.0;
+      if (c * kOneCell < v.vocab) {  // (uniform)
+        double w[kEach];
+        load(c, rest, w);
+        run[c] = wave_scan(sum_of(w));
+      }
+      if (lane == kWave - 1) part[c * kWaves + wave] = run[c];
+    }
+    __syncthreads();
+    // the waves' sums, cell by cell: one of them a lane
+    static_assert(kOneCells * kWaves == kWave, "a lane for each wave and cell");
+    running = wave_scan(part[lane]);
+    total = lane_value(running, kWave - 1);
+    if (total > 0.0 || rest == kAsIs) break;  // (uniform)
+    rest = kAsIs;  // nothing is left: the row itself
+    __syncthreads();
+  }
+  if (!(total > 0.0)) {
+    if (tid == 0) v.next_token[tree_id] = -1;
+    return;
+  }
+  const double limit = u * total;
+  // where rounding leaves no sum above the limit, the last wave, lane and entry that hold any weight
+  const uint64_t past = __ballot(running > limit), some = __ballot(part[lane] > 0.0);
+  const int at_wave = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
+  if (wave != at_wave % kWaves) return;  // (uniform)
+  const int cell = at_wave / kWaves;
+  double mine = 0.0;
+#pragma unroll
+  for (int c = 0; c < kOneCells; ++c) mine = c == cell ? run[c] : mine;
+  const double before = lane_value(lane_below(running, 0.0), at_wave);
+  double w[kEach];
+  load(cell, rest, w);
+  const double below = lane_below(mine, 0.0);
+  const uint64_t past_lanes = __ballot(before + mine > limit), some_lanes = __ballot(sum_of(w) > 0.0);
+  const int at_lane = past_lanes ? __builtin_ctzll(past_lanes) : 63 - __builtin_clzll(some_lanes);
+  if (lane != at_lane) return;
+  double at = before + below;
+  int found = -1, last = -1;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    at += w[i];
+    if (w[i] > 0.0) {
+      last = cell * kOneCell + tid * kEach + i;
+      if (at > limit && found < 0) found = last;
+    }
+  }
+  v.next_token[tree_id] = found >= 0 ? found : last;
+}
+
+// The last node's weights, a cell at a time, by one wave.
 template <class T>
 struct Rows {
   const T *p, *q;
@@ -241,35 +363,22 @@ struct Rows {
     node = r.node;
   }
 
-  // the thread's 8 entries of a cell, 0 behind the row's end; `gone` (LDS) takes a bit for
-  // each of the cell's tokens that failed under the last node
+  // the lane's 8 entries of a cell, 0 behind the row's end; `gone` (the wave's own, in LDS) takes a
+  // bit for each of the cell's tokens that failed under the last node
   __device__ __forceinline__ void load(int cell, uint32_t* gone, double (&w)[kEach]) const {
-    const int tid = threadIdx.x, lo = cell * kCell, t0 = lo + tid * kEach;
+    const int lane = threadIdx.x & 63, lo = cell * kCell, t0 = lo + lane * kEach;
     float x[kEach], y[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) x[i] = y[i] = 0.0f;
-    if (t0 + kEach <= vocab) {
-      load8(p + t0, x);
-      if (rest == kResidual) load8(q + t0, y);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i)
-        if (t0 + i < vocab) {
-          x[i] = clean(to_float(p[t0 + i]));
-          if (rest == kResidual) y[i] = clean(to_float(q[t0 + i]));
-        }
-    }
+    load_entries(p, t0, vocab, x);
+    if (rest == kResidual) load_entries(q, t0, vocab, y);
     uint32_t out = 0;
-    if (rest == kWithout) {
-      __syncthreads();
-      if (tid < kCell / 32) gone[tid] = 0;
-      __syncthreads();
-      for (int i = node + 1 + tid; i < tree.n; i += kCellThreads) {
+    if (rest == kWithout) {  // (a wave's LDS accesses stay in order)
+      volatile uint32_t* bits = gone;
+      if (lane < kCell / 32) bits[lane] = 0;
+      for (int i = node + 1 + lane; i < tree.n; i += kWave) {
         const int32_t t = tokens[i];
         if (parents[i] == node && t >= lo && t - lo < kCell) atomicOr(&gone[(t - lo) >> 5], 1u << ((t - lo) & 31));
       }
-      __syncthreads();
-      out = gone[tid * kEach >> 5] >> (tid * kEach & 31);
+      out = bits[lane * kEach >> 5] >> (lane * kEach & 31);
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
@@ -277,39 +386,24 @@ struct Rows {
   }
 };
 
-__device__ __forceinline__ double sum_of(const double (&w)[kEach]) {
-  return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-}
-
-// sum over the workgroup, for every thread
-__device__ __forceinline__ double group_sum(double x, double* part) {
-  x = wave_sum(x);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-  __syncthreads();
-  return (part[0] + part[1]) + (part[2] + part[3]);
-}
-
 template <class T>
-__global__ __launch_bounds__(kCellThreads) void msa_verify_sums_kernel(VerifyParams v) {
-  __shared__ uint32_t gone[kCell / 32];
-  __shared__ double part[kCellThreads / kWave];
+__global__ __launch_bounds__(kSumsThreads) void msa_verify_sums_kernel(VerifyParams v) {
+  __shared__ uint32_t gone[kSumsThreads / kWave][kCell / 32];
   const int tree_id = blockIdx.x / v.groups, group = blockIdx.x - tree_id * v.groups;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Rows<T> rows(v, tree_id);
-  for (int cell = group; cell < v.cells; cell += v.groups) {
+  for (int cell = group * (kSumsThreads / kWave) + wave; cell < v.cells; cell += v.groups * (kSumsThreads / kWave)) {
     double w[kEach];
-    rows.load(cell, gone, w);
-    const double sum = group_sum(sum_of(w), part);
-    if (threadIdx.x == 0) v.sums[(int64_t)tree_id * v.cells + cell] = sum;
+    rows.load(cell, gone[wave], w);
+    const double sum = wave_sum(sum_of(w));
+    if ((threadIdx.x & 63) == 0) v.sums[(int64_t)tree_id * v.cells + cell] = sum;
   }
 }
 
 template <class T>
-__global__ __launch_bounds__(kCellThreads) void msa_verify_pick_kernel(VerifyParams v) {
+__global__ __launch_bounds__(kWave) void msa_verify_pick_kernel(VerifyParams v) {
   __shared__ uint32_t gone[kCell / 32];
-  __shared__ double part[kCellThreads / kWave];
-  __shared__ int s_found, s_last;
-  const int tree_id = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tree_id = blockIdx.x, lane = threadIdx.x;
   const double* sums = v.sums + (int64_t)tree_id * v.cells;
   const double u = (double)fminf(fmaxf(v.u_sample[tree_id], 0.0f), 0x1.fffffep-1f);  // (fmaxf of NaN and 0 is 0)
   Rows<T> rows(v, tree_id);
@@ -321,23 +415,23 @@ __global__ __launch_bounds__(kCellThreads) void msa_verify_pick_kernel(VerifyPar
     total = 0.0;
     for (int c = 0; c < v.cells; ++c) {
       rows.load(c, gone, w);
-      total += group_sum(sum_of(w), part);
+      total += wave_sum(sum_of(w));
     }
-    if (!(total > 0.0)) {  // (uniform over the workgroup)
-      if (tid == 0) v.next_token[tree_id] = -1;
+    if (!(total > 0.0)) {
+      if (lane == 0) v.next_token[tree_id] = -1;
       return;
     }
   }
-  const double x = u * total;
-  // the first cell whose running sum passes x; where rounding leaves none, the
+  const double limit = u * total;
+  // the first cell whose running sum passes the limit; where rounding leaves none, the
   // last one that holds any weight
   int found = -1, holds = 0;
   double before = 0.0, holds_before = 0.0, carry = 0.0;
   if (again) {
     for (int c = 0; c < v.cells && found < 0; ++c) {
       rows.load(c, gone, w);
-      const double s = group_sum(sum_of(w), part);
-      if (carry + s > x) {
+      const double s = wave_sum(sum_of(w));
+      if (carry + s > limit) {
         found = c;
         before = carry;
       } else if (s > 0.0) {
@@ -350,7 +444,7 @@ __global__ __launch_bounds__(kCellThreads) void msa_verify_pick_kernel(VerifyPar
   for (int c0 = 0; c0 < v.cells && found < 0 && !again; c0 += kWave) {
     const double s = c0 + lane < v.cells ? sums[c0 + lane] : 0.0;
     const double run = carry + wave_scan(s);
-    const uint64_t past = __ballot(run > x), some = __ballot(s > 0.0);
+    const uint64_t past = __ballot(run > limit), some = __ballot(s > 0.0);
     const double prev = lane_below(run, carry);
     if (past) {
       const int l = __builtin_ctzll(past);
@@ -369,38 +463,35 @@ __global__ __launch_bounds__(kCellThreads) void msa_verify_pick_kernel(VerifyPar
   }
   rows.load(found, gone, w);
   const double own = sum_of(w), run = wave_scan(own);
-  __syncthreads();
-  if (lane == kWave - 1) part[wave] = run;
-  if (tid == 0) s_found = 0x7fffffff, s_last = -1;
-  __syncthreads();
-  double at = before;
-  for (int i = 0; i < wave; ++i) at += part[i];
-  at += lane_below(run, 0.0);
-  int first = 0x7fffffff, last = -1;
+  const uint64_t past = __ballot(before + run > limit), some = __ballot(own > 0.0);
+  const int at_lane = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
+  double at = before + lane_below(run, 0.0);
+  int first = -1, last = -1;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     at += w[i];
     if (w[i] > 0.0) {
-      last = found * kCell + tid * kEach + i;
-      if (at > x && first == 0x7fffffff) first = last;
+      last = found * kCell + lane * kEach + i;
+      if (at > limit && first < 0) first = last;
     }
   }
-  if (first != 0x7fffffff) atomicMin(&s_found, first);
-  if (last >= 0) atomicMax(&s_last, last);
-  __syncthreads();
-  if (tid == 0) v.next_token[tree_id] = s_found != 0x7fffffff ? s_found : s_last;
+  if (lane == at_lane) v.next_token[tree_id] = first >= 0 ? first : last;
 }
 
 template <class T>
 int launch_verify(const VerifyParams& v, int trees, hipStream_t s) {
+  if (v.vocab <= kOneCells * kOneCell) {
+    hipLaunchKernelGGL(msa_verify_one_kernel<T>, dim3(trees), dim3(kWalkThreads), 0, s, v);
+    return (int)hipGetLastError();
+  }
   hipLaunchKernelGGL(msa_verify_walk_kernel<T>, dim3(trees), dim3(kWalkThreads), 0, s, v);
   int rc = (int)hipGetLastError();
   if (rc != 0) return rc;
-  hipLaunchKernelGGL(msa_verify_sums_kernel<T>, dim3((uint32_t)trees * (uint32_t)v.groups), dim3(kCellThreads), 0, s,
+  hipLaunchKernelGGL(msa_verify_sums_kernel<T>, dim3((uint32_t)trees * (uint32_t)v.groups), dim3(kSumsThreads), 0, s,
                      v);
   rc = (int)hipGetLastError();
   if (rc != 0) return rc;
-  hipLaunchKernelGGL(msa_verify_pick_kernel<T>, dim3(trees), dim3(kCellThreads), 0, s, v);
+  hipLaunchKernelGGL(msa_verify_pick_kernel<T>, dim3(trees), dim3(kWave), 0, s, v);
   return (int)hipGetLastError();
 }
 
@@ -480,8 +571,8 @@ extern "C" msa_status msa_tree_verify(msa_plan_t plan, int32_t prob_type, int32_
   v.vocab = vocab;
   v.max_slots = hp.max_slots;
   v.cells = (int32_t)msa::cells_of(vocab);
-  // a workgroup per cell, up to some 8192 of them
-  v.groups = (int32_t)std::min<int64_t>(v.cells, std::max<int64_t>(1, 8192 / trees));
+  // a wave per cell, up to some 8192 workgroups of them
+  v.groups = (int32_t)std::min<int64_t>((v.cells + 3) / 4, std::max<int64_t>(1, 8192 / trees));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int rc = prob_type == MSA_PROB_F32    ? msa::launch_verify<float>(v, (int)trees, s)
                  : prob_type == MSA_PROB_BF16 ? msa::launch_verify<__hip_bfloat16>(v, (int)trees, s)

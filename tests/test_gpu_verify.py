@@ -174,7 +174,7 @@ def test_shapes_and_types(shape, kind, dtype):
     Drafts(trees_of(1, [1, 2, 3, 8, 8, 16, 33, 64, 65, 5, 90], shape), 997, kind, dtype, pad=3).check()
 
 
-@pytest.mark.parametrize("vocab", [1, 2, 3, 7, 64, 255, 2047, 2048, 2049, 4099, 32000, 50257])
+@pytest.mark.parametrize("vocab", [1, 2, 3, 7, 64, 255, 511, 513, 2047, 4099, 8192, 8193, 32000, 32768, 32769, 50257])
 @pytest.mark.parametrize("kind", ["drawn", "best"])
 def test_vocabularies(vocab, kind):
     Drafts(trees_of(2, [6, 9, 1, 4], "tree"), vocab, kind).check()
