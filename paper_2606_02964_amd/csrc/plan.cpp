@@ -621,7 +621,17 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
   // even out the workgroups, where cutting every long unit sends more
   // partial results through the workspace (20 mixed sequences up to 4.6K,
   // 64 heads: 150 us with 512 of 944 units cut, 118 us with 240).
-  const int wgs_per_xcd = (int)(slots_total / kXcds);
+  // A plan with trees of less than one step of 1024 keys per CU and tile (one
+  // sequence or a few, whose whole tree is in one or two tiles) is cut down to 512 keys
+  // to give each CU one piece, alone on it (61 slots, 4 heads a KV head, 8 KV heads, over
+  // 8K keys: 26.0 us in 144 pieces of 15 steps, 22.5 us in 240 of 9).
+  int64_t unit_steps = 0;
+  for (const Unit& u : units) unit_steps += steps(u.kv_hi);
+  const bool lone = with_trees && cut_to_fit && P.tile_rows == kTileRowsNarrow && (int64_t)units.size() <= kCUs &&
+                    unit_steps < kCUs * kMinSplitSteps;
+  const int64_t min_steps = lone ? kMinSplitSteps / 2 : kMinSplitSteps;
+  const int64_t min_tail = lone ? kMinTailSteps / 2 : kMinTailSteps;
+  const int wgs_per_xcd = lone ? kCUs / kXcds : (int)(slots_total / kXcds);
   // a cut adds at most two partials: all of them fit the workspace of msa_forward_noalloc
   int64_t cuts_left = (int64_t)(MSA_NOALLOC_WORKSPACE_BYTES / sizeof(float)) / slot_floats(d, P.tile_rows) / 2;
   std::vector<Piece> pieces;
@@ -643,7 +653,7 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
         for (int32_t ci : qx) c += (steps(chunks[(size_t)ci].hi) + len - 1) / len;
         return c;
       };
-      int64_t key_steps = 0, longest = kMinSplitSteps;
+      int64_t key_steps = 0, longest = min_steps;
       for (int32_t ci : qx) {
         key_steps += steps(chunks[(size_t)ci].hi);
         longest = std::max(longest, steps(chunks[(size_t)ci].hi));
@@ -652,7 +662,7 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
       double mean_load = load[(size_t)x] / wgs_per_xcd;
       if ((double)longest + ov > mean_load)
         for (int it = 0; it < 2; ++it) {
-          const int64_t len = std::max<int64_t>(kMinSplitSteps, (int64_t)(mean_load - ov));
+          const int64_t len = std::max<int64_t>(min_steps, (int64_t)(mean_load - ov));
           const double items = std::min((double)pieces_at(len), (double)qx.size() + wgs_per_xcd);
           mean_load = ((double)key_steps + ov * items) / wgs_per_xcd;
         }
@@ -661,14 +671,14 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
       // few chunks: the shortest length whose pieces take one workgroup
       // each, if that is no longer than packing them would take
       if ((int64_t)qx.size() <= wgs_per_xcd) {
-        int64_t lo = kMinSplitSteps, hi = longest;
+        int64_t lo = min_steps, hi = longest;
         while (lo < hi) {
           const int64_t mid = (lo + hi) / 2;
           if (pieces_at(mid) <= wgs_per_xcd) hi = mid; else lo = mid + 1;
         }
         if ((double)lo + ov <= kOneRoundFactor * capacity) capacity = (double)lo + ov;
       }
-      capacity = std::max(capacity, kMinSplitSteps + ov);
+      capacity = std::max(capacity, min_steps + ov);
     }
     typedef std::pair<double, int> Slot;  // (load, workgroup of this XCD): least loaded first, then lowest
     std::vector<Slot> slots;  // heap of the workgroups in use; pieces take the idle ones first, in turn
@@ -692,10 +702,10 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
           slots.pop_back();
         }
         const int64_t n = steps(p.hi - p.lo);
-        if (cut_to_fit && cuts_left > 0 && n > kMinSplitSteps && s0.first + (double)n + ov > capacity) {
+        if (cut_to_fit && cuts_left > 0 && n > min_steps && s0.first + (double)n + ov > capacity) {
           --cuts_left;
           const int64_t fit = (int64_t)(capacity - s0.first - ov);
-          const int64_t take = std::min(std::max(fit, kMinTailSteps), n - kMinTailSteps);
+          const int64_t take = std::min(std::max(fit, min_tail), n - min_tail);
           const int32_t mid = (int32_t)(p.lo + take * kKvStep);
           tails.push(Piece{p.unit, mid, p.hi, -1});
           p.hi = mid;
