@@ -72,8 +72,8 @@ __global__ __launch_bounds__(kSelectThreads) void msa_kv_select_kernel(SelectPar
   const int seq = blockIdx.x / p.num_lists, list = blockIdx.x - seq * p.num_lists;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = max(0, min(p.seq_len[seq], p.max_len));
-  const int k = max(0, min(min(p.keep[seq], p.max_keep), n));
+  const int n = __builtin_amdgcn_readfirstlane(max(0, min(p.seq_len[seq], p.max_len)));
+  const int k = __builtin_amdgcn_readfirstlane(max(0, min(min(p.keep[seq], p.max_keep), n)));
   if (list == 0 && tid == 0) p.count[seq] = k;
   if (k == 0) return;
   const float* scores = p.scores + (int64_t)seq * p.s_sb + (int64_t)list * p.s_sl;
@@ -97,13 +97,14 @@ __global__ __launch_bounds__(kSelectThreads) void msa_kv_select_kernel(SelectPar
   // f(position, key) for the wave's elements, in order
   auto for_each = [&](auto&& f) __attribute__((always_inline)) {
     uint32_t start = first_of;
-    asm volatile("" : "+v"(start));  // (positions are not kept from one loop to the next)
+    int count = each;
+    asm volatile("" : "+v"(start), "+s"(count));  // (positions and bounds are not kept from one loop to the next)
     if constexpr (kEach > 0) {
 #pragma unroll
       for (int e = 0; e < kEach; ++e)
-        if (e < each) f(start + (uint32_t)e * 64u, held[e]);
+        if (e < count) f(start + (uint32_t)e * 64u, held[e]);
     } else {
-      for (int e = 0; e < each; ++e) f(start + (uint32_t)e * 64u, key_at(start + (uint32_t)e * 64u));
+      for (int e = 0; e < count; ++e) f(start + (uint32_t)e * 64u, key_at(start + (uint32_t)e * 64u));
     }
   };
 
@@ -111,21 +112,11 @@ __global__ __launch_bounds__(kSelectThreads) void msa_kv_select_kernel(SelectPar
   uint32_t found = 0;
   int ties = 0;
   if (k < n) {
-    int want = k, shift = 32, bits = 0;
+    int want = k, shift = 32;
     for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
     __syncthreads();
-    do {
-      const int above_bits = shift;  // bits of a key from here up are found
-      bits = min(kRadixBits, shift);
-      shift -= bits;
-      if (above_bits == 32) {
-        for_each([&](uint32_t, uint32_t key) { atomicAdd(&hist[key >> (32 - kRadixBits)], 1); });
-      } else {
-        const uint32_t share = found >> above_bits;
-        for_each([&](uint32_t, uint32_t key) {
-          if (key >> above_bits == share) atomicAdd(&hist[__builtin_amdgcn_ubfe(key, (uint32_t)shift, (uint32_t)bits)], 1);
-        });
-      }
+    // counted: bits of a key from `shift` up are found, or in the histogram
+    auto fix_bin = [&]() __attribute__((always_inline)) {
       __syncthreads();
       // the bin, from the top, in which the want-th key lies: each thread has two bins
       const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
@@ -149,7 +140,19 @@ __global__ __launch_bounds__(kSelectThreads) void msa_kv_select_kernel(SelectPar
         found -= 1;                                        // (their bin is not 0: key 0 is no position's)
         want = 0;
       }
-    } while (shift > 0 && want > 0);
+    };
+    shift -= kRadixBits;
+    for_each([&](uint32_t, uint32_t key) { atomicAdd(&hist[key >> (32 - kRadixBits)], 1); });
+    fix_bin();
+    while (shift > 0 && want > 0) {
+      const uint32_t share = found >> shift, above_bits = (uint32_t)shift;
+      const int bits = min(kRadixBits, shift);
+      shift -= bits;
+      for_each([&](uint32_t, uint32_t key) {
+        if (key >> above_bits == share) atomicAdd(&hist[__builtin_amdgcn_ubfe(key, (uint32_t)shift, (uint32_t)bits)], 1);
+      });
+      fix_bin();
+    }
     ties = want;
   }
 
