@@ -37,7 +37,7 @@ extern "C" {
  *                exp(scale * <q[r, h], k_j> - lse[r, h])
  *
  *   lse            device float32 [total_q, Hq], as msa_forward writes it (a row
- *                  whose lse is -inf gives no weight)
+ *                  whose lse is -inf gives no weight, if its q is finite)
  *   weights        device float32: w[b, g, j] at weights + b * stride_seq +
  *                  g * stride_head + j, 4-byte aligned; written at positions
  *                  0 .. (largest query position of b) of every sequence with

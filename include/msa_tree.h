@@ -117,7 +117,7 @@ msa_status msa_tree_forward(msa_plan_t plan, const void *q, const void *k_cache,
  *
  *   with draft probabilities q (each child of c drawn from q[c], independently):
  *     r = p[c], P = 1;  child i with token x stays iff u_i * q[c][x] * P < r[x];
- *     else r <- max(r / P - q[c], 0) and P <- sum r
+ *     else r <- max(r / P - q[c], 0) and P <- sum r  (where P is 0, every later child fails)
  *   without (children chosen by any rule that knows no random number of the
  *   target, such as the draft's best tokens):
  *     r = p[c], M = 1;  child i with token x stays iff u_i * M < r[x];

@@ -266,7 +266,7 @@ __global__ __launch_bounds__(kWalkThreads) void msa_verify_one_kernel(VerifyPara
   const double u = (double)fminf(fmaxf(v.u_sample[tree_id], 0.0f), 0x1.fffffep-1f);  // (fmaxf of NaN and 0 is 0)
   const WalkResult r = walk_tree<T>(v, tree_id, tree, s);
   const T* p = static_cast<const T*>(v.target) + (int64_t)r.tree_row * v.target_stride;
-  const T* q = static_cast<const T*>(v.draft) + (int64_t)r.tree_row * v.draft_stride;
+  const T* q = v.draft ? static_cast<const T*>(v.draft) + (int64_t)r.tree_row * v.draft_stride : nullptr;
   if (r.rest == kWithout) {
     for (int i = tid; i < kOneCells * kOneCell / 32; i += kWalkThreads) gone[i] = 0;
     __syncthreads();
@@ -356,7 +356,7 @@ struct Rows {
       : vocab(v.vocab), tree(v.trees[tree_id]), tokens(v.tokens + tree.row0), parents(v.parents + tree.row0) {
     const WalkResult r = v.walk[tree_id];
     p = static_cast<const T*>(v.target) + (int64_t)r.tree_row * v.target_stride;
-    q = static_cast<const T*>(v.draft) + (int64_t)r.tree_row * v.draft_stride;
+    q = v.draft ? static_cast<const T*>(v.draft) + (int64_t)r.tree_row * v.draft_stride : nullptr;
     a = r.a;
     b = r.b;
     rest = r.rest;

@@ -217,6 +217,31 @@ def test_select_more_to_keep_than_the_list_holds():
     check_select(rng.random((3, 1, 500), dtype=np.float32), [500, 300, 40], [400, 2 ** 31 - 1, -7], 4, 8, max_keep=60)
 
 
+def test_select_in_a_graph_and_on_another_stream():
+    g = torch.Generator().manual_seed(6)
+    x = torch.rand(3, 4, 3000, generator=g).cuda()
+    n, k = torch.tensor([3000, 17, 1200], dtype=torch.int32).cuda(), torch.tensor([900, 30, 1], dtype=torch.int32).cuda()
+    out = [torch.full((3, 4, 900), -1, dtype=torch.int32, device="cuda") for _ in range(3)]
+    cnt = torch.empty(3, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    msa.msa_kv_select(x, n, k, out[0], cnt, 4, 8, stream=torch.cuda.Stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        msa.msa_kv_select(x, n, k, out[1], cnt, 4, 8)
+    for _ in range(3):
+        x.copy_(torch.rand(3, 4, 3000, generator=g))
+        out[1].fill_(-1)
+        out[2].fill_(-1)
+        graph.replay()
+        msa.msa_kv_select(x, n, k, out[2], cnt, 4, 8)
+        torch.cuda.synchronize()
+        assert torch.equal(out[1], out[2])
+        for b in range(3):
+            want = select64(x[b, 2].cpu().numpy().astype(np.float64), int(n[b]), int(k[b]), 4, 8)
+            assert np.array_equal(out[1][b, 2, :len(want)].cpu().numpy(), want)
+
+
 def test_select_many_and_strided_lists():
     rng = np.random.default_rng(5)
     B, H, L = 40, 8, 777

@@ -136,6 +136,15 @@ def test_every_kernel_and_split(flags, split, heads):
     s.check()
 
 
+@pytest.mark.parametrize("ctx,slots,heads", [(8190, 61, (32, 8, 128)), (3000, 40, (16, 2, 128)), (5000, 100, (4, 4, 64))])
+def test_one_long_sequence(ctx, slots, heads):
+    """A small plan, cut to a piece per CU."""
+    s = Step([[tree(random.Random(1), ctx, slots)]], heads)
+    assert s.plan.info()["num_merge"] > 0 and s.plan.info()["num_workgroups"] <= 256
+    s.forward()
+    s.check()
+
+
 def test_many_workgroups():
     """More tiles than CUs: the 128-row kernel without helpers, several items a workgroup."""
     r = random.Random(2)
