@@ -50,7 +50,9 @@ extern "C" {
  *
  * plan, q, k_cache and block_table are those of the msa_forward call.  Sums
  * are in fp32, in a fixed order: equal calls give equal bits.  MSA_ERR_UNSUPPORTED
- * for a plan of msa_plan_tree; otherwise the statuses of msa_forward.
+ * for a plan of msa_plan_tree, or with too many rows or keys for a launch (2^31 (row,
+ * query head of a group) pairs, or some 2^32 (key, KV head) pairs); otherwise the statuses
+ * of msa_forward.
  */
 msa_status msa_kv_weights(msa_plan_t plan, const void *q, const void *k_cache,
                           const int32_t *block_table, const float *lse, float *weights,
@@ -85,7 +87,7 @@ msa_status msa_kv_weights_workspace(msa_plan_t plan, size_t *bytes);
  *
  * The whole of [0, n) is a list that msa_kv_compact takes with base 0.
  * MSA_ERR_INVALID_ARG for NULL or misaligned pointers, negative sizes or strides;
- * MSA_ERR_UNSUPPORTED for more than 2^31 - 1 lists.
+ * MSA_ERR_UNSUPPORTED for 2^22 lists or more.
  */
 msa_status msa_kv_select(int32_t num_seqs, int32_t num_lists, const float *scores,
                          int64_t score_stride_seq, int64_t score_stride_list, int32_t max_len,
@@ -117,7 +119,8 @@ msa_status msa_kv_select(int32_t num_seqs, int32_t num_lists, const float *score
  * ascending, the values moved are unspecified.  Sequences must not share the
  * blocks that are written, nor one sequence write a block that another reads.
  * MSA_ERR_INVALID_ARG, MSA_ERR_UNSUPPORTED as for msa_plan's shape; NULL or
- * misaligned pointers, negative max_count or strides: MSA_ERR_INVALID_ARG.
+ * misaligned pointers, negative max_count or strides: MSA_ERR_INVALID_ARG;
+ * MSA_ERR_UNSUPPORTED also for 2^21 (sequence, KV head) pairs or more.
  */
 msa_status msa_kv_compact(const msa_shape *shape, const int32_t *base, const int32_t *index,
                           int64_t index_stride_seq, int64_t index_stride_head,

@@ -51,7 +51,7 @@ extern "C" {
  *
  * The other arguments, the packed row order and the statuses are those of
  * msa_plan; MSA_ERR_UNSUPPORTED also for a tree of more than
- * MSA_TREE_MAX_SLOTS slots.  msa_kv_append, msa_check_block_table,
+ * MSA_TREE_MAX_SLOTS slots, and for 2^22 trees or more.  msa_kv_append, msa_check_block_table,
  * msa_plan_info (whose useful_flops counts tree rows as causal ones) and
  * msa_plan_export take the plan as any other; msa_forward does too and
  * attends to all segments as causal ones.

@@ -181,7 +181,9 @@ msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq
     const size_t n_joins = hp.weight_joins.size() * sizeof(msa::WeightsJoin);
     const size_t off_weights = off_trees + align_up(n_trees, 256);
     const size_t off_joins = off_weights + align_up(n_weights, 256);
-    const size_t bytes = std::max<size_t>(off_joins + n_joins, 256);
+    const size_t n_streams = hp.streams.size() * sizeof(msa::StreamItem);
+    const size_t off_streams = off_joins + align_up(n_joins, 256);
+    const size_t bytes = std::max<size_t>(off_streams + n_streams, 256);
     try {
       plan->staging.assign(bytes, 0);
     } catch (const std::bad_alloc&) {
@@ -197,6 +199,7 @@ msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq
     if (n_trees) std::memcpy(plan->staging.data() + off_trees, hp.trees.data(), n_trees);
     if (n_weights) std::memcpy(plan->staging.data() + off_weights, hp.weights.data(), n_weights);
     if (n_joins) std::memcpy(plan->staging.data() + off_joins, hp.weight_joins.data(), n_joins);
+    if (n_streams) std::memcpy(plan->staging.data() + off_streams, hp.streams.data(), n_streams);
     for (size_t i = 0; i < n_wg; ++i) {
       msa::WgHead h{};
       const int32_t first = hp.wg_ptr[i], end = hp.wg_ptr[i + 1];
@@ -234,6 +237,7 @@ msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq
     plan->d_trees = reinterpret_cast<const msa::TreeSpan*>(plan->dev + off_trees);
     plan->d_weights = reinterpret_cast<const msa::WeightsItem*>(plan->dev + off_weights);
     plan->d_weight_joins = reinterpret_cast<const msa::WeightsJoin*>(plan->dev + off_joins);
+    plan->d_streams = reinterpret_cast<const msa::StreamItem*>(plan->dev + off_streams);
   }
   *out = plan;
   return MSA_OK;

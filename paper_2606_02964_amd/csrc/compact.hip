@@ -41,7 +41,9 @@ constexpr int kSlice = 64;   // channels of a workgroup
 constexpr int kCompactThreads = 512;
 constexpr int kRing = 5;     // runs whose places are held: the one written, three ahead, one that slow waves still write
 constexpr int kAhead = 3;    // V blocks of a run that a wave reads ahead
-constexpr int kShort = 64;   // entries of a list that one workgroup holds
+constexpr int kShort = 64;   // entries of a list that are held between reading and writing
+constexpr int kShortSlice = 32;     // channels of a workgroup that does
+constexpr int kShortThreads = 128;
 
 struct CompactParams {
   const int32_t* base;  // may be null
@@ -307,10 +309,12 @@ __global__ __launch_bounds__(kCompactThreads, 4) void msa_kv_compact_kernel(Comp
 
 // Lists of up to kShort entries: everything is read before anything is written.
 template <int D>
-__global__ __launch_bounds__(256) void msa_kv_compact_short_kernel(CompactParams p) {
-  __shared__ __attribute__((aligned(16))) uint16_t s_k[kShort][D], s_v[kShort][D];
+__global__ __launch_bounds__(kShortThreads) void msa_kv_compact_short_kernel(CompactParams p) {
+  __shared__ __attribute__((aligned(16))) uint16_t s_k[kShort][kShortSlice], s_v[kShort][kShortSlice];
   __shared__ int64_t k_src[kShort], k_dst[kShort], v_src[kShort], v_dst[kShort];
-  const int seq = blockIdx.x / p.num_kv_heads, head = blockIdx.x - seq * p.num_kv_heads, tid = threadIdx.x;
+  constexpr int kParts = D / kShortSlice;
+  const int item = blockIdx.x / kParts, channel = (blockIdx.x - item * kParts) * kShortSlice;
+  const int seq = item / p.num_kv_heads, head = item - seq * p.num_kv_heads, tid = threadIdx.x;
   const int n = max(0, min(min(p.count[seq], p.max_count), kShort));
   if (n == 0) return;
   Moves mv;
@@ -332,42 +336,43 @@ __global__ __launch_bounds__(256) void msa_kv_compact_short_kernel(CompactParams
     v_dst[tid] = moves ? db * p.v_sb + dt : -1;
   }
   __syncthreads();
-  uint16_t* k = p.k + (int64_t)head * p.k_sh;
-  uint16_t* v = p.v + (int64_t)head * p.v_sh;
-  constexpr int kPieces = D / 8, kBatch = 8;  // reads of a thread under way together
-  const int pieces = n * kPieces, tokens = n * D;
-  for (int e0 = tid; e0 < tokens; e0 += 256 * kBatch) {
+  uint16_t* k = p.k + (int64_t)head * p.k_sh + channel;
+  uint16_t* v = p.v + (int64_t)head * p.v_sh + channel * p.v_sd;
+  constexpr int kPieces = kShortSlice / 8, kBatch = 8;  // reads of a thread under way together
+  const int pieces = n * kPieces, tokens = n * kShortSlice;
+  for (int e0 = tid; e0 < tokens; e0 += kShortThreads * kBatch) {
     uint16_t x[kBatch];
     uint4 y;
     const int ek = (e0 - tid) / kBatch + tid;  // a piece of K for 8 tokens of V
     if (ek < pieces) y = *reinterpret_cast<const uint4*>(k + k_src[ek / kPieces] + ek % kPieces * 8);
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int e = min(e0 + i * 256, tokens - 1);
-      x[i] = v[v_src[e / D] + e % D * p.v_sd];
+      const int e = min(e0 + i * kShortThreads, tokens - 1);
+      x[i] = v[v_src[e / kShortSlice] + e % kShortSlice * p.v_sd];
     }
     if (ek < pieces) *reinterpret_cast<uint4*>(&s_k[ek / kPieces][ek % kPieces * 8]) = y;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int e = min(e0 + i * 256, tokens - 1);
-      s_v[e / D][e % D] = x[i];
+      const int e = min(e0 + i * kShortThreads, tokens - 1);
+      s_v[e / kShortSlice][e % kShortSlice] = x[i];
     }
   }
   __syncthreads();
-  for (int e = tid; e < pieces; e += 256) {
+  for (int e = tid; e < pieces; e += kShortThreads) {
     const int64_t dst = k_dst[e / kPieces];
     if (dst >= 0) *reinterpret_cast<uint4*>(k + dst + e % kPieces * 8) = *reinterpret_cast<const uint4*>(&s_k[e / kPieces][e % kPieces * 8]);
   }
-  for (int e = tid; e < tokens; e += 256) {
-    const int64_t dst = v_dst[e / D];
-    if (dst >= 0) v[dst + e % D * p.v_sd] = s_v[e / D][e % D];
+  for (int e = tid; e < tokens; e += kShortThreads) {
+    const int64_t dst = v_dst[e / kShortSlice];
+    if (dst >= 0) v[dst + e % kShortSlice * p.v_sd] = s_v[e / kShortSlice][e % kShortSlice];
   }
 }
 
 template <int D>
 int launch_compact(const CompactParams& p, int64_t heads, hipStream_t s) {
   if (p.max_count <= kShort)
-    hipLaunchKernelGGL(msa_kv_compact_short_kernel<D>, dim3((uint32_t)heads), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(msa_kv_compact_short_kernel<D>, dim3((uint32_t)heads * (D / kShortSlice)), dim3(kShortThreads), 0,
+                       s, p);
   else
     hipLaunchKernelGGL(msa_kv_compact_kernel<D>, dim3((uint32_t)heads * (2 * D / kSlice)), dim3(kCompactThreads), 0, s,
                        p);
@@ -401,7 +406,9 @@ extern "C" msa_status msa_kv_compact(const msa_shape* shape, const int32_t* base
   if (!msa::aligned(k_cache, 16) || !msa::aligned(v_cache, 16) || !msa::aligned(base, 4) || !msa::aligned(index, 4) ||
       !msa::aligned(count, 4) || !msa::aligned(block_table, 4))
     return msa::fail(MSA_ERR_INVALID_ARG, "caches must be 16-byte, the others 4-byte aligned");
-  if ((int64_t)s.num_seqs * s.num_kv_heads >= ((int64_t)1 << 29)) return msa::fail(MSA_ERR_UNSUPPORTED, "too many heads for one launch");
+  // (a launch counts its threads in 32 bits: up to 4 x 512 for each)
+  if ((int64_t)s.num_seqs * s.num_kv_heads >= ((int64_t)1 << 21))
+    return msa::fail(MSA_ERR_UNSUPPORTED, "too many heads for one launch");
   msa::CompactParams p{};
   p.base = base;
   p.index = index;

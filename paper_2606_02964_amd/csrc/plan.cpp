@@ -104,6 +104,9 @@ struct Unit {
 // together read the same Q, from their XCD's L2, which they would not in long items
 // (one prompt of 16384 1166 us in items of 150 tiles, 1484 us in one round of
 // 1057): kMost tiles at most.
+// Sequences of up to kPairs pairs take as many waves as need no more than `wave_keys` keys
+// each, which is such that all of them are two rounds of the waves that the card holds
+// (12 a CU), 64 to 1024 keys.
 void plan_weights(HostPlan* plan) {
   constexpr int64_t kShortest = 8, kMost = 160, kSlots = 2 * kCUs, kItemTiles = 5, kRounds = 3, kStep = 4;
   HostPlan& P = *plan;
@@ -113,14 +116,15 @@ void plan_weights(HostPlan* plan) {
   };
   std::vector<Chunk> chunks;
   int64_t work = 0, longest = kShortest;  // tiles in all, of a chunk at most
+  int64_t stream_keys = 0;
   for (int64_t b = 0; b < B; ++b) {
     const int32_t lo = P.seq_row0[(size_t)b], hi = P.seq_row0[(size_t)b + 1];
     const int64_t pairs = (int64_t)(hi - lo) * G;
     if (pairs == 0) continue;
     const int32_t last = P.row_pos[(size_t)hi - 1];
     if (pairs <= kPairs) {
-      P.stream_keys += last + 1;
-      P.longest_stream = std::max<int64_t>(P.longest_stream, last + 1);
+      stream_keys += last + 1;
+      P.streams.push_back(StreamItem{(int32_t)b, lo, hi - lo, last, 0, 0});
       continue;
     }
     if (pairs >= (int64_t)1 << 31) continue;  // (such a call is refused)
@@ -132,6 +136,21 @@ void plan_weights(HostPlan* plan) {
       chunks.push_back(Chunk{(int32_t)b, (int32_t)key0, (int32_t)first, (int32_t)tiles, last});
       work += (tiles - first) * heads;
       longest = std::max(longest, tiles - first);
+    }
+  }
+  if (!P.streams.empty()) {
+    const int64_t share = stream_keys * heads / (2 * 12 * kCUs) / 64 * 64;
+    const int64_t most = std::min<int64_t>(std::max<int64_t>(share, 64), kStreamMost);
+    std::vector<StreamItem> seqs;
+    seqs.swap(P.streams);
+    P.streams.reserve((size_t)(stream_keys / (4 * most)) + seqs.size());
+    for (StreamItem s : seqs) {
+      const int64_t keys = (int64_t)s.last + 1, waves = (keys + 4 * most - 1) / (4 * most) * 4;
+      s.wave_keys = (int32_t)((keys + 32 * waves - 1) / (32 * waves) * 32);
+      for (int64_t key0 = 0; key0 < keys; key0 += 4 * s.wave_keys) {
+        s.key0 = (int32_t)key0;
+        P.streams.push_back(s);
+      }
     }
   }
   if (chunks.empty()) return;
@@ -260,7 +279,7 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
   P.precise_weights = (o.flags & MSA_PLAN_PRECISE_WEIGHTS) != 0;
   std::vector<int64_t> seq_row0(B + 1, 0);
   std::vector<int32_t> seq_maxpos(B, -1);
-  int64_t total = 0;
+  int64_t total = 0, num_trees = 0;
   const int64_t cap = (int64_t)s.max_blocks_per_seq * s.block_size;
   for (int32_t b = 0; b < B; ++b) {
     const int32_t L = seq_kv_len[b];
@@ -284,6 +303,9 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
         return fail(err, MSA_ERR_UNSUPPORTED,
                     "segment " + std::to_string(k) + " is a tree of more than " +
                         std::to_string(MSA_TREE_MAX_SLOTS) + " slots");
+      // (a workgroup of up to 512 threads each, and a launch counts its threads in 32 bits)
+      if (with_trees && (!seg_tree || seg_tree[k]) && ++num_trees >= ((int64_t)1 << 22))
+        return fail(err, MSA_ERR_UNSUPPORTED, "2^22 trees or more");
       total += n;
       if (total >= ((int64_t)1 << 31)) return fail(err, MSA_ERR_INVALID_ARG, "total_q >= 2^31");
       prev_end = st + n;

@@ -29,7 +29,7 @@ struct HostPlan {
   std::vector<WeightsItem> weights;      // key weights of sequences of more than kPairs pairs
   std::vector<WeightsJoin> weight_joins;
   int32_t weight_slots = 0;
-  int64_t stream_keys = 0, longest_stream = 0;  // key weights of the others: keys in all, of the longest
+  std::vector<StreamItem> streams;       // key weights of the others
   bool has_trees = false;         // built by msa_plan_tree (it may hold no tree all the same)
   std::vector<RowTree> row_tree;  // [total_q] if has_trees
   std::vector<TreeSpan> trees;    // one per tree segment

@@ -12,7 +12,7 @@ struct msa_plan_s {
   int device = -1;
   std::vector<char> staging;  // host image of the device buffer (kept alive for the async copy)
   char* dev = nullptr;        // device buffer: row_pos | work | merge | append | heads | seq rows | row trees | trees
-                              // | weights | joins
+                              // | weights | joins | streams
   const int32_t* d_row_pos = nullptr;
   const msa::WorkItem* d_work = nullptr;
   const msa::WgHead* d_heads = nullptr;
@@ -23,4 +23,5 @@ struct msa_plan_s {
   const msa::TreeSpan* d_trees = nullptr;      // [trees]
   const msa::WeightsItem* d_weights = nullptr;
   const msa::WeightsJoin* d_weight_joins = nullptr;
+  const msa::StreamItem* d_streams = nullptr;
 };

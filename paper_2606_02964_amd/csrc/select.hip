@@ -217,7 +217,7 @@ extern "C" msa_status msa_kv_select(int32_t num_seqs, int32_t num_lists, const f
     return msa::fail(MSA_ERR_INVALID_ARG, "strides must be >= 0");
   const int64_t lists = (int64_t)num_seqs * num_lists;
   if (lists == 0) return MSA_OK;
-  if (lists >= ((int64_t)1 << 31)) return msa::fail(MSA_ERR_UNSUPPORTED, "too many lists for one launch");
+  if (lists >= ((int64_t)1 << 32) / msa::kSelectThreads) return msa::fail(MSA_ERR_UNSUPPORTED, "too many lists for one launch");
   if (!scores || !seq_len || !keep || !index || !count)
     return msa::fail(MSA_ERR_INVALID_ARG, "scores, seq_len, keep, index, count must be non-null");
   if (!msa::aligned4(scores) || !msa::aligned4(seq_len) || !msa::aligned4(keep) || !msa::aligned4(index) ||

@@ -1,4 +1,4 @@
-// weights.h -- tables of the key weights' tiles kernel (msa_kv_weights), made with the plan.
+// weights.h -- tables of the key weights' kernels (msa_kv_weights), made with the plan.
 #pragma once
 
 #include <cstdint>
@@ -7,6 +7,17 @@ namespace msa {
 
 constexpr int kPairs = 32;        // (row, query head of a KV head) pairs of a tile
 constexpr int kGroupKeys = 256;   // keys of a workgroup
+
+// Keys of a sequence of up to kPairs pairs for the four waves of a workgroup (for every KV head):
+// wave w takes key0 + w wave_keys and the wave_keys - 1 after it, as far as `last`.
+struct StreamItem {
+  int32_t seq;
+  int32_t row0, nrows;  // the sequence's packed rows
+  int32_t last;         // position of the last of them
+  int32_t key0;
+  int32_t wave_keys;    // a multiple of 32, at most kStreamMost
+};
+constexpr int kStreamMost = 1024;  // a lane holds the id of one of a wave's blocks
 
 // Tiles tile0 .. tile1 - 1 of a sequence's pairs against 256 of its keys (for every KV head).
 struct WeightsItem {

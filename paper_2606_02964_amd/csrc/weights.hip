@@ -53,6 +53,7 @@ typedef __attribute__((address_space(3))) void lds_void_t;
 
 constexpr int kWaveKeys = kGroupKeys / 4;
 constexpr int kRing = 4;  // tiles in LDS
+constexpr int64_t kMostGroups = ((int64_t)1 << 32) / 256;  // workgroups of a launch: its threads are counted in 32 bits
 
 struct WeightsParams {
   const uint16_t* q;
@@ -63,11 +64,11 @@ struct WeightsParams {
   const float* lse;
   float* weights;
   float* sums;  // [slots][KV heads][kGroupKeys]
+  const StreamItem* streams;
   const WeightsItem* items;
   const WeightsJoin* joins;
   int64_t q_st, q_sh, k_sb, k_sh, k_st, w_sb, w_sh;
-  int32_t num_seqs, num_q_heads, num_kv_heads, max_blocks, group;
-  int32_t wave_keys;  // stream: keys of a wave, a multiple of 32, at most 1024
+  int32_t num_q_heads, num_kv_heads, max_blocks, group;
   uint32_t group_inv; // ceil(2^20 / G): r / G = r * group_inv >> 20 for r < 288
   float inv_scale, scale_log2;
   int32_t accumulate;
@@ -115,18 +116,15 @@ __device__ __forceinline__ float key_sum(const f32x16& s, float scale_log2, bool
 
 template <int D>
 __global__ __launch_bounds__(256, 3) void msa_kv_weights_stream_kernel(WeightsParams p) {
-  const int per_chunk = p.num_seqs * p.num_kv_heads;
-  const int chunk = blockIdx.x / per_chunk, rest = blockIdx.x - chunk * per_chunk;
-  const int seq = rest / p.num_kv_heads, kv_head = rest - seq * p.num_kv_heads;
+  const uint32_t item = blockIdx.x / (uint32_t)p.num_kv_heads;
+  const int kv_head = (int)(blockIdx.x - item * (uint32_t)p.num_kv_heads);
+  const StreamItem it = p.streams[item];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, hl = lane >> 5, ln = lane & 31;
-  const int row0 = p.seq_row0[seq], nrows = p.seq_row0[seq + 1] - row0;
-  const int G = p.group, n = nrows * G;
-  if (n == 0 || n > kPairs) return;
-  const int last = p.row_pos[row0 + nrows - 1];
-  const int64_t begin = ((int64_t)chunk * 4 + wave) * p.wave_keys;
-  if (begin > last) return;
-  const int k0 = (int)begin, k1 = min(k0 + p.wave_keys, last + 1);
+  const int seq = it.seq, row0 = it.row0, G = p.group, n = it.nrows * G;
+  const int64_t begin = (int64_t)it.key0 + wave * it.wave_keys;
+  if (begin > it.last) return;
+  const int k0 = (int)begin, k1 = min(it.wave_keys, it.last + 1 - k0) + k0;
 
   // the wave's block ids, one a lane
   const int32_t* table = p.block_table + (int64_t)seq * p.max_blocks + (k0 >> 4);
@@ -482,15 +480,10 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
   const size_t need = msa::workspace_of(hp);
   if (need > workspace_bytes || (need > 0 && (!workspace || !msa::aligned(workspace, 16))))
     return invalid("workspace must be 16-byte aligned and hold " + std::to_string(need) + " bytes");
-  // stream: two rounds of the waves that the card holds (12 a CU), 64 to 1024 keys each
-  int64_t wave_keys = hp.stream_keys * s.num_kv_heads / (2 * 12 * msa::kCUs) / 64 * 64;
-  wave_keys = wave_keys < 64 ? 64 : wave_keys > 1024 ? 1024 : wave_keys;
-  const int64_t stream_groups =
-      (hp.longest_stream + 4 * wave_keys - 1) / (4 * wave_keys) * s.num_seqs * s.num_kv_heads;
+  const int64_t streams = (int64_t)hp.streams.size() * s.num_kv_heads;
   const int64_t items = (int64_t)hp.weights.size() * s.num_kv_heads;
   const int64_t joins = (int64_t)hp.weight_joins.size() * s.num_kv_heads;
-  if (hp.total_q * hp.group >= ((int64_t)1 << 31) - 64 || stream_groups >= ((int64_t)1 << 31) ||
-      items >= ((int64_t)1 << 31))
+  if (hp.total_q * hp.group >= ((int64_t)1 << 31) - 64 || std::max(streams, items) >= msa::kMostGroups)
     return msa::fail(who, MSA_ERR_UNSUPPORTED, "too many rows or keys for one launch");
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev != plan->device)
@@ -510,7 +503,6 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
   p.k_st = s.k_stride_tok;
   p.w_sb = stride_seq;
   p.w_sh = stride_head;
-  p.num_seqs = s.num_seqs;
   p.num_q_heads = s.num_q_heads;
   p.num_kv_heads = s.num_kv_heads;
   p.max_blocks = s.max_blocks_per_seq;
@@ -519,14 +511,14 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
   p.inv_scale = 1.0f / s.scale;
   p.scale_log2 = s.scale * 1.4426950408889634f;
   p.accumulate = accumulate;
-  p.wave_keys = (int32_t)wave_keys;
+  p.streams = plan->d_streams;
   p.items = plan->d_weights;
   p.joins = plan->d_weight_joins;
   p.sums = static_cast<float*>(workspace);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   const bool d128 = s.head_dim == 128;
-  if (stream_groups > 0) {
-    const dim3 grid((uint32_t)stream_groups);
+  if (streams > 0) {
+    const dim3 grid((uint32_t)streams);
     if (d128)
       hipLaunchKernelGGL(msa::msa_kv_weights_stream_kernel<128>, grid, dim3(256), 0, st, p);
     else

@@ -67,6 +67,7 @@ def test_select_refusals():
     for kw in (dict(scores=P + 2), dict(n=P + 1), dict(keep=P + 3), dict(index=P + 2), dict(count=P + 2)):
         expect(INV, "aligned", call(**kw))
     expect(UNS, "too many", call(b=1 << 20, h=1 << 20))
+    expect(UNS, "too many", call(b=1 << 22, h=1))
     assert call(b=0) == OK and call(h=0) == OK
 
 
@@ -88,6 +89,7 @@ def test_compact_refusals():
         expect(INV, "non-null", call(**kw))
     for kw in (dict(k=P + 8), dict(v=P + 8), dict(base=P + 2), dict(index=P + 2), dict(count=P + 1), dict(bt=P + 2)):
         expect(INV, "aligned", call(**kw))
+    expect(UNS, "too many", call(s=shape(1 << 21)))
     assert call(s=shape(0)) == OK and call(mc=0) == OK
 
 

@@ -101,6 +101,13 @@ def test_weights_of_segments(heads):
     w.check(w.run())
 
 
+@pytest.mark.parametrize("heads", ["d128", "d64"])
+def test_weights_of_one_long_row_among_short_ones(heads):
+    ends = [3, 40000, 1, 0, 130, 2000] + [65] * 20
+    w = Weights([[(n - 1, 1)] if n else [] for n in ends], HEADS[heads], more=1)
+    w.check(w.run())
+
+
 def test_weights_sum_to_the_rows():
     """Each row's weights sum to one: over all keys, rows x heads."""
     w = Weights([[(0, 1500)], [(3000, 1), (3100, 100)]], (32, 8, 128))

@@ -55,6 +55,14 @@ def test_tree_size_limit(n, ok):
         msa.msa_plan_tree(shape(1), *layout, [0], flags=HOST)  # a causal segment may be longer
 
 
+def test_tree_count_limit():
+    n = 1 << 22
+    with pytest.raises(msa.MsaError, match="trees") as e:
+        msa.msa_plan_tree(shape(1, max_blocks_per_seq=n // 16), [n], [0, n], range(n), np.ones(n, dtype=np.int32),
+                          flags=msa.MSA_PLAN_HOST_ONLY)
+    assert e.value.status == msa.MSA_ERR_UNSUPPORTED
+
+
 def test_plan_refusals():
     layout = ([500, 300], [0, 1, 2], [10, 200], [20, 100])
     for bad in ([0, 2], [-1, 1], [1]):
