@@ -189,11 +189,12 @@ def check_select(scores, lens, keep, first=4, recent=16, max_keep=None):
             assert (index[b, h, k:] == -9).all()
 
 
+# buffers whose lists are held in 32 or 64 registers a thread, or read again
+@pytest.mark.parametrize("L", [70001, 65536, 32769, 32768, 8193])
 @pytest.mark.parametrize("values", ["spread", "ties", "equal", "signed", "odd"])
-def test_select_lengths(values):
+def test_select_lengths(values, L):
     rng = np.random.default_rng(2)
-    lens = [0, 1, 2, 20, 21, 63, 64, 65, 1000, 1023, 1024, 1025, 2049, 5000, 70000, -3, 99999]
-    L = 70001
+    lens = [0, 1, 2, 20, 21, 63, 64, 65, 1000, 1023, 1024, 1025, 2049, 5000, L - 1, -3, 99999]
     x = rng.random((len(lens), 2, L), dtype=np.float32) ** 4 * 8
     if values == "ties":
         x = np.round(x * 8) / 8
@@ -208,7 +209,7 @@ def test_select_lengths(values):
         x[:, :, 1::7] = -np.inf
         x[:, :, 2::11] = np.inf
         x[:, :, 3::5] = 1e-42
-    keep = [3, 1, 1, 20, 20, 30, 64, 10, 500, 1, 1024, 700, 0, 4999, 30000, 5, 70001]
+    keep = [3, 1, 1, 20, 20, 30, 64, 10, 500, 1, 1024, 700, 0, 4999, L // 7 * 3, 5, L]
     check_select(x.astype(np.float32), lens, keep)
 
 
