@@ -9,9 +9,14 @@
 // lies before everything that later runs read, so later runs' reads may be under way
 // already, and the only wait is for the run's own reads, of all waves, before
 // its writes (one barrier a run).
-// The places of the moves (index, then two block-table entries) are looked up four
-// runs ahead and the reads are issued two runs ahead, so that no run waits for a
-// chain of reads.
+// The places of the moves (index, then two block-table entries) are entered three runs
+// ahead, from reads issued one and two calls before that, and K and V are read two
+// runs ahead, so that no run waits for a chain of reads.  Reads and writes of a wave
+// complete in the order of their issue and are waited for by number, so every
+// read here is unconditional and so are the writes of a run whose places all move
+// (otherwise a wait for a run's reads would be one for all writes too, or, behind a
+// conditional look-up, for all reads: one sequence of 16K, half of it kept, 8 heads,
+// d = 128, took 124 us, now 89; of 128K 1182 us, now 677).
 //   K: rows of 128 bytes, in 16-byte pieces from register to register.
 //   V: a block holds the 16 tokens of a channel side by side, and kept tokens
 //   change their place in it.  The channel rows (32 bytes) of each source block
@@ -39,11 +44,13 @@ namespace {
 constexpr int kRun = 128;  // moves of a run: two waves' lanes hold one each
 constexpr int kSlice = 64;   // channels of a workgroup
 constexpr int kCompactThreads = 512;
-constexpr int kRing = 5;     // runs whose places are held: the one written, three ahead, one that slow waves still write
+constexpr int kRing = 5;     // runs whose places are held: the one written, three ahead, one slow waves still write
 constexpr int kAhead = 3;    // V blocks of a run that a wave reads ahead
 constexpr int kShort = 64;   // entries of a list that are held between reading and writing
 constexpr int kShortSlice = 32;     // channels of a workgroup that does
 constexpr int kShortThreads = 128;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));  // (stays in neighbouring registers)
 
 struct CompactParams {
   const int32_t* base;  // may be null
@@ -72,6 +79,8 @@ struct __attribute__((aligned(16))) PlacesV {
   uint8_t moved[kRun / 8];
   int32_t blocks[2];
 };
+// s_waitcnt's operand: no loads or stores outstanding
+constexpr int kNoLoads = 0x0f70;
 constexpr int kNoMove = kRun;  // a column of the staging buffer that is not written out
 
 // The list's positions, and where they are in the cache.
@@ -81,11 +90,15 @@ struct Moves {
   int64_t base, end, sb, st;
   int n, lead, num_blocks;
 
-  // the move at entry i (of the list's entries shifted by lead): index[i], or -1
-  __device__ __forceinline__ int32_t from(int i) const { return i >= 0 && i < n ? index[i] : -1; }
-  __device__ __forceinline__ int32_t block_at(int64_t pos) const {
-    const int32_t blk = pos >= 0 && pos < end ? table[pos / kBlockSize] : -1;
-    return blk < num_blocks ? blk : -1;
+  // the move at entry i (of the list's entries shifted by lead): index[i], or -1; read, and tested
+  __device__ __forceinline__ int32_t read_from(int i) const { return index[min(max(i, 0), n - 1)]; }
+  __device__ __forceinline__ int32_t from(int i, int32_t read) const { return i >= 0 && i < n ? read : -1; }
+  // the block of a position, or -1; likewise
+  __device__ __forceinline__ int32_t read_block(int64_t pos) const {
+    return table[min(max(pos, (int64_t)0), end - 1) / kBlockSize];
+  }
+  __device__ __forceinline__ int32_t block(int64_t pos, int32_t read) const {
+    return pos >= 0 && pos < end && read < num_blocks ? read : -1;
   }
 };
 
@@ -95,7 +108,7 @@ struct Lookup {
 };
 
 __device__ __forceinline__ bool is_move(const Moves& mv, int i, const Lookup& l) {
-  return l.from > i && l.src_blk >= 0 && l.dst_blk >= 0;  // (a place kept where it is needs no move)
+  return l.from > i && l.from >= 0 && l.src_blk >= 0 && l.dst_blk >= 0;  // (a place kept where it is needs no move)
 }
 __device__ __forceinline__ void enter_places(PlacesK& at, const Moves& mv, int i, const Lookup& l) {
   const int m = threadIdx.x;
@@ -128,29 +141,34 @@ __device__ __forceinline__ void enter_places(PlacesV& at, const Moves& mv, int i
 static_assert(kNoMove == 0x80, "the empty slot");
 
 // The lookups, by waves 0 and 1: each call enters one more run's places and issues
-// the reads of the runs behind it, which arrive until the next call.
+// the reads of the runs behind it, which arrive until the next call (each is used, and
+// tested, there and not before: a wait here would be one for all reads under way).
 struct Lookups {
-  Lookup held;       // of run `next`
-  int32_t from = -1; // index entry, of run next + 1
+  int32_t from = -1;             // index entry, of run `next`
+  int32_t src_blk = 0, dst_blk = 0;  // as read from the table, of run `next`
+  int32_t behind = 0;            // as read from the index, of run next + 1
   int next = 0;
-  __device__ __forceinline__ int entry(const Moves& mv, int run) const { return run * kRun - mv.lead + (int)threadIdx.x; }
-  __device__ __forceinline__ void start(const Moves& mv) {
-    held.from = mv.from(entry(mv, 0));
-    from = mv.from(entry(mv, 1));
-    blocks(mv, 0);
+  __device__ __forceinline__ int entry(const Moves& mv, int run) const {
+    return run * kRun - mv.lead + (int)threadIdx.x;
   }
-  __device__ __forceinline__ void blocks(const Moves& mv, int run) {
-    held.src_blk = held.from >= 0 ? mv.block_at(mv.base + held.from) : -1;
-    held.dst_blk = mv.block_at(mv.base + entry(mv, run));
+  __device__ __forceinline__ void start(const Moves& mv) {
+    from = mv.from(entry(mv, 0), mv.read_from(entry(mv, 0)));
+    read(mv);
+  }
+  __device__ __forceinline__ void read(const Moves& mv) {
+    src_blk = mv.read_block(mv.base + from);
+    dst_blk = mv.read_block(mv.base + entry(mv, next));
+    behind = mv.read_from(entry(mv, next + 1));
   }
   template <class P>
-  __device__ __forceinline__ void step(const Moves& mv, P (&ring)[kRing], int runs) {
-    if (threadIdx.x >= kRun || next >= runs) return;
-    enter_places(ring[next % kRing], mv, entry(mv, next), held);
+  __device__ __forceinline__ void step(const Moves& mv, P (&ring)[kRing]) {
+    if (threadIdx.x >= kRun) return;
+    const int i = entry(mv, next);
+    const Lookup l{from, mv.block(mv.base + from, src_blk), mv.block(mv.base + i, dst_blk)};
+    enter_places(ring[next % kRing], mv, i, l);
     ++next;
-    held.from = from;
-    blocks(mv, next);
-    from = mv.from(entry(mv, next + 1));
+    from = mv.from(entry(mv, next), behind);
+    read(mv);
   }
 };
 
@@ -162,31 +180,42 @@ __device__ __forceinline__ void compact_k(uint16_t* cache, const Moves& mv, Plac
                                           Lookups& look, int runs) {
   constexpr int kPieces = kSlice / 8, kEach = kRun * kPieces / kCompactThreads;
   const int tid = threadIdx.x;
-  uint4 x[2][kEach];
-  auto read = [&](uint4 (&y)[kEach], int r) __attribute__((always_inline)) {
+  u32x4 x[2][kEach];
+  auto read = [&](u32x4 (&y)[kEach], int r) __attribute__((always_inline)) {
     const PlacesK& at = ring[r % kRing];
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
-      y[e] = *reinterpret_cast<const uint4*>(cache + at.src[(e * kCompactThreads + tid) / kPieces] + tid % kPieces * 8);
+      y[e] = *reinterpret_cast<const u32x4*>(cache + at.src[(e * kCompactThreads + tid) / kPieces] + tid % kPieces * 8);
   };
-  auto step = [&](uint4 (&now)[kEach], int r) __attribute__((always_inline)) {
-    look.step(mv, ring, runs);
+  auto step = [&](u32x4 (&now)[kEach], int r) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) asm volatile("" : "+v"(now[e].x), "+v"(now[e].y), "+v"(now[e].z), "+v"(now[e].w));
+    for (int e = 0; e < kEach; ++e) asm volatile("" : "+v"(now[e]));
+    look.step(mv, ring);
     run_barrier();
     const PlacesK& at = ring[r % kRing];
+    int64_t dst[kEach];
+    bool all = true;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      const int64_t dst = at.dst[(e * kCompactThreads + tid) / kPieces];
-      if (dst >= 0) *reinterpret_cast<uint4*>(cache + dst + tid % kPieces * 8) = now[e];
+      dst[e] = at.dst[(e * kCompactThreads + tid) / kPieces];
+      all = all && dst[e] >= 0;
     }
-    read(now, min(r + 2, runs - 1));  // (unconditional, so that the wait for the run before it can leave it out)
+    if (__ballot(all) == ~0ull) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) *reinterpret_cast<u32x4*>(cache + dst[e] + tid % kPieces * 8) = now[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (dst[e] >= 0) *reinterpret_cast<u32x4*>(cache + dst[e] + tid % kPieces * 8) = now[e];
+      __builtin_amdgcn_s_waitcnt(kNoLoads);
+    }
+    read(now, r + 2);  // (unconditional, so that the wait for the run before it can leave it out)
   };
   read(x[0], 0);
-  read(x[1], min(1, runs - 1));
+  read(x[1], 1);
   for (int r = 0; r < runs; r += 2) {
     step(x[0], r);
-    if (r + 1 < runs) step(x[1], r + 1);
+    step(x[1], r + 1);  // (behind the last run nothing moves)
   }
 }
 
@@ -202,22 +231,22 @@ __device__ __forceinline__ void compact_v(uint16_t* cache, int64_t v_sd, const M
   // a lane holds 8 tokens of one channel, and of the channel 32 further on
   const int c = lane >> 1, side = lane & 1;
   const uint16_t* from = cache + c * v_sd + side * 8;
-  uint4 x[2][kAhead][2];
-  auto read_block = [&](uint4 (&y)[2], int64_t block) __attribute__((always_inline)) {
-    y[0] = *reinterpret_cast<const uint4*>(from + block);
-    y[1] = *reinterpret_cast<const uint4*>(from + block + 32 * v_sd);
+  u32x4 x[2][kAhead][2];
+  auto read_block = [&](u32x4 (&y)[2], int64_t block) __attribute__((always_inline)) {
+    y[0] = *reinterpret_cast<const u32x4*>(from + block);
+    y[1] = *reinterpret_cast<const u32x4*>(from + block + 32 * v_sd);
   };
-  auto read = [&](uint4 (&y)[kAhead][2], int r) __attribute__((always_inline)) {
+  auto read = [&](u32x4 (&y)[kAhead][2], int r) __attribute__((always_inline)) {
     const PlacesV& at = ring[r % kRing];
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) read_block(y[a], at.block[half][first_block + 4 * a]);
   };
-  auto step = [&](uint4 (&now)[kAhead][2], int r) __attribute__((always_inline)) {
+  auto step = [&](u32x4 (&now)[kAhead][2], int r) __attribute__((always_inline)) {
     const PlacesV& at = ring[r % kRing];
     const int blocks = __builtin_amdgcn_readfirstlane(at.blocks[half]);
     uint16_t(&to)[kSlice][kStagePitch] = stage[r & 1];
     // each of a lane's tokens to the column of its move (most hold one), or to the spare one
-    auto put = [&](const uint4 a, const uint4 b, int g) __attribute__((always_inline)) {
+    auto put = [&](const u32x4 a, const u32x4 b, int g) __attribute__((always_inline)) {
       const uint2 slot = *reinterpret_cast<const uint2*>(&at.slot[half][g][side * 8]);
       const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
@@ -227,45 +256,60 @@ __device__ __forceinline__ void compact_v(uint16_t* cache, int64_t v_sd, const M
         to[c + 32][m] = (uint16_t)(wb[t / 2] >> (t % 2 * 16));
       }
     };
-    look.step(mv, ring, runs);
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) asm volatile("" : "+v"(now[a][h]));
+    look.step(mv, ring);
 #pragma unroll
     for (int a = 0; a < kAhead; ++a)
       if (first_block + 4 * a < blocks) put(now[a][0], now[a][1], first_block + 4 * a);
     for (int g = first_block + 4 * kAhead; g < blocks; g += 4) {  // kept tokens far apart
-      uint4 y[2];
+      u32x4 y[2];
       read_block(y, at.block[half][g]);
       put(y[0], y[1], g);
     }
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) asm volatile("" : "+v"(now[a][h].x), "+v"(now[a][h].y), "+v"(now[a][h].z), "+v"(now[a][h].w));
     run_barrier();
+    // 32 channels of one destination block a wave
+    constexpr int kOut = kSlice * (kRun / 8) / kCompactThreads;
+    int moved[kOut], ch[kOut], piece[kOut];
+    bool all = true;
 #pragma unroll
-    for (int e = 0; e < kSlice * (kRun / 8) / kCompactThreads; ++e) {
-      // 32 channels of one destination block a wave
+    for (int e = 0; e < kOut; ++e) {
       const int unit = e * (kCompactThreads / 64) + wave;  // (block of the run, channel half)
-      const int piece = (unit >> 1) * 2 + side, ch = (unit & 1) * 32 + c;
-      const int moved = at.moved[piece];
-      if (moved == 0) continue;
-      const uint4 y = *reinterpret_cast<const uint4*>(&to[ch][piece * 8]);
-      uint16_t* dst = cache + at.piece[piece] + ch * v_sd;
-      if (moved == 0xff) {
-        *reinterpret_cast<uint4*>(dst) = y;
-      } else {
-        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-          if (moved >> t & 1) dst[t] = (uint16_t)(w[t / 2] >> (t % 2 * 16));
-      }
+      piece[e] = (unit >> 1) * 2 + side, ch[e] = (unit & 1) * 32 + c;
+      moved[e] = at.moved[piece[e]];
+      all = all && moved[e] == 0xff;
     }
-    read(now, min(r + 2, runs - 1));  // (unconditional, so that the wait for the run before it can leave it out)
+    if (__ballot(all) == ~0ull) {
+#pragma unroll
+      for (int e = 0; e < kOut; ++e)
+        *reinterpret_cast<u32x4*>(cache + at.piece[piece[e]] + ch[e] * v_sd) =
+            *reinterpret_cast<const u32x4*>(&to[ch[e]][piece[e] * 8]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kOut; ++e) {
+        if (moved[e] == 0) continue;
+        const u32x4 y = *reinterpret_cast<const u32x4*>(&to[ch[e]][piece[e] * 8]);
+        uint16_t* dst = cache + at.piece[piece[e]] + ch[e] * v_sd;
+        const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+        if (moved[e] == 0xff) {
+          *reinterpret_cast<u32x4*>(dst) = y;
+        } else {
+#pragma unroll
+          for (int t = 0; t < 8; ++t)
+            if (moved[e] >> t & 1) dst[t] = (uint16_t)(w[t / 2] >> (t % 2 * 16));
+        }
+      }
+      __builtin_amdgcn_s_waitcnt(kNoLoads);
+    }
+    read(now, r + 2);  // (unconditional, so that the wait for the run before it can leave it out)
   };
   read(x[0], 0);
-  read(x[1], min(1, runs - 1));
+  read(x[1], 1);
   for (int r = 0; r < runs; r += 2) {
     step(x[0], r);
-    if (r + 1 < runs) step(x[1], r + 1);
+    step(x[1], r + 1);  // (behind the last run nothing moves)
   }
 }
 
@@ -297,11 +341,11 @@ __global__ __launch_bounds__(kCompactThreads, 4) void msa_kv_compact_kernel(Comp
   Lookups look;
   if (tid < kRun) look.start(mv);
   if (is_v) {
-    for (int r = 0; r < 3; ++r) look.step(mv, ring.v, runs);
+    for (int r = 0; r < 3; ++r) look.step(mv, ring.v);
     __syncthreads();
     compact_v(p.v + (int64_t)head * p.v_sh + slice * kSlice * p.v_sd, p.v_sd, mv, ring.v, look, stage, runs);
   } else {
-    for (int r = 0; r < 3; ++r) look.step(mv, ring.k, runs);
+    for (int r = 0; r < 3; ++r) look.step(mv, ring.k);
     __syncthreads();
     compact_k(p.k + (int64_t)head * p.k_sh + slice * kSlice, mv, ring.k, look, runs);
   }
@@ -327,7 +371,7 @@ __global__ __launch_bounds__(kShortThreads) void msa_kv_compact_short_kernel(Com
   if (tid < n) {
     const int32_t from = mv.index[tid];
     const int64_t src = mv.base + from, dst = mv.base + tid;
-    const int32_t sb = from > tid ? mv.block_at(src) : -1, db = mv.block_at(dst);
+    const int32_t sb = from > tid ? mv.block(src, mv.read_block(src)) : -1, db = mv.block(dst, mv.read_block(dst));
     const bool moves = sb >= 0 && db >= 0;
     const int st = (int)(src & (kBlockSize - 1)), dt = (int)(dst & (kBlockSize - 1));
     k_src[tid] = moves ? sb * p.k_sb + st * p.k_st : 0;  // (what is read where nothing moves is not used)
