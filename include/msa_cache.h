@@ -120,7 +120,7 @@ msa_status msa_kv_select(int32_t num_seqs, int32_t num_lists, const float *score
  * blocks that are written, nor one sequence write a block that another reads.
  * MSA_ERR_INVALID_ARG, MSA_ERR_UNSUPPORTED as for msa_plan's shape; NULL or
  * misaligned pointers, negative max_count or strides: MSA_ERR_INVALID_ARG;
- * MSA_ERR_UNSUPPORTED also for 2^21 (sequence, KV head) pairs or more.
+ * MSA_ERR_UNSUPPORTED also for 2^20 (sequence, KV head) pairs or more.
  */
 msa_status msa_kv_compact(const msa_shape *shape, const int32_t *base, const int32_t *index,
                           int64_t index_stride_seq, int64_t index_stride_head,

@@ -10,13 +10,13 @@
 // already, and the only wait is for the run's own reads, of all waves, before
 // its writes (one barrier a run).
 // The places of the moves (index, then two block-table entries) are entered three runs
-// ahead, from reads issued one and two calls before that, and K and V are read two
-// runs ahead, so that no run waits for a chain of reads.  Reads and writes of a wave
-// complete in the order of their issue and are waited for by number, so every
-// read here is unconditional and so are the writes of a run whose places all move
-// (otherwise a wait for a run's reads would be one for all writes too, or, behind a
-// conditional look-up, for all reads: one sequence of 16K, half of it kept, 8 heads,
-// d = 128, took 124 us, now 89; of 128K 1182 us, now 677).
+// ahead by two waves of their own, and K and V are read two runs ahead.  Reads and
+// writes of a wave are waited for by number, in the order of their issue, so every
+// read is unconditional and so are the writes of a run whose places all move: else a
+// wait for a run's reads would be one for the last writes too, or, in a wave that
+// looks up places between them, for all reads (one sequence of 16K, half of it kept,
+// 8 heads, d = 128: 124 us like that, 89 waiting by number, 75 with the two waves; of
+// 128K: 1182, 680, 624 us).
 //   K: rows of 128 bytes, in 16-byte pieces from register to register.
 //   V: a block holds the 16 tokens of a channel side by side, and kept tokens
 //   change their place in it.  The channel rows (32 bytes) of each source block
@@ -24,10 +24,16 @@
 //   buffer in LDS, from where full pieces of 8 tokens are written.  (Gathered
 //   token by token in 2-byte reads, half of 16 x 16K tokens, 8 heads, d = 128, took
 //   955 us; a 2-byte read of a wave touches 16 lines for 128 bytes.)
-// Lists of up to 64 entries (a tree's path) take one workgroup per (sequence, KV
-// head), which holds all of their K and V in LDS between reading and writing.
-// Bound by HBM: each moved byte is read and written once, and whole blocks of V are
-// read where half of their tokens stay.
+// Bound by HBM where there are enough sequences: each moved byte is read and written
+// once, and whole blocks of V are read where half of their tokens stay (16 sequences
+// of up to 16K, half kept: 183 us for 0.75 GB).  One sequence alone is bound by
+// its runs, one after the other, 1.2 us each: the staging's 2-byte LDS writes and
+// the barrier (three or four runs ahead, or more blocks of one, take as long).
+// Lists of up to 64 entries (a tree's path) take a workgroup per (sequence, KV head,
+// 32 channels), which holds them in LDS between reading and writing: 48 x 8 heads,
+// 4 entries, 3.6 us; 128 x 8 heads, 8 and 64 entries 8.8 and 37 us, in runs 35 and
+// 51; one sequence of 64 entries 5.6 and 5.4.  (A workgroup for all 128 channels:
+// 10.2 us for the last, as 2-byte reads go one line each.)
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -43,8 +49,9 @@ namespace {
 
 constexpr int kRun = 128;  // moves of a run: two waves' lanes hold one each
 constexpr int kSlice = 64;   // channels of a workgroup
-constexpr int kCompactThreads = 512;
+constexpr int kCompactThreads = 512;  // that move; kRun more look up places
 constexpr int kRing = 5;     // runs whose places are held: the one written, three ahead, one slow waves still write
+constexpr int kReadAhead = 2;  // runs
 constexpr int kAhead = 3;    // V blocks of a run that a wave reads ahead
 constexpr int kShort = 64;   // entries of a list that are held between reading and writing
 constexpr int kShortSlice = 32;     // channels of a workgroup that does
@@ -102,7 +109,7 @@ struct Moves {
   }
 };
 
-// What lane m of waves 0 and 1 knows of move m of a run on the way to its places.
+// What lane m of the last two waves knows of move m of a run on the way to its places.
 struct Lookup {
   int32_t from = -1, src_blk = -1, dst_blk = -1;
 };
@@ -111,14 +118,14 @@ __device__ __forceinline__ bool is_move(const Moves& mv, int i, const Lookup& l)
   return l.from > i && l.from >= 0 && l.src_blk >= 0 && l.dst_blk >= 0;  // (a place kept where it is needs no move)
 }
 __device__ __forceinline__ void enter_places(PlacesK& at, const Moves& mv, int i, const Lookup& l) {
-  const int m = threadIdx.x;
+  const int m = threadIdx.x - kCompactThreads;
   const bool moves = is_move(mv, i, l);
   const int src_tok = (int)((mv.base + l.from) & (kBlockSize - 1)), dst_tok = (int)((mv.base + i) & (kBlockSize - 1));
   at.src[m] = moves ? l.src_blk * mv.sb + src_tok * mv.st : 0;  // (what is read where nothing moves is not used)
   at.dst[m] = moves ? l.dst_blk * mv.sb + dst_tok * mv.st : -1;
 }
 __device__ __forceinline__ void enter_places(PlacesV& at, const Moves& mv, int i, const Lookup& l) {
-  const int m = threadIdx.x, lane = m & 63, half = m >> 6;
+  const int m = threadIdx.x - kCompactThreads, lane = m & 63, half = m >> 6;
   const bool moves = is_move(mv, i, l);
   const int src_tok = (int)((mv.base + l.from) & (kBlockSize - 1)), dst_tok = (int)((mv.base + i) & (kBlockSize - 1));
   const int32_t blk = moves ? l.src_blk : -1;
@@ -140,7 +147,7 @@ __device__ __forceinline__ void enter_places(PlacesV& at, const Moves& mv, int i
 }
 static_assert(kNoMove == 0x80, "the empty slot");
 
-// The lookups, by waves 0 and 1: each call enters one more run's places and issues
+// The lookups, by the last two waves: each call enters one more run's places and issues
 // the reads of the runs behind it, which arrive until the next call (each is used, and
 // tested, there and not before: a wait here would be one for all reads under way).
 struct Lookups {
@@ -149,7 +156,7 @@ struct Lookups {
   int32_t behind = 0;            // as read from the index, of run next + 1
   int next = 0;
   __device__ __forceinline__ int entry(const Moves& mv, int run) const {
-    return run * kRun - mv.lead + (int)threadIdx.x;
+    return run * kRun - mv.lead + (int)threadIdx.x - kCompactThreads;
   }
   __device__ __forceinline__ void start(const Moves& mv) {
     from = mv.from(entry(mv, 0), mv.read_from(entry(mv, 0)));
@@ -162,7 +169,6 @@ struct Lookups {
   }
   template <class P>
   __device__ __forceinline__ void step(const Moves& mv, P (&ring)[kRing]) {
-    if (threadIdx.x >= kRun) return;
     const int i = entry(mv, next);
     const Lookup l{from, mv.block(mv.base + from, src_blk), mv.block(mv.base + i, dst_blk)};
     enter_places(ring[next % kRing], mv, i, l);
@@ -176,11 +182,23 @@ struct Lookups {
 // (the reads have arrived: their registers were used before it)
 __device__ __forceinline__ void run_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-__device__ __forceinline__ void compact_k(uint16_t* cache, const Moves& mv, PlacesK (&ring)[kRing],
-                                          Lookups& look, int runs) {
+// The last two waves' part: as many barriers as the others meet.
+template <class P>
+__device__ __forceinline__ void look_up(const Moves& mv, P (&ring)[kRing], int runs) {
+  Lookups look;
+  look.start(mv);
+  for (int r = 0; r < kReadAhead + 1; ++r) look.step(mv, ring);
+  __syncthreads();
+  for (int r = 0; r < (runs + 1) / 2 * 2; ++r) {
+    look.step(mv, ring);
+    run_barrier();
+  }
+}
+
+__device__ __forceinline__ void compact_k(uint16_t* cache, const PlacesK (&ring)[kRing], int runs) {
   constexpr int kPieces = kSlice / 8, kEach = kRun * kPieces / kCompactThreads;
   const int tid = threadIdx.x;
-  u32x4 x[2][kEach];
+  u32x4 x[kReadAhead][kEach];
   auto read = [&](u32x4 (&y)[kEach], int r) __attribute__((always_inline)) {
     const PlacesK& at = ring[r % kRing];
 #pragma unroll
@@ -190,7 +208,6 @@ __device__ __forceinline__ void compact_k(uint16_t* cache, const Moves& mv, Plac
   auto step = [&](u32x4 (&now)[kEach], int r) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) asm volatile("" : "+v"(now[e]));
-    look.step(mv, ring);
     run_barrier();
     const PlacesK& at = ring[r % kRing];
     int64_t dst[kEach];
@@ -209,7 +226,7 @@ __device__ __forceinline__ void compact_k(uint16_t* cache, const Moves& mv, Plac
         if (dst[e] >= 0) *reinterpret_cast<u32x4*>(cache + dst[e] + tid % kPieces * 8) = now[e];
       __builtin_amdgcn_s_waitcnt(kNoLoads);
     }
-    read(now, r + 2);  // (unconditional, so that the wait for the run before it can leave it out)
+    read(now, r + kReadAhead);  // (unconditional, so that the wait for the run before it can leave it out)
   };
   read(x[0], 0);
   read(x[1], 1);
@@ -223,15 +240,15 @@ __device__ __forceinline__ void compact_k(uint16_t* cache, const Moves& mv, Plac
 // columns for what does not stay
 constexpr int kStagePitch = kRun + 8;
 
-__device__ __forceinline__ void compact_v(uint16_t* cache, int64_t v_sd, const Moves& mv, PlacesV (&ring)[kRing],
-                                          Lookups& look, uint16_t (&stage)[2][kSlice][kStagePitch], int runs) {
+__device__ __forceinline__ void compact_v(uint16_t* cache, int64_t v_sd, const PlacesV (&ring)[kRing],
+                                          uint16_t (&stage)[2][kSlice][kStagePitch], int runs) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = wave & 1, first_block = wave >> 1;  // four waves share a half run's blocks
   // a lane holds 8 tokens of one channel, and of the channel 32 further on
   const int c = lane >> 1, side = lane & 1;
   const uint16_t* from = cache + c * v_sd + side * 8;
-  u32x4 x[2][kAhead][2];
+  u32x4 x[kReadAhead][kAhead][2];
   auto read_block = [&](u32x4 (&y)[2], int64_t block) __attribute__((always_inline)) {
     y[0] = *reinterpret_cast<const u32x4*>(from + block);
     y[1] = *reinterpret_cast<const u32x4*>(from + block + 32 * v_sd);
@@ -260,7 +277,6 @@ __device__ __forceinline__ void compact_v(uint16_t* cache, int64_t v_sd, const M
     for (int a = 0; a < kAhead; ++a)
 #pragma unroll
       for (int h = 0; h < 2; ++h) asm volatile("" : "+v"(now[a][h]));
-    look.step(mv, ring);
 #pragma unroll
     for (int a = 0; a < kAhead; ++a)
       if (first_block + 4 * a < blocks) put(now[a][0], now[a][1], first_block + 4 * a);
@@ -303,7 +319,7 @@ __device__ __forceinline__ void compact_v(uint16_t* cache, int64_t v_sd, const M
       }
       __builtin_amdgcn_s_waitcnt(kNoLoads);
     }
-    read(now, r + 2);  // (unconditional, so that the wait for the run before it can leave it out)
+    read(now, r + kReadAhead);  // (unconditional, so that the wait for the run before it can leave it out)
   };
   read(x[0], 0);
   read(x[1], 1);
@@ -314,7 +330,7 @@ __device__ __forceinline__ void compact_v(uint16_t* cache, int64_t v_sd, const M
 }
 
 template <int D>
-__global__ __launch_bounds__(kCompactThreads, 4) void msa_kv_compact_kernel(CompactParams p) {
+__global__ __launch_bounds__(kCompactThreads + kRun, 5) void msa_kv_compact_kernel(CompactParams p) {
   __shared__ union {
     PlacesK k[kRing];
     PlacesV v[kRing];
@@ -338,17 +354,18 @@ __global__ __launch_bounds__(kCompactThreads, 4) void msa_kv_compact_kernel(Comp
   mv.st = is_v ? 1 : p.k_st;
   mv.lead = (int)(mv.base & (kBlockSize - 1));  // runs end at block borders of the destination
   const int runs = (int)(((int64_t)mv.lead + mv.n + kRun - 1) / kRun);
-  Lookups look;
-  if (tid < kRun) look.start(mv);
-  if (is_v) {
-    for (int r = 0; r < 3; ++r) look.step(mv, ring.v);
-    __syncthreads();
-    compact_v(p.v + (int64_t)head * p.v_sh + slice * kSlice * p.v_sd, p.v_sd, mv, ring.v, look, stage, runs);
-  } else {
-    for (int r = 0; r < 3; ++r) look.step(mv, ring.k);
-    __syncthreads();
-    compact_k(p.k + (int64_t)head * p.k_sh + slice * kSlice, mv, ring.k, look, runs);
+  if (tid >= kCompactThreads) {
+    if (is_v)
+      look_up(mv, ring.v, runs);
+    else
+      look_up(mv, ring.k, runs);
+    return;
   }
+  __syncthreads();  // the first runs' places are entered
+  if (is_v)
+    compact_v(p.v + (int64_t)head * p.v_sh + slice * kSlice * p.v_sd, p.v_sd, ring.v, stage, runs);
+  else
+    compact_k(p.k + (int64_t)head * p.k_sh + slice * kSlice, ring.k, runs);
 }
 
 // Lists of up to kShort entries: everything is read before anything is written.
@@ -418,7 +435,7 @@ int launch_compact(const CompactParams& p, int64_t heads, hipStream_t s) {
     hipLaunchKernelGGL(msa_kv_compact_short_kernel<D>, dim3((uint32_t)heads * (D / kShortSlice)), dim3(kShortThreads), 0,
                        s, p);
   else
-    hipLaunchKernelGGL(msa_kv_compact_kernel<D>, dim3((uint32_t)heads * (2 * D / kSlice)), dim3(kCompactThreads), 0, s,
+    hipLaunchKernelGGL(msa_kv_compact_kernel<D>, dim3((uint32_t)heads * (2 * D / kSlice)), dim3(kCompactThreads + kRun), 0, s,
                        p);
   return (int)hipGetLastError();
 }
@@ -450,8 +467,8 @@ extern "C" msa_status msa_kv_compact(const msa_shape* shape, const int32_t* base
   if (!msa::aligned(k_cache, 16) || !msa::aligned(v_cache, 16) || !msa::aligned(base, 4) || !msa::aligned(index, 4) ||
       !msa::aligned(count, 4) || !msa::aligned(block_table, 4))
     return msa::fail(MSA_ERR_INVALID_ARG, "caches must be 16-byte, the others 4-byte aligned");
-  // (a launch counts its threads in 32 bits: up to 4 x 512 for each)
-  if ((int64_t)s.num_seqs * s.num_kv_heads >= ((int64_t)1 << 21))
+  // (a launch counts its threads in 32 bits: up to 4 x 640 for each)
+  if ((int64_t)s.num_seqs * s.num_kv_heads >= ((int64_t)1 << 20))
     return msa::fail(MSA_ERR_UNSUPPORTED, "too many heads for one launch");
   msa::CompactParams p{};
   p.base = base;
