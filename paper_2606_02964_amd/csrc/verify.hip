@@ -2,8 +2,11 @@
 // probabilities (msa_tree_verify; the rule is in include/msa_tree.h).
 //
 // A row of up to 32768 entries: one launch, a workgroup per tree that walks it and
-// then holds the last node's weights in registers (msa_verify_one).  Longer ones, whose
-// reading one CU would take too long over, in three:
+// then sums the last node's weights (msa_verify_one).  Longer ones, whose reading one
+// CU would take too long over, in three (in a captured graph, one launch and three: a
+// row of 8000 6.4 and 8.9 us, of 32768 8.5 and 8.7, two rows of that 10.0 and 9.0; 64
+// trees with two rows of 16000 9.0 and 11.2, of 32768 12.2 and 12.2; launched one by
+// one, two more launches take the host 7 us):
 // msa_verify_walk, one workgroup per tree: the walk reads two numbers a slot
 // (p and q of the slot's token in its parent's row), all at once, and then
 // takes one decision after the other in registers.  Where a node's children
@@ -16,7 +19,8 @@
 // msa_verify_pick, one wave per tree: the cell, then the lane, then the entry at which
 // the running sum passes u T.
 // Bound by reading one or two rows of the vocabulary per tree, and for few trees by
-// the chains of dependent reads in walk and pick.  (The pick used to be done by
+// the chains of dependent reads in walk and pick (32 trees, two rows of 131072 fp32
+// each: 17.4 us, a third in each launch; the rows' 34 MB alone take 6.1 us).  (The pick used to be done by
 // the last workgroup of the sums to finish: the fences that this takes write
 // back the whole L2 of an XCD, for every workgroup.)
 // Sums are in 64 bits: with 10^5 tokens the borders between neighbouring tokens
