@@ -100,15 +100,14 @@ struct Unit {
 // two or three rounds (8 KV heads: one prompt of 4096 93 us in one round, 105 us in
 // items of 24 tiles; of 8192 356 us in two full rounds, 395 us in items of 160;
 // 8 prompts of 2048 217 us in items of 32, 260 us in one round, whose longest item is
-// twice the mean).  Items in the order of their first tile: workgroups that run
-// together read the same Q, from their XCD's L2, which they would not in long items
-// (one prompt of 16384 1166 us in items of 150 tiles, 1484 us in one round of
-// 1057): kMost tiles at most.
+// twice the mean; one prompt of 131072 64.8 ms in items of some 800, 65.5 ms and a
+// list five times as long in items of 160).  Items in the order of their first tile:
+// workgroups that run together read the same Q, from their XCD's L2.
 // Sequences of up to kPairs pairs take as many waves as need no more than `wave_keys` keys
 // each, which is such that all of them are two rounds of the waves that the card holds
 // (12 a CU), 64 to 1024 keys.
 void plan_weights(HostPlan* plan) {
-  constexpr int64_t kShortest = 8, kMost = 160, kSlots = 2 * kCUs, kItemTiles = 5, kRounds = 3, kStep = 4;
+  constexpr int64_t kShortest = 8, kSlots = 2 * kCUs, kItemTiles = 5, kRounds = 3, kStep = 4;
   HostPlan& P = *plan;
   const int64_t G = P.group, B = P.shape.num_seqs, heads = P.shape.num_kv_heads;
   struct Chunk {
@@ -164,7 +163,7 @@ void plan_weights(HostPlan* plan) {
     return rounds <= kRounds ? (double)(rounds * (len + kItemTiles))
                              : (double)(work + items * kItemTiles) / kSlots + 0.5 * (double)(len + kItemTiles);
   };
-  int64_t part = std::min(longest, kMost);
+  int64_t part = longest;
   double least = cost_of(part);
   auto consider = [&](int64_t len) {
     const double cost = cost_of(len);
@@ -174,14 +173,14 @@ void plan_weights(HostPlan* plan) {
     }
   };
   for (int64_t rounds = 1; rounds <= kRounds; ++rounds) {  // the shortest that needs no more rounds
-    int64_t len = 1, most = (std::min(longest, kMost) + kStep - 1) / kStep;  // in steps of 4 tiles
+    int64_t len = 1, most = (longest + kStep - 1) / kStep;  // in steps of 4 tiles
     while (len < most) {
       const int64_t mid = (len + most) / 2;
       if (items_of(mid * kStep) <= rounds * kSlots) most = mid; else len = mid + 1;
     }
     consider(std::max(kShortest, len * kStep));
   }
-  for (int64_t len = kShortest; len < std::min(longest, kMost); len += len / 2) consider(len);
+  for (int64_t len = kShortest; len < longest; len += len / 2) consider(len);
   for (const Chunk& c : chunks) {
     const int64_t len = c.tiles - c.first, parts = (len + part - 1) / part;
     const int32_t slot0 = P.weight_slots;
@@ -303,7 +302,7 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
         return fail(err, MSA_ERR_UNSUPPORTED,
                     "segment " + std::to_string(k) + " is a tree of more than " +
                         std::to_string(MSA_TREE_MAX_SLOTS) + " slots");
-      // (a workgroup of up to 512 threads each, and a launch counts its threads in 32 bits)
+      // (a workgroup of up to 1024 threads each, and a launch counts its threads in 32 bits)
       if (with_trees && (!seg_tree || seg_tree[k]) && ++num_trees >= ((int64_t)1 << 22))
         return fail(err, MSA_ERR_UNSUPPORTED, "2^22 trees or more");
       total += n;
