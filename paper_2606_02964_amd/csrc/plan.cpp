@@ -110,12 +110,12 @@ void plan_weights(HostPlan* plan) {
   constexpr int64_t kShortest = 8, kSlots = 2 * kCUs, kItemTiles = 5, kRounds = 3, kStep = 4;
   HostPlan& P = *plan;
   const int64_t G = P.group, B = P.shape.num_seqs, heads = P.shape.num_kv_heads;
-  struct Chunk {
-    int32_t seq, key0, first, tiles, last;
+  struct Chunk {  // `count` times 256 keys from key0 that tiles first .. tiles - 1 see
+    int32_t seq, key0, count, first, tiles, last;
   };
   std::vector<Chunk> chunks;
   int64_t work = 0, longest = kShortest;  // tiles in all, of a chunk at most
-  int64_t stream_keys = 0;
+  int64_t stream_keys = 0, groups = 0;
   for (int64_t b = 0; b < B; ++b) {
     const int32_t lo = P.seq_row0[(size_t)b], hi = P.seq_row0[(size_t)b + 1];
     const int64_t pairs = (int64_t)(hi - lo) * G;
@@ -128,13 +128,17 @@ void plan_weights(HostPlan* plan) {
     }
     if (pairs >= (int64_t)1 << 31) continue;  // (such a call is refused)
     auto row = P.row_pos.begin() + lo;
-    for (int64_t key0 = 0; key0 <= last; key0 += kGroupKeys) {
+    const int64_t tiles = (pairs + kPairs - 1) / kPairs;
+    const int32_t whole = *row / kGroupKeys + 1;  // seen by all rows
+    chunks.push_back(Chunk{(int32_t)b, 0, whole, 0, (int32_t)tiles, last});
+    work += tiles * whole * heads;
+    longest = std::max(longest, tiles);
+    groups += last / kGroupKeys + 1;
+    for (int64_t key0 = (int64_t)whole * kGroupKeys; key0 <= last; key0 += kGroupKeys) {
       row = std::lower_bound(row, P.row_pos.begin() + hi, (int32_t)key0);
       const int64_t first = (int64_t)(row - P.row_pos.begin() - lo) * G / kPairs;
-      const int64_t tiles = (pairs + kPairs - 1) / kPairs;
-      chunks.push_back(Chunk{(int32_t)b, (int32_t)key0, (int32_t)first, (int32_t)tiles, last});
+      chunks.push_back(Chunk{(int32_t)b, (int32_t)key0, 1, (int32_t)first, (int32_t)tiles, last});
       work += (tiles - first) * heads;
-      longest = std::max(longest, tiles - first);
     }
   }
   if (!P.streams.empty()) {
@@ -155,7 +159,7 @@ void plan_weights(HostPlan* plan) {
   if (chunks.empty()) return;
   auto items_of = [&](int64_t len) {
     int64_t items = 0;
-    for (const Chunk& c : chunks) items += (uint32_t)(c.tiles - c.first + len - 1) / (uint32_t)len;
+    for (const Chunk& c : chunks) items += (int64_t)((uint32_t)(c.tiles - c.first + len - 1) / (uint32_t)len) * c.count;
     return items * heads;
   };
   auto cost_of = [&](int64_t len) {
@@ -163,8 +167,8 @@ void plan_weights(HostPlan* plan) {
     return rounds <= kRounds ? (double)(rounds * (len + kItemTiles))
                              : (double)(work + items * kItemTiles) / kSlots + 0.5 * (double)(len + kItemTiles);
   };
-  int64_t part = longest;
-  double least = cost_of(part);
+  int64_t part = longest;  // (kShortest: no chunk is cut)
+  double least = longest > kShortest ? cost_of(part) : 0.0;
   auto consider = [&](int64_t len) {
     const double cost = cost_of(len);
     if (cost < least) {
@@ -172,7 +176,7 @@ void plan_weights(HostPlan* plan) {
       part = len;
     }
   };
-  for (int64_t rounds = 1; rounds <= kRounds; ++rounds) {  // the shortest that needs no more rounds
+  for (int64_t rounds = 1; rounds <= kRounds && longest > kShortest; ++rounds) {  // the shortest that needs no more rounds
     int64_t len = 1, most = (longest + kStep - 1) / kStep;  // in steps of 4 tiles
     while (len < most) {
       const int64_t mid = (len + most) / 2;
@@ -181,22 +185,26 @@ void plan_weights(HostPlan* plan) {
     consider(std::max(kShortest, len * kStep));
   }
   for (int64_t len = kShortest; len < longest; len += len / 2) consider(len);
+  P.weights.reserve((size_t)groups);
   for (const Chunk& c : chunks) {
     const int64_t len = c.tiles - c.first, parts = (len + part - 1) / part;
-    const int32_t slot0 = P.weight_slots;
-    if (parts > 1) {
-      P.weight_joins.push_back(WeightsJoin{c.seq, c.key0, slot0, (int32_t)parts});
-      P.weight_slots += (int32_t)parts;
+    const int32_t row0 = P.seq_row0[(size_t)c.seq], nrows = P.seq_row0[(size_t)c.seq + 1] - row0;
+    for (int32_t g = 0; g < c.count; ++g) {
+      const int32_t key0 = c.key0 + g * kGroupKeys;
+      if (parts == 1) {
+        P.weights.push_back(WeightsItem{c.seq, key0, row0, nrows, c.first, c.tiles, -1, c.last});
+        continue;
+      }
+      P.weight_joins.push_back(WeightsJoin{c.seq, key0, P.weight_slots, (int32_t)parts});
+      for (int64_t i = 0; i < parts; ++i)
+        P.weights.push_back(WeightsItem{c.seq, key0, row0, nrows, (int32_t)(c.first + len * i / parts),
+                                        (int32_t)(c.first + len * (i + 1) / parts), P.weight_slots++, c.last});
     }
-    for (int64_t i = 0; i < parts; ++i)
-      P.weights.push_back(WeightsItem{c.seq, c.key0, P.seq_row0[(size_t)c.seq],
-                                      P.seq_row0[(size_t)c.seq + 1] - P.seq_row0[(size_t)c.seq],
-                                      (int32_t)(c.first + len * i / parts), (int32_t)(c.first + len * (i + 1) / parts),
-                                      parts > 1 ? (int32_t)(slot0 + i) : -1, c.last});
   }
-  std::stable_sort(P.weights.begin(), P.weights.end(), [](const WeightsItem& a, const WeightsItem& b) {
-    return a.seq != b.seq ? a.seq < b.seq : a.tile0 < b.tile0;
-  });
+  if (!P.weight_joins.empty())  // (uncut, they are in that order)
+    std::stable_sort(P.weights.begin(), P.weights.end(), [](const WeightsItem& a, const WeightsItem& b) {
+      return a.seq != b.seq ? a.seq < b.seq : a.tile0 < b.tile0;
+    });
 }
 
 }  // namespace
