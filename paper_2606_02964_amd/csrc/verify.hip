@@ -318,8 +318,10 @@ __global__ __launch_bounds__(kWalkThreads) void msa_verify_one_kernel(VerifyPara
     return;
   }
   const double limit = u * total;
-  // where rounding leaves no sum above the limit, the last wave, lane and entry that hold any weight
-  const uint64_t past = __ballot(running > limit), some = __ballot(part[lane] > 0.0);
+  // Where rounding leaves no sum above the limit, the last wave, lane and entry that hold any weight.
+  // (Neighbouring sums of a scan are added up in another order, so one without any weight may
+  // pass the limit where the one before it does not.)
+  const uint64_t some = __ballot(part[lane] > 0.0), past = __ballot(running > limit) & some;
   const int at_wave = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
   if (wave != at_wave % kWaves) return;  // (uniform)
   const int cell = at_wave / kWaves;
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(kWalkThreads) void msa_verify_one_kernel(VerifyPara
   double w[kEach];
   load(cell, rest, w);
   const double below = lane_below(mine, 0.0);
-  const uint64_t past_lanes = __ballot(before + mine > limit), some_lanes = __ballot(sum_of(w) > 0.0);
+  const uint64_t some_lanes = __ballot(sum_of(w) > 0.0), past_lanes = __ballot(before + mine > limit) & some_lanes;
   const int at_lane = past_lanes ? __builtin_ctzll(past_lanes) : 63 - __builtin_clzll(some_lanes);
   if (lane != at_lane) return;
   double at = before + below;
@@ -435,7 +437,7 @@ __global__ __launch_bounds__(kWave) void msa_verify_pick_kernel(VerifyParams v) 
     for (int c = 0; c < v.cells && found < 0; ++c) {
       rows.load(c, gone, w);
       const double s = wave_sum(sum_of(w));
-      if (carry + s > limit) {
+      if (s > 0.0 && carry + s > limit) {
         found = c;
         before = carry;
       } else if (s > 0.0) {
@@ -448,7 +450,7 @@ __global__ __launch_bounds__(kWave) void msa_verify_pick_kernel(VerifyParams v) 
   for (int c0 = 0; c0 < v.cells && found < 0 && !again; c0 += kWave) {
     const double s = c0 + lane < v.cells ? sums[c0 + lane] : 0.0;
     const double run = carry + wave_scan(s);
-    const uint64_t past = __ballot(run > limit), some = __ballot(s > 0.0);
+    const uint64_t some = __ballot(s > 0.0), past = __ballot(run > limit) & some;
     const double prev = lane_below(run, carry);
     if (past) {
       const int l = __builtin_ctzll(past);
@@ -467,7 +469,7 @@ __global__ __launch_bounds__(kWave) void msa_verify_pick_kernel(VerifyParams v) 
   }
   rows.load(found, gone, w);
   const double own = sum_of(w), run = wave_scan(own);
-  const uint64_t past = __ballot(before + run > limit), some = __ballot(own > 0.0);
+  const uint64_t some = __ballot(own > 0.0), past = __ballot(before + run > limit) & some;
   const int at_lane = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
   double at = before + lane_below(run, 0.0);
   int first = -1, last = -1;

@@ -230,6 +230,19 @@ def test_odd_probabilities_and_tokens():
         d.check()
 
 
+@pytest.mark.parametrize("vocab,cell", [(600, 8), (40000, 8), (40000, 512), (30000, 512)])
+def test_a_drawn_token_has_weight(vocab, cell):
+    """Sums whose rounding depends on their order: e + e + 1 + 0 is 1 or 1 + 2 e, with e = 2^-53, and half the total
+    lies between.  Cells of 8 entries are a lane's, of 512 a wave's."""
+    row = torch.zeros(1, vocab)
+    row[0, 0] = row[0, cell] = 2.0 ** -53
+    row[0, 2 * cell] = row[0, 4 * cell] = 1.0
+    d = Drafts([[-1]], vocab)
+    d.target, d.draft, d.u_sample = row, None, torch.tensor([0.5])
+    _, _, token = d.run()
+    assert int(token[0]) in (2 * cell, 4 * cell)
+
+
 def test_tokens_follow_the_target():
     """First kept token of 40000 one-level trees of three drafts, against the target's probabilities: each frequency
     within 5 standard deviations, and the drafts' own distribution is not."""
