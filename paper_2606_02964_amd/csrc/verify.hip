@@ -3,10 +3,10 @@
 //
 // A row of up to 32768 entries: one launch, a workgroup per tree that walks it and
 // then sums the last node's weights (msa_verify_one).  Longer ones, whose reading one
-// CU would take too long over, in three (in a captured graph, one launch and three: a
-// row of 8000 6.4 and 8.9 us, of 32768 8.5 and 8.7, two rows of that 10.0 and 9.0; 64
-// trees with two rows of 16000 9.0 and 11.2, of 32768 12.2 and 12.2; launched one by
-// one, two more launches take the host 7 us):
+// CU would take too long over, in two (in a captured graph, one launch and two: a
+// row of 8000 6.5 and 8.7 us, of 32768 8.5 and 8.5, two rows of that 10.1 and 9.0; 64
+// trees with two rows of 16000 9.0 and 10.2, of 32768 12.1 and 11.7; launched one by
+// one, another launch takes the host 3.6 us):
 // msa_verify_walk, one workgroup per tree: the walk reads two numbers a slot
 // (p and q of the slot's token in its parent's row), all at once, and then
 // takes one decision after the other in registers.  Where a node's children
@@ -15,14 +15,14 @@
 // so nothing of the vocabulary's length is stored; a second or later child's test
 // needs that residual's mass, for which the workgroup reads the node's two rows.
 // msa_verify_sums: the sum of r over each cell of 512 entries of the vocabulary, a wave
-// a cell, 8 neighbouring entries a lane.
-// msa_verify_pick, one wave per tree: the cell, then the lane, then the entry at which
-// the running sum passes u T.
+// a cell, 8 neighbouring entries a lane.  The tree's last workgroup to finish picks, by
+// one wave: the cell, then the lane, then the entry at which the running sum passes u T.
+// It learns the others' sums by accesses that go through to where the XCDs meet; as a
+// launch of its own the pick took as long and the host 3.6 us more, and with fences
+// that write back an XCD's whole L2, for every workgroup, 32 trees took 80 us.
 // Bound by reading one or two rows of the vocabulary per tree, and for few trees by
 // the chains of dependent reads in walk and pick (32 trees, two rows of 131072 fp32
-// each: 17.4 us, a third in each launch; the rows' 34 MB alone take 6.1 us).  (The pick used to be done by
-// the last workgroup of the sums to finish: the fences that this takes write
-// back the whole L2 of an XCD, for every workgroup.)
+// each: 16.8 us; the rows' 34 MB alone take 6.1 us).
 // Sums are in 64 bits: with 10^5 tokens the borders between neighbouring tokens
 // are about 10^-5 of the mass apart and a 32-bit running sum would pick a
 // neighbour once in some hundred draws; and the tests' products (24 + 24 bits)
@@ -50,7 +50,7 @@ constexpr int kWalkThreads = 1024;
 constexpr int kWave = 64;
 constexpr int kEach = 8;                // neighbouring entries of a lane
 constexpr int kCell = kWave * kEach;    // entries of a cell
-constexpr int kSumsThreads = 256;
+constexpr int kSumsThreads = 512;
 
 // How the next token's weights follow from the last node's row(s).
 enum Rest { kAsIs = 0, kResidual = 1, kWithout = 2 };
@@ -60,7 +60,7 @@ struct WalkResult {
   int32_t tree_row;  // of the last node
   int32_t node;      // its slot
   int32_t rest;
-  int32_t pad;
+  uint32_t done;     // workgroups of the sums that are finished
 };
 
 struct VerifyParams {
@@ -392,29 +392,25 @@ struct Rows {
   }
 };
 
-template <class T>
-__global__ __launch_bounds__(kSumsThreads) void msa_verify_sums_kernel(VerifyParams v) {
-  __shared__ uint32_t gone[kSumsThreads / kWave][kCell / 32];
-  const int tree_id = blockIdx.x / v.groups, group = blockIdx.x - tree_id * v.groups;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Rows<T> rows(v, tree_id);
-  for (int cell = group * (kSumsThreads / kWave) + wave; cell < v.cells; cell += v.groups * (kSumsThreads / kWave)) {
-    double w[kEach];
-    rows.load(cell, gone[wave], w);
-    const double sum = wave_sum(sum_of(w));
-    if ((threadIdx.x & 63) == 0) v.sums[(int64_t)tree_id * v.cells + cell] = sum;
-  }
+// Sums on their way from one workgroup to another of the launch: written and read
+// through to where all XCDs meet, so that no cache has to be written back or emptied.
+__device__ __forceinline__ void shared_store(double* at, double x) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(at), __builtin_bit_cast(uint64_t, x), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ double shared_load(const double* at) {
+  return __builtin_bit_cast(double, __hip_atomic_load(reinterpret_cast<const uint64_t*>(at), __ATOMIC_RELAXED,
+                                                      __HIP_MEMORY_SCOPE_AGENT));
 }
 
+// The cell, then the lane, then the entry at which the running sum passes u T, by one wave.
 template <class T>
-__global__ __launch_bounds__(kWave) void msa_verify_pick_kernel(VerifyParams v) {
-  __shared__ uint32_t gone[kCell / 32];
-  const int tree_id = blockIdx.x, lane = threadIdx.x;
+__device__ __forceinline__ void pick(const VerifyParams& v, int tree_id, Rows<T> rows, uint32_t* gone) {
+  const int lane = threadIdx.x & 63;
   const double* sums = v.sums + (int64_t)tree_id * v.cells;
   const double u = (double)fminf(fmaxf(v.u_sample[tree_id], 0.0f), 0x1.fffffep-1f);  // (fmaxf of NaN and 0 is 0)
-  Rows<T> rows(v, tree_id);
   double w[kEach], total = 0.0;
-  for (int c0 = 0; c0 < v.cells; c0 += kWave) total += wave_sum(c0 + lane < v.cells ? sums[c0 + lane] : 0.0);
+  for (int c0 = 0; c0 < v.cells; c0 += kWave) total += wave_sum(c0 + lane < v.cells ? shared_load(sums + c0 + lane) : 0.0);
   const bool again = !(total > 0.0);  // nothing is left: the row itself, summed here (it hardly ever is)
   if (again) {
     rows.rest = kAsIs;
@@ -448,7 +444,7 @@ __global__ __launch_bounds__(kWave) void msa_verify_pick_kernel(VerifyParams v) 
     }
   }
   for (int c0 = 0; c0 < v.cells && found < 0 && !again; c0 += kWave) {
-    const double s = c0 + lane < v.cells ? sums[c0 + lane] : 0.0;
+    const double s = c0 + lane < v.cells ? shared_load(sums + c0 + lane) : 0.0;
     const double run = carry + wave_scan(s);
     const uint64_t some = __ballot(s > 0.0), past = __ballot(run > limit) & some;
     const double prev = lane_below(run, carry);
@@ -485,6 +481,28 @@ __global__ __launch_bounds__(kWave) void msa_verify_pick_kernel(VerifyParams v) 
 }
 
 template <class T>
+__global__ __launch_bounds__(kSumsThreads) void msa_verify_sums_kernel(VerifyParams v) {
+  __shared__ uint32_t gone[kSumsThreads / kWave][kCell / 32];
+  __shared__ uint32_t before;
+  const int tree_id = blockIdx.x / v.groups, group = blockIdx.x - tree_id * v.groups;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Rows<T> rows(v, tree_id);
+  for (int cell = group * (kSumsThreads / kWave) + wave; cell < v.cells; cell += v.groups * (kSumsThreads / kWave)) {
+    double w[kEach];
+    rows.load(cell, gone[wave], w);
+    const double sum = wave_sum(sum_of(w));
+    if ((threadIdx.x & 63) == 0) shared_store(v.sums + (int64_t)tree_id * v.cells + cell, sum);
+  }
+  // The tree's last workgroup to arrive here picks: every wave's sums have arrived before its workgroup is counted.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    before = __hip_atomic_fetch_add(&v.walk[tree_id].done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  if (before + 1 == (uint32_t)v.groups && wave == 0) pick<T>(v, tree_id, rows, gone[0]);
+}
+
+template <class T>
 int launch_verify(const VerifyParams& v, int trees, hipStream_t s) {
   if (v.vocab <= kOneCells * kOneCell) {
     hipLaunchKernelGGL(msa_verify_one_kernel<T>, dim3(trees), dim3(kWalkThreads), 0, s, v);
@@ -495,9 +513,6 @@ int launch_verify(const VerifyParams& v, int trees, hipStream_t s) {
   if (rc != 0) return rc;
   hipLaunchKernelGGL(msa_verify_sums_kernel<T>, dim3((uint32_t)trees * (uint32_t)v.groups), dim3(kSumsThreads), 0, s,
                      v);
-  rc = (int)hipGetLastError();
-  if (rc != 0) return rc;
-  hipLaunchKernelGGL(msa_verify_pick_kernel<T>, dim3(trees), dim3(kWave), 0, s, v);
   return (int)hipGetLastError();
 }
 
@@ -577,8 +592,9 @@ extern "C" msa_status msa_tree_verify(msa_plan_t plan, int32_t prob_type, int32_
   v.vocab = vocab;
   v.max_slots = hp.max_slots;
   v.cells = (int32_t)msa::cells_of(vocab);
-  // a wave per cell, up to some 8192 workgroups of them
-  v.groups = (int32_t)std::min<int64_t>((v.cells + 3) / 4, std::max<int64_t>(1, 8192 / trees));
+  // a wave per cell, up to some 4096 workgroups of them
+  constexpr int kCellsAtOnce = msa::kSumsThreads / msa::kWave;
+  v.groups = (int32_t)std::min<int64_t>((v.cells + kCellsAtOnce - 1) / kCellsAtOnce, std::max<int64_t>(1, 4096 / trees));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int rc = prob_type == MSA_PROB_F32    ? msa::launch_verify<float>(v, (int)trees, s)
                  : prob_type == MSA_PROB_BF16 ? msa::launch_verify<__hip_bfloat16>(v, (int)trees, s)
