@@ -12,9 +12,11 @@ from typing import Optional, Sequence
 
 try:
     import torch
+    Tensor = torch.Tensor
     INT32, FLOAT32, MASK = (torch.int32,), (torch.float32,), (torch.int64, torch.uint64)
     _PROB = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # MSA_PROB_*
 except ImportError:  # the package itself does without; then nothing here is a tensor
+    Tensor = None
     INT32 = FLOAT32 = MASK = ()
     _PROB = {}
 
@@ -45,20 +47,11 @@ _bind("msa_tree_verify", [_P, _i32, _i32, _P, _i64, _P, _i64, _P, _P, _P, _P, _P
 _bind("msa_tree_verify_workspace", [_P, _i32, ctypes.POINTER(ctypes.c_size_t)])
 
 
-def check_tensor(who: str, name: str, x, dtypes, need: int, rows: Optional[int] = None) -> None:
+def refuse_tensor(who: str, name: str, x, dtypes, need: int, rows: Optional[int] = None) -> None:
     """Refuses a tensor of another type, on the host, not contiguous, or with fewer than ``need`` elements; with
-    ``rows``, a 2-D one (rows, need) whose last dimension is contiguous.  Other objects pass.  (These checks run on
-    every call: the common case is a few attribute reads.)"""
+    ``rows``, a 2-D one (rows, need) whose last dimension is contiguous.  Other objects pass."""
     if x is None or type(x) is int or not hasattr(x, "stride"):
         return
-    if x.dtype in dtypes and x.is_cuda:
-        if rows is None:
-            if x.numel() >= need and x.is_contiguous():
-                return
-        elif x.dim() == 2:
-            have = x.shape
-            if have[0] >= rows and have[1] >= need and (need <= 1 or rows == 0 or x.stride(1) == 1):
-                return
     if x.dtype not in dtypes:
         bad = f"has type {x.dtype}, not {' or '.join(str(d) for d in dtypes)}"
     elif not x.is_cuda:
@@ -66,12 +59,35 @@ def check_tensor(who: str, name: str, x, dtypes, need: int, rows: Optional[int] 
     elif rows is not None and (x.dim() != 2 or x.shape[0] < rows or x.shape[1] < need):
         bad = f"has shape {tuple(x.shape)}, ({rows}, {need}) is needed"
     elif rows is not None:
+        if need <= 1 or rows == 0 or x.stride(1) == 1:
+            return
         bad = "is not contiguous along its last dimension"
     elif x.numel() < need:
         bad = f"has {x.numel()} elements, {need} are needed"
     else:
+        if x.is_contiguous():
+            return
         bad = "is not contiguous"
     raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {name} {bad}")
+
+
+def address(who: str, name: str, x, dtypes, need: int) -> Optional[int]:
+    """Address of a tensor, checked as in ``refuse_tensor``, or of another object.  (These checks run on every call,
+    which may be as short as a launch: the common case is a few attribute reads.)"""
+    if type(x) is Tensor and x.dtype in dtypes and x.is_cuda and x.numel() >= need and x.is_contiguous():
+        return x.data_ptr()
+    refuse_tensor(who, name, x, dtypes, need)
+    return _addr(x)
+
+
+def rows_address(who: str, name: str, x, dtypes, need: int, rows: int, given: Optional[int] = None):
+    """(address, elements from row to row) of a 2-D tensor, checked likewise; ``given``: the latter, where it is."""
+    if type(x) is Tensor and x.dtype in dtypes and x.is_cuda and x.dim() == 2:
+        have, step = x.shape, x.stride()
+        if have[0] >= rows and have[1] >= need and (step[1] == 1 or need <= 1 or rows == 0):
+            return x.data_ptr(), (int(given) if given is not None else step[0] if have[0] > 1 else max(have[1], need))
+    refuse_tensor(who, name, x, dtypes, need, rows)
+    return _addr(x), _row_stride(x, given, need)
 
 
 def size_of(workspace, given: int = 0) -> int:
@@ -126,10 +142,9 @@ def msa_tree_mask(plan: Plan, parents, mask, mask_stride: Optional[int] = None, 
     """Enqueue the trees' ancestor masks: ``parents`` int32 [tree_rows] to ``mask`` int64 or uint64
     [tree_rows, >= mask_words]."""
     _, rows, _, words = _figures(plan)
-    check_tensor("msa_tree_mask", "parents", parents, INT32, rows)
-    check_tensor("msa_tree_mask", "mask", mask, MASK, words, rows)
-    _check(_lib.msa_tree_mask(plan.handle, _addr(parents), _addr(mask), _row_stride(mask, mask_stride, words),
-                              _stream(stream)))
+    up = address("msa_tree_mask", "parents", parents, INT32, rows)
+    at, step = rows_address("msa_tree_mask", "mask", mask, MASK, words, rows, mask_stride)
+    _check(_lib.msa_tree_mask(plan.handle, up, at, step, _stream(stream)))
 
 
 def msa_tree_forward(plan: Plan, q, k_cache, v_cache, block_table, mask, o, lse=None, workspace=None,
@@ -137,10 +152,10 @@ def msa_tree_forward(plan: Plan, q, k_cache, v_cache, block_table, mask, o, lse=
     """Enqueue the attention of a plan with trees for one layer; ``mask`` as of ``msa_tree_mask`` (None if the plan
     has no tree), the rest as of ``msa_forward``."""
     _, rows, _, words = _figures(plan)
-    check_tensor("msa_tree_forward", "mask", mask, MASK, words, rows)
-    _check(_lib.msa_tree_forward(plan.handle, _addr(q), _addr(k_cache), _addr(v_cache), _addr(block_table),
-                                 _addr(mask), _row_stride(mask, mask_stride, words), _addr(o), _addr(lse),
-                                 _addr(workspace), size_of(workspace, workspace_bytes), _stream(stream)))
+    at, step = rows_address("msa_tree_forward", "mask", mask, MASK, words, rows, mask_stride)
+    _check(_lib.msa_tree_forward(plan.handle, _addr(q), _addr(k_cache), _addr(v_cache), _addr(block_table), at, step,
+                                 _addr(o), _addr(lse), _addr(workspace), size_of(workspace, workspace_bytes),
+                                 _stream(stream)))
 
 
 def msa_tree_verify_workspace(plan: Plan, vocab: int) -> int:
@@ -160,18 +175,14 @@ def msa_tree_verify(plan: Plan, target, tokens, parents, u_accept, u_sample, pat
     if target is None or target.dim() != 2:
         raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: target is not a 2-D tensor")
     vocab, kind = target.shape[1], target.dtype
-    check_tensor(who, "target", target, _PROB, vocab, rows)
-    if draft is not None:
-        check_tensor(who, "draft", draft, (kind,), vocab, rows)
-    check_tensor(who, "tokens", tokens, INT32, rows)
-    check_tensor(who, "parents", parents, INT32, rows)
-    check_tensor(who, "u_accept", u_accept, FLOAT32, rows)
-    check_tensor(who, "u_sample", u_sample, FLOAT32, trees)
-    check_tensor(who, "path", path, INT32, slots, trees)
-    check_tensor(who, "path_len", path_len, INT32, trees)
-    check_tensor(who, "next_token", next_token, INT32, trees)
-    _check(_lib.msa_tree_verify(plan.handle, _PROB[kind], vocab, _addr(target), _row_stride(target, None, vocab),
-                                _addr(draft), 0 if draft is None else _row_stride(draft, None, vocab), _addr(tokens),
-                                _addr(parents), _addr(u_accept), _addr(u_sample), _addr(path),
-                                _row_stride(path, None, slots), _addr(path_len), _addr(next_token), _addr(workspace),
+    p, p_step = rows_address(who, "target", target, _PROB, vocab, rows)
+    q, q_step = (None, 0) if draft is None else rows_address(who, "draft", draft, (kind,), vocab, rows)
+    at, step = rows_address(who, "path", path, INT32, slots, trees)
+    _check(_lib.msa_tree_verify(plan.handle, _PROB[kind], vocab, p, p_step, q, q_step,
+                                address(who, "tokens", tokens, INT32, rows),
+                                address(who, "parents", parents, INT32, rows),
+                                address(who, "u_accept", u_accept, FLOAT32, rows),
+                                address(who, "u_sample", u_sample, FLOAT32, trees), at, step,
+                                address(who, "path_len", path_len, INT32, trees),
+                                address(who, "next_token", next_token, INT32, trees), _addr(workspace),
                                 size_of(workspace), _stream(stream)))
