@@ -32,7 +32,8 @@
 //   each over 32 cache lines.  The plan deals out the tiles (see plan_weights); where
 //   keys have several items, their sums go through the workspace and are added in
 //   order.  Prompts of 4099 and less, three of them, 32 heads: 94 us with the join;
-//   one of 16384 1.09 ms, 1007 TFLOP/s.  Bound by vector instructions and MFMAs: a tile of 32 pairs x 64 keys
+//   one of 16384 1.06-1.11 ms, 990-1040 TFLOP/s.  Bound by vector instructions and
+//   MFMAs: a tile of 32 pairs x 64 keys
 //   takes a wave 17 MFMAs of 32 cycles and about 150 vector instructions, 32 of them
 //   exponentials of 8 cycles, beside them.
 // Sums are in fp32, 16 rows of a tile added pairwise and then to the running sum;
