@@ -191,10 +191,13 @@ def test_a_vocabulary_in_few_and_in_many_chunks():
     Drafts(trees_of(5, [2] * 600, "chain"), 5003, "drawn", noise=2.0).check()
     d = Drafts(trees_of(6, [1] * 1500, "chain"), 3001, "drawn")
     d.check()
+    Drafts(trees_of(6, [1] * 700, "chain"), 33003, "best").check()  # workgroups that take several cells each
 
 
-def test_graph_replays():
-    Drafts(trees_of(7, [8] * 6, "tree"), 2500, "drawn").check(graph=True)
+@pytest.mark.parametrize("vocab", [2500, 40000])
+@pytest.mark.parametrize("kind", ["drawn", "best"])
+def test_graph_replays(vocab, kind):
+    Drafts(trees_of(7, [8] * 6, "tree"), vocab, kind).check(graph=True)
 
 
 def test_ends_of_the_random_numbers():
@@ -206,11 +209,12 @@ def test_ends_of_the_random_numbers():
     d.check()
 
 
-def test_odd_probabilities_and_tokens():
+@pytest.mark.parametrize("vocab", [203, 40203])
+def test_odd_probabilities_and_tokens(vocab):
     """Zeros, negatives, NaN and infinities count as 0; a token outside the vocabulary never stays; equal rows always
     accept, and a residual without mass falls back to the row."""
     for kind in ("drawn", "best"):
-        d = Drafts(trees_of(9, [7] * 9, "star"), 203, kind)
+        d = Drafts(trees_of(9, [7] * 9, "star"), vocab, kind)
         n = 7
         d.target[0, ::2] = 0.0                         # a row with zeros
         d.target[n, ::3] = float("nan")
@@ -219,7 +223,7 @@ def test_odd_probabilities_and_tokens():
         d.target[3 * n:4 * n] = 0.0                    # nothing at all: -1
         d.target[4 * n, :] = 0.0
         d.target[4 * n, 17] = 1.0                      # one token
-        d.tokens[5 * n + 1] = 203
+        d.tokens[5 * n + 1] = vocab
         d.tokens[5 * n + 2] = -1
         d.tokens[5 * n + 3] = 1 << 30
         d.tokens[6 * n + 1:7 * n] = d.tokens[6 * n + 1]  # one token six times
