@@ -384,6 +384,18 @@ def test_compact_with_any_block_anywhere():
         check_compact(lens, [0, 3], [len(idx)] * 2, [[idx, idx]] * 2, shared=True, swap=table_order)
 
 
+@pytest.mark.parametrize("part", [0.02, 0.1, 0.3, 0.6, 0.9, 0.99])
+@pytest.mark.parametrize("first", [0, 4, 70])
+def test_compact_parts_of_a_list(part, first):
+    """Few and many kept tokens a block, runs whose places all move and runs where some stay where they are."""
+    r = random.Random(int(part * 100) + first)
+    lens, base = [3001, 40, 6000, 130], [0, 5, 16, 39]
+    counts = [max(1, int(n * part)) for n in lens]
+    lists = [[(sorted(set(range(min(first, n))) | set(r.sample(range(n), k)))[:k]) for _ in range(2)]
+             for n, k in zip(lens, counts)]
+    check_compact([n + b for n, b in zip(lens, base)], base, counts, lists, seed=first + 2)
+
+
 def test_compact_skips_what_lies_outside():
     """Blocks outside the cache, positions past the table, counts past the list."""
     idx = list(range(3, 80, 2))
