@@ -128,7 +128,6 @@ EXPORTED = ("msa_plan", "msa_plan_info", "msa_forward", "msa_kv_append", "msa_pl
             "msa_evictor_size", "msa_evictor_log_weight", "msa_evictor_replay")
 
 
-
 def _bind(name, argtypes) -> None:
     """Argument types of an entry point of msa_tree.h or msa_cache.h.  A build
     of the host code alone (the host-sanitizer test's) lacks most of them."""
