@@ -461,7 +461,8 @@ extern "C" msa_status msa_kv_compact(const msa_shape* shape, const int32_t* base
   const msa_shape& s = *shape;
   if (max_count < 0 || index_stride_seq < 0 || index_stride_head < 0)
     return msa::fail(MSA_ERR_INVALID_ARG, "max_count and the index strides must be >= 0");
-  if (s.num_seqs == 0 || max_count == 0 || s.num_blocks == 0) return MSA_OK;
+  // (a table without entries has no position to move: the kernels read an entry for every list)
+  if (s.num_seqs == 0 || max_count == 0 || s.num_blocks == 0 || s.max_blocks_per_seq == 0) return MSA_OK;
   if (!index || !count || !block_table || !k_cache || !v_cache)
     return msa::fail(MSA_ERR_INVALID_ARG, "index, count, block_table, k_cache, v_cache must be non-null");
   if (!msa::aligned(k_cache, 16) || !msa::aligned(v_cache, 16) || !msa::aligned(base, 4) || !msa::aligned(index, 4) ||
