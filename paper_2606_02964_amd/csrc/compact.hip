@@ -342,11 +342,11 @@ __global__ __launch_bounds__(kCompactThreads + kRun, 5) void msa_kv_compact_kern
   const bool is_v = part >= kParts / 2;
   const int slice = is_v ? part - kParts / 2 : part;
   Moves mv;
-  // (entries past the table's positions are no moves: index[i] >= i)
+  // (entries from end - base on have no destination in the table; base may be negative, then the first ones have none)
   mv.end = (int64_t)p.max_blocks * kBlockSize;
-  mv.n = (int)max((int64_t)0, min(min((int64_t)p.count[seq], (int64_t)p.max_count), min(mv.end, (int64_t)0x7ffff000)));
-  if (mv.n == 0) return;
   mv.base = p.base ? p.base[seq] : 0;
+  mv.n = (int)max((int64_t)0, min((int64_t)min(p.count[seq], p.max_count), min(mv.end - mv.base, (int64_t)0x7ffff000)));
+  if (mv.n == 0) return;
   mv.index = p.index + (int64_t)seq * p.i_sb + (int64_t)head * p.i_sh;
   mv.table = p.block_table + (int64_t)seq * p.max_blocks;
   mv.num_blocks = p.num_blocks;
