@@ -1,23 +1,18 @@
 """Binding of ``include/msa_cache.h``: the attention weight each cached key has
 received, the positions a reduced cache keeps, and their compaction.
 
-The functions carry the C names and are re-exported by the package.  Tensor
-arguments are checked for type, device and size; integer addresses are passed as
-they are.
+The functions carry the C names and are re-exported by the package.  Tensors
+are checked as in ``tree.py``: type, device, and size and layout, except where a
+shape's strides give those (q and the caches).  Integer addresses are passed as
+they are, where a function does not ask for a tensor.
 """
 from __future__ import annotations
 
 import ctypes
 
-try:
-    import torch
-    # torch's own lookup takes 0.15 us, the public call 0.26
-    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-except ImportError:  # the package itself does without
-    torch = None
-
-from . import MSA_ERR_INVALID_ARG, MsaError, Plan, _addr, _bind, _check, _i32, _i64, _lib, _P, _stream, msa_shape
-from .tree import FLOAT32, INT32, address, rows_address, size_of
+from . import MSA_ERR_INVALID_ARG, MsaError, Plan, _bind, _check, _i32, _i64, _lib, _P, _stream, msa_shape
+from .tree import (FLOAT32, INT32, address, refuse_tensor, rows_address, sizes_of, this_device, values_address,
+                   workspace_of)
 
 __all__ = ["msa_kv_weights", "msa_kv_weights_workspace", "msa_kv_select", "msa_kv_compact"]
 
@@ -33,23 +28,18 @@ def _refuse(who: str, what: str) -> None:
     raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {what}")
 
 
-def _lists(who: str, name: str, x, dtypes, a: int, b: int, c: int):
+def _lists(who: str, name: str, x, dtypes, a: int, b: int, c: int, dev: int):
     """(address, strides) of a tensor [sequences, lists, entries] of at least (a, b, c), its entries contiguous."""
+    if not hasattr(x, "stride") or len(x.shape) != 3:
+        _refuse(who, f"{name} is not a tensor [sequences, lists, entries]")
     have, step = x.shape, x.stride()
-    if x.dtype in dtypes and x.is_cuda and len(have) == 3 and have[0] >= a and have[1] >= b and have[2] >= c \
-            and (step[2] == 1 or have[2] <= 1):
-        return x.data_ptr(), step
-    if x.dtype not in dtypes or not x.is_cuda:
-        _refuse(who, f"{name} is not a {dtypes[0]} tensor on a GPU")
-    if len(have) != 3 or have[0] < a or have[1] < b or have[2] < c:
+    if x.dtype not in dtypes or x.get_device() != dev:
+        refuse_tensor(who, name, x, dtypes, None, dev)
+    if have[0] < a or have[1] < b or have[2] < c:
         _refuse(who, f"{name} has shape {tuple(have)}, {(a, b, c)} is needed")
-    _refuse(who, f"{name} is not contiguous along its last dimension")
-
-
-def _here(who: str, x) -> None:
-    """Calls without a plan know no device of their own: their tensors are on the current one."""
-    if x.get_device() != _device():
-        _refuse(who, f"tensors are on device {x.get_device()}, the current device is {_device()}")
+    if step[2] != 1 and have[2] > 1:
+        _refuse(who, f"{name} is not contiguous along its last dimension")
+    return x.data_ptr(), step
 
 
 def msa_kv_weights_workspace(plan: Plan) -> int:
@@ -60,48 +50,55 @@ def msa_kv_weights_workspace(plan: Plan) -> int:
 
 
 def msa_kv_weights(plan: Plan, q, k_cache, block_table, lse, weights, workspace=None, accumulate: bool = True,
-                   stream=None) -> None:
-    """Enqueue the sum of the plan's softmax weights by key into ``weights`` float32 [sequences, KV heads, positions];
-    ``accumulate`` adds to what is there."""
-    who, sh = "msa_kv_weights", plan.shape
+                   stream=None, workspace_bytes: int = 0) -> None:
+    """Enqueue the sum of the plan's softmax weights by key into the tensor ``weights`` float32 [sequences, KV heads,
+    positions]; ``accumulate`` adds to what is there.  ``lse`` float32 [total_q, query heads] is that of msa_forward."""
+    who, sh, dev = "msa_kv_weights", plan.shape, this_device()
     need = getattr(plan, "positions", None)
     if need is None:  # the most positions a sequence may have
         need = plan.positions = sh.max_blocks_per_seq * sh.block_size
         plan.heads = (sh.num_seqs, sh.num_kv_heads)
-    at, step = _lists(who, "weights", weights, FLOAT32, *plan.heads, need)
-    _check(_lib.msa_kv_weights(plan.handle, _addr(q), _addr(k_cache), _addr(block_table), _addr(lse), at, step[0],
-                               step[1], int(accumulate), _addr(workspace), size_of(workspace), _stream(stream)))
+    entries, lses = sizes_of(plan)
+    at, step = _lists(who, "weights", weights, FLOAT32, *plan.heads, need, dev)
+    ws, ws_bytes = workspace_of(who, workspace, workspace_bytes, dev)
+    _check(_lib.msa_kv_weights(plan.handle, values_address(who, "q", q, dev),
+                               values_address(who, "k_cache", k_cache, dev),
+                               address(who, "block_table", block_table, INT32, entries, dev),
+                               address(who, "lse", lse, FLOAT32, lses, dev), at, step[0], step[1], int(accumulate),
+                               ws, ws_bytes, _stream(stream)))
 
 
 def msa_kv_select(scores, seq_len, keep, index, count, first: int = 0, recent: int = 0, stream=None) -> None:
-    """Enqueue the choice of the positions that stay: ``scores`` float32 [sequences, lists, positions], ``seq_len`` and
-    ``keep`` int32 [sequences]; ``index`` int32 [sequences, lists, entries] and ``count`` int32 [sequences] are
-    written."""
-    who = "msa_kv_select"
+    """Enqueue the choice of the positions that stay: tensors ``scores`` float32 [sequences, lists, positions] and
+    ``index`` int32 [sequences, lists, entries]; ``seq_len`` and ``keep`` int32 [sequences].  ``index`` and ``count``
+    int32 [sequences] are written."""
+    who, dev = "msa_kv_select", this_device()
     if len(getattr(scores, "shape", ())) != 3:
         _refuse(who, "scores is not a tensor [sequences, lists, positions]")
     B, H, L = scores.shape
-    at, step = _lists(who, "scores", scores, FLOAT32, B, H, 0)
-    to, to_step = _lists(who, "index", index, INT32, B, H, 0)
-    _here(who, scores)
-    _check(_lib.msa_kv_select(B, H, at, step[0], step[1], L, address(who, "seq_len", seq_len, INT32, B),
-                              address(who, "keep", keep, INT32, B), int(first), int(recent), index.shape[2], to,
-                              to_step[0], to_step[1], address(who, "count", count, INT32, B), _stream(stream)))
+    at, step = _lists(who, "scores", scores, FLOAT32, B, H, 0, dev)
+    to, to_step = _lists(who, "index", index, INT32, B, H, 0, dev)
+    _check(_lib.msa_kv_select(B, H, at, step[0], step[1], L, address(who, "seq_len", seq_len, INT32, B, dev),
+                              address(who, "keep", keep, INT32, B, dev), int(first), int(recent), index.shape[2], to,
+                              to_step[0], to_step[1], address(who, "count", count, INT32, B, dev), _stream(stream)))
 
 
 def msa_kv_compact(shape: msa_shape, base, index, count, block_table, k_cache, v_cache, stream=None) -> None:
     """Enqueue the moves of K and V at ``base[b] + index[b, (head,) i]`` to ``base[b] + i``, i < ``count[b]``.
-    ``index`` int32 [sequences, entries], the same for all heads, or [sequences, KV heads, entries]; ``base`` (or None:
-    0) and ``count`` int32 [sequences]."""
-    who, B = "msa_kv_compact", shape.num_seqs
+    ``index`` is an int32 tensor [sequences, entries], the same for all heads, or [sequences, KV heads, entries];
+    ``base`` (or None: 0) and ``count`` int32 [sequences], ``block_table`` int32 [sequences, max_blocks_per_seq]."""
+    who, B, dev = "msa_kv_compact", shape.num_seqs, this_device()
+    if not hasattr(index, "stride"):
+        _refuse(who, "index is not a tensor")
     if index.dim() == 2:
         entries = index.shape[1]
-        at, _ = rows_address(who, "index", index, INT32, entries, B)
-        per_seq, per_head = index.stride(0), 0
+        at, per_seq = rows_address(who, "index", index, INT32, entries, B, dev)
+        per_head = 0
     else:
-        at, (per_seq, per_head, _) = _lists(who, "index", index, INT32, B, shape.num_kv_heads, 0)
+        at, (per_seq, per_head, _) = _lists(who, "index", index, INT32, B, shape.num_kv_heads, 0, dev)
         entries = index.shape[2]
-    _here(who, index)
-    _check(_lib.msa_kv_compact(ctypes.byref(shape), address(who, "base", base, INT32, B), at, per_seq, per_head, entries,
-                               address(who, "count", count, INT32, B), _addr(block_table), _addr(k_cache),
-                               _addr(v_cache), _stream(stream)))
+    _check(_lib.msa_kv_compact(ctypes.byref(shape), address(who, "base", base, INT32, B, dev), at, per_seq, per_head,
+                               entries, address(who, "count", count, INT32, B, dev),
+                               address(who, "block_table", block_table, INT32, B * shape.max_blocks_per_seq, dev),
+                               values_address(who, "k_cache", k_cache, dev),
+                               values_address(who, "v_cache", v_cache, dev), _stream(stream)))

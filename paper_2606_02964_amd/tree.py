@@ -1,9 +1,12 @@
 """Binding of ``include/msa_tree.h``: attention of trees of drafted tokens over
 the paged cache, and the verification of the drafts.
 
-The functions carry the C names and are re-exported by the package.  Tensor
-arguments are checked for type, device and size (the library sees addresses
-only); integer addresses are passed as they are.
+The functions carry the C names and are re-exported by the package.  The library
+sees addresses only, so tensors are checked here, and refused with MsaError: their
+type, that they are on the current device (the library compares it with the
+plan's), and their size and layout, except where a shape's strides give those: of
+q, o and the caches.  Integer addresses are passed as they are, where a function
+does not ask for a tensor.
 """
 from __future__ import annotations
 
@@ -14,14 +17,17 @@ try:
     import torch
     Tensor = torch.Tensor
     INT32, FLOAT32, MASK = (torch.int32,), (torch.float32,), (torch.int64, torch.uint64)
+    BF16 = (torch.bfloat16, torch.int16, torch.uint16)  # or its bits
+    # torch's own lookup takes 0.15 us, the public call 0.26
+    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _PROB = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # MSA_PROB_*
 except ImportError:  # the package itself does without; then nothing here is a tensor
     Tensor = None
-    INT32 = FLOAT32 = MASK = ()
+    INT32 = FLOAT32 = MASK = BF16 = ()
     _PROB = {}
 
 from . import (MSA_ERR_INVALID_ARG, MSA_PLAN_HOST_ONLY, MsaError, Plan, _addr, _bind, _check, _host_i32, _i32, _i64,
-               _lib, _P, _stream, msa_plan_opts, msa_shape)
+               _lib, _P, _stream, msa_plan_info, msa_plan_opts, msa_shape)
 
 __all__ = ["MSA_TREE_MAX_SLOTS", "MSA_PROB_F32", "MSA_PROB_BF16", "MSA_PROB_F16", "msa_tree_info_t", "msa_plan_tree",
            "msa_plan_tree_info", "msa_tree_mask", "msa_tree_forward", "msa_tree_verify", "msa_tree_verify_workspace"]
@@ -47,15 +53,28 @@ _bind("msa_tree_verify", [_P, _i32, _i32, _P, _i64, _P, _i64, _P, _P, _P, _P, _P
 _bind("msa_tree_verify_workspace", [_P, _i32, ctypes.POINTER(ctypes.c_size_t)])
 
 
-def refuse_tensor(who: str, name: str, x, dtypes, need: int, rows: Optional[int] = None) -> None:
-    """Refuses a tensor of another type, on the host, not contiguous, or with fewer than ``need`` elements; with
-    ``rows``, a 2-D one (rows, need) whose last dimension is contiguous.  Other objects pass."""
+def this_device() -> int:
+    """The current device, -1 (a host tensor's) or an exception's -2 where there is none."""
+    try:
+        return _device()
+    except (NameError, RuntimeError):
+        return -2
+
+
+def refuse_tensor(who: str, name: str, x, dtypes, need: Optional[int], dev: int, rows: Optional[int] = None) -> None:
+    """Refuses a tensor of another type, not on device ``dev``, not contiguous, or with fewer than ``need`` elements
+    (None: any number, with any strides); with ``rows``, a 2-D one (rows, need) whose last dimension is contiguous.
+    Other objects pass."""
     if x is None or type(x) is int or not hasattr(x, "stride"):
         return
     if x.dtype not in dtypes:
         bad = f"has type {x.dtype}, not {' or '.join(str(d) for d in dtypes)}"
     elif not x.is_cuda:
         bad = "is not on a GPU"
+    elif x.get_device() != dev:
+        bad = f"is on device {x.get_device()}, the current device is {dev}"
+    elif need is None:
+        return
     elif rows is not None and (x.dim() != 2 or x.shape[0] < rows or x.shape[1] < need):
         bad = f"has shape {tuple(x.shape)}, ({rows}, {need}) is needed"
     elif rows is not None:
@@ -71,35 +90,60 @@ def refuse_tensor(who: str, name: str, x, dtypes, need: int, rows: Optional[int]
     raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {name} {bad}")
 
 
-def address(who: str, name: str, x, dtypes, need: int) -> Optional[int]:
+def address(who: str, name: str, x, dtypes, need: int, dev: int) -> Optional[int]:
     """Address of a tensor, checked as in ``refuse_tensor``, or of another object.  (These checks run on every call,
     which may be as short as a launch: the common case is a few attribute reads.)"""
-    if type(x) is Tensor and x.dtype in dtypes and x.is_cuda and x.numel() >= need and x.is_contiguous():
+    if type(x) is Tensor and x.dtype in dtypes and x.get_device() == dev and x.numel() >= need and x.is_contiguous():
         return x.data_ptr()
-    refuse_tensor(who, name, x, dtypes, need)
+    refuse_tensor(who, name, x, dtypes, need, dev)
     return _addr(x)
 
 
-def rows_address(who: str, name: str, x, dtypes, need: int, rows: int, given: Optional[int] = None):
+def values_address(who: str, name: str, x, dev: int) -> Optional[int]:
+    """Address of bfloat16 values that a shape's strides lay out; type and device are checked."""
+    if type(x) is Tensor and x.dtype in BF16 and x.get_device() == dev:
+        return x.data_ptr()
+    refuse_tensor(who, name, x, BF16, None, dev)
+    return _addr(x)
+
+
+def rows_address(who: str, name: str, x, dtypes, need: int, rows: int, dev: int, given: Optional[int] = None):
     """(address, elements from row to row) of a 2-D tensor, checked likewise; ``given``: the latter, where it is."""
-    if type(x) is Tensor and x.dtype in dtypes and x.is_cuda and x.dim() == 2:
+    if type(x) is Tensor and x.dtype in dtypes and x.get_device() == dev and x.dim() == 2:
         have, step = x.shape, x.stride()
-        if have[0] >= rows and have[1] >= need and (step[1] == 1 or need <= 1 or rows == 0):
-            return x.data_ptr(), (int(given) if given is not None else step[0] if have[0] > 1 else max(have[1], need))
-    refuse_tensor(who, name, x, dtypes, need, rows)
-    return _addr(x), _row_stride(x, given, need)
+        if have[0] >= rows and have[1] >= need and (step[1] == 1 or need <= 1 or rows == 0) and given is None:
+            return x.data_ptr(), (step[0] if have[0] > 1 else max(have[1], need))
+    refuse_tensor(who, name, x, dtypes, need, dev, rows)
+    step = _row_stride(x, need)
+    if given is not None and rows > 1 and hasattr(x, "stride") and int(given) != step:
+        raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {name} has {step} elements from row to row, not {int(given)}")
+    return _addr(x), step if given is None else int(given)
 
 
-def size_of(workspace, given: int = 0) -> int:
-    """Bytes of a workspace tensor, or as given."""
-    if workspace is None or given:
-        return int(given)
-    return workspace.numel() * workspace.element_size()
+def workspace_of(who: str, workspace, given: int, dev: int):
+    """(address, bytes) of a workspace: a tensor, whose bytes are taken from it unless given, or an address."""
+    if workspace is None:
+        return None, int(given)
+    if not hasattr(workspace, "stride"):
+        if not given:
+            raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: workspace_bytes is needed with a workspace's address")
+        return _addr(workspace), int(given)
+    have = workspace.numel() * workspace.element_size()
+    if workspace.get_device() != dev or not workspace.is_contiguous() or have < given:
+        refuse_tensor(who, "workspace", workspace, (workspace.dtype,), -(-int(given) // workspace.element_size()), dev)
+    return workspace.data_ptr(), int(given) or have
 
 
-def _row_stride(x, given: Optional[int], width: int) -> int:
-    if given is not None:
-        return int(given)
+def sizes_of(plan: Plan):
+    """(entries of the plan's block table, of its lse)."""
+    sizes = getattr(plan, "sizes", None)
+    if sizes is None:
+        sh = plan.shape
+        sizes = plan.sizes = (sh.num_seqs * sh.max_blocks_per_seq, msa_plan_info(plan)["total_q"] * sh.num_q_heads)
+    return sizes
+
+
+def _row_stride(x, width: int) -> int:
     if hasattr(x, "stride") and x.dim() == 2:
         return x.stride(0) if x.shape[0] > 1 else max(x.shape[1], width)
     return width
@@ -142,20 +186,28 @@ def msa_tree_mask(plan: Plan, parents, mask, mask_stride: Optional[int] = None, 
     """Enqueue the trees' ancestor masks: ``parents`` int32 [tree_rows] to ``mask`` int64 or uint64
     [tree_rows, >= mask_words]."""
     _, rows, _, words = _figures(plan)
-    up = address("msa_tree_mask", "parents", parents, INT32, rows)
-    at, step = rows_address("msa_tree_mask", "mask", mask, MASK, words, rows, mask_stride)
+    dev = this_device()
+    up = address("msa_tree_mask", "parents", parents, INT32, rows, dev)
+    at, step = rows_address("msa_tree_mask", "mask", mask, MASK, words, rows, dev, mask_stride)
     _check(_lib.msa_tree_mask(plan.handle, up, at, step, _stream(stream)))
 
 
 def msa_tree_forward(plan: Plan, q, k_cache, v_cache, block_table, mask, o, lse=None, workspace=None,
                      workspace_bytes: int = 0, mask_stride: Optional[int] = None, stream=None) -> None:
     """Enqueue the attention of a plan with trees for one layer; ``mask`` as of ``msa_tree_mask`` (None if the plan
-    has no tree), the rest as of ``msa_forward``."""
+    has no tree), ``block_table`` int32 [sequences, max_blocks_per_seq], ``lse`` float32 [total_q, query heads], the rest
+    as of ``msa_forward``."""
+    who, dev = "msa_tree_forward", this_device()
+    entries, lses = sizes_of(plan)
     _, rows, _, words = _figures(plan)
-    at, step = rows_address("msa_tree_forward", "mask", mask, MASK, words, rows, mask_stride)
-    _check(_lib.msa_tree_forward(plan.handle, _addr(q), _addr(k_cache), _addr(v_cache), _addr(block_table), at, step,
-                                 _addr(o), _addr(lse), _addr(workspace), size_of(workspace, workspace_bytes),
-                                 _stream(stream)))
+    at, step = rows_address(who, "mask", mask, MASK, words, rows, dev, mask_stride)
+    ws, ws_bytes = workspace_of(who, workspace, workspace_bytes, dev)
+    _check(_lib.msa_tree_forward(plan.handle, values_address(who, "q", q, dev),
+                                 values_address(who, "k_cache", k_cache, dev),
+                                 values_address(who, "v_cache", v_cache, dev),
+                                 address(who, "block_table", block_table, INT32, entries, dev), at, step,
+                                 values_address(who, "o", o, dev),
+                                 None if lse is None else address(who, "lse", lse, FLOAT32, lses, dev), ws, ws_bytes, _stream(stream)))
 
 
 def msa_tree_verify_workspace(plan: Plan, vocab: int) -> int:
@@ -166,23 +218,24 @@ def msa_tree_verify_workspace(plan: Plan, vocab: int) -> int:
 
 
 def msa_tree_verify(plan: Plan, target, tokens, parents, u_accept, u_sample, path, path_len, next_token, draft=None,
-                    workspace=None, stream=None) -> None:
+                    workspace=None, stream=None, workspace_bytes: int = 0) -> None:
     """Enqueue the verification of the plan's trees.  ``target`` (and ``draft``, or None) are tensors
     [tree_rows, vocab] of float32, bfloat16 or float16; ``path`` int32 [trees, >= max_slots], ``path_len`` and
     ``next_token`` int32 [trees] are written."""
-    who = "msa_tree_verify"
+    who, dev = "msa_tree_verify", this_device()
     trees, rows, slots, _ = _figures(plan)
-    if target is None or target.dim() != 2:
+    if not hasattr(target, "stride") or target.dim() != 2:
         raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: target is not a 2-D tensor")
     vocab, kind = target.shape[1], target.dtype
-    p, p_step = rows_address(who, "target", target, _PROB, vocab, rows)
-    q, q_step = (None, 0) if draft is None else rows_address(who, "draft", draft, (kind,), vocab, rows)
-    at, step = rows_address(who, "path", path, INT32, slots, trees)
+    p, p_step = rows_address(who, "target", target, _PROB, vocab, rows, dev)
+    q, q_step = (None, 0) if draft is None else rows_address(who, "draft", draft, (kind,), vocab, rows, dev)
+    at, step = rows_address(who, "path", path, INT32, slots, trees, dev)
+    ws, ws_bytes = workspace_of(who, workspace, workspace_bytes, dev)
     _check(_lib.msa_tree_verify(plan.handle, _PROB[kind], vocab, p, p_step, q, q_step,
-                                address(who, "tokens", tokens, INT32, rows),
-                                address(who, "parents", parents, INT32, rows),
-                                address(who, "u_accept", u_accept, FLOAT32, rows),
-                                address(who, "u_sample", u_sample, FLOAT32, trees), at, step,
-                                address(who, "path_len", path_len, INT32, trees),
-                                address(who, "next_token", next_token, INT32, trees), _addr(workspace),
-                                size_of(workspace), _stream(stream)))
+                                address(who, "tokens", tokens, INT32, rows, dev),
+                                address(who, "parents", parents, INT32, rows, dev),
+                                address(who, "u_accept", u_accept, FLOAT32, rows, dev),
+                                address(who, "u_sample", u_sample, FLOAT32, trees, dev), at, step,
+                                address(who, "path_len", path_len, INT32, trees, dev),
+                                address(who, "next_token", next_token, INT32, trees, dev), ws, ws_bytes,
+                                _stream(stream)))
