@@ -116,8 +116,9 @@ msa_status msa_kv_select(int32_t num_seqs, int32_t num_lists, const float *score
  *
  * A move whose source or destination lies outside [0, max_blocks_per_seq * 16)
  * or in a block outside [0, num_blocks) is skipped.  Where a list is not strictly
- * ascending, the values moved are unspecified.  Sequences must not share the
- * blocks that are written, nor one sequence write a block that another reads.
+ * ascending, the values moved are unspecified.  No list may write a place (a
+ * token of a block) that the list of another sequence reads or writes; two lists
+ * may lie side by side in a block.
  * MSA_ERR_INVALID_ARG, MSA_ERR_UNSUPPORTED as for msa_plan's shape; NULL or
  * misaligned pointers, negative max_count or strides: MSA_ERR_INVALID_ARG;
  * MSA_ERR_UNSUPPORTED also for 2^20 (sequence, KV head) pairs or more.

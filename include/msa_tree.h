@@ -155,8 +155,13 @@ msa_status msa_tree_forward(msa_plan_t plan, const void *q, const void *k_cache,
  *   workspace      device buffer of at least msa_tree_verify_workspace bytes,
  *                  16-byte aligned; needs no initialisation, is clobbered
  *
- * path and path_len are the lists that msa_kv_compact (msa_cache.h) takes to
- * move the kept slots' K/V to the front of the tree.  Nothing is synchronised.
+ * path and path_len are lists for msa_kv_compact (msa_cache.h), which moves the
+ * kept slots' K/V to the front of the tree, with base = the tree's first
+ * position.  They are numbered by tree, compaction's lists by the rows of its
+ * block table: where every sequence has exactly one tree, the plan's shape and
+ * table do; else (a sequence without a tree or with several) it takes a table
+ * that has a row for each tree, its sequence's, and a shape with as many
+ * sequences.  Nothing is synchronised.
  * MSA_ERR_INVALID_ARG for NULL or misaligned pointers (to their element size),
  * bad strides, types or sizes, a small workspace, a host-only plan; a plan
  * without trees returns MSA_OK and launches nothing.
