@@ -5,14 +5,18 @@
  *
  * A sequence whose cache is to stay within a budget keeps its first and its
  * latest positions and, of the others, those that received the most attention
- * weight so far.  The three calls go together
+ * weight so far.  The calls go together
  *
  *   msa_kv_weights(plan, ..., lse, weights)       after msa_forward, every step
  *   msa_kv_select(weights, ..., index, count)     when the budget is reached
  *   msa_kv_compact(shape, ..., index, count, ...) moves K/V of the kept positions
  *
- * and the same compaction brings the accepted slots of a verified tree
- * (msa_tree.h) to the front of the tree.  A moved key keeps its values: where
+ *   weights[b, g, i] = weights[b, g, index[b, g, i]], i < count[b]; 0 behind
+ *
+ * (the last by the caller: sums are numbered by place in the cache, so they go
+ * where their keys go, and the places that new keys take start from 0).  The same
+ * compaction brings the accepted slots of a verified tree (msa_tree.h) to the
+ * front of the tree.  A moved key keeps its values: where
  * positions are encoded in K (rotary embeddings), it keeps the position it was
  * written with, while the positions of msa.h are places in the cache.
  * Statuses, layouts and ownership are those of msa.h.
@@ -102,7 +106,8 @@ msa_status msa_kv_select(int32_t num_seqs, int32_t num_lists, const float *score
  *
  *   K and V at position base[b] + i  <-  those at base[b] + index[b, g, i]
  *
- * as they were before the call.  Nothing else in the caches is written.
+ * as they were before the call.  Nothing else in the caches is written.  Sums
+ * of key weights stay where they are: see above.
  *
  *   shape        heads, head_dim, block size, cache strides, max_blocks_per_seq,
  *                num_blocks and num_seqs are used (the rest must be valid)
