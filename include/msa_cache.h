@@ -41,7 +41,7 @@ extern "C" {
  *                exp(scale * <q[r, h], k_j> - lse[r, h])
  *
  *   lse            device float32 [total_q, Hq], as msa_forward writes it (a row
- *                  whose lse is -inf gives no weight, if its q is finite)
+ *                  whose lse is -inf gives no weight, if its q and K are finite)
  *   weights        device float32: w[b, g, j] at weights + b * stride_seq +
  *                  g * stride_head + j, 4-byte aligned; written at positions
  *                  0 .. (largest query position of b) of every sequence with
@@ -57,6 +57,11 @@ extern "C" {
  * for a plan of msa_plan_tree, or with too many rows or keys for a launch (2^31 (row,
  * query head of a group) pairs, or some 2^32 (key, KV head) pairs); otherwise the statuses
  * of msa_forward.
+ *
+ * Trees: which slots' rows are to give weight is known only after the verification.
+ * Behind compaction the kept ones are causal rows at the tree's first positions: a
+ * plan of msa_plan for the same segments adds their weights up, given q and lse of row
+ * path[i] at row i, and an lse of -inf at the rows from path_len on.
  */
 msa_status msa_kv_weights(msa_plan_t plan, const void *q, const void *k_cache,
                           const int32_t *block_table, const float *lse, float *weights,
