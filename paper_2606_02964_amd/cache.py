@@ -11,8 +11,8 @@ from __future__ import annotations
 import ctypes
 
 from . import MSA_ERR_INVALID_ARG, MsaError, Plan, _bind, _check, _i32, _i64, _lib, _P, _stream, msa_shape
-from .tree import (FLOAT32, INT32, address, refuse_tensor, rows_address, sizes_of, this_device, values_address,
-                   workspace_of)
+from .tree import (FLOAT32, INT32, address, refuse_large, refuse_tensor, rows_address, sizes_of, this_device,
+                   values_address, workspace_of)
 
 __all__ = ["msa_kv_weights", "msa_kv_weights_workspace", "msa_kv_select", "msa_kv_compact"]
 
@@ -78,8 +78,11 @@ def msa_kv_select(scores, seq_len, keep, index, count, first: int = 0, recent: i
     B, H, L = scores.shape
     at, step = _lists(who, "scores", scores, FLOAT32, B, H, 0, dev)
     to, to_step = _lists(who, "index", index, INT32, B, H, 0, dev)
+    first, recent, entries = int(first), int(recent), index.shape[2]
+    if (first | recent | B | H | L | entries) >> 31:  # (negative ones too)
+        refuse_large(who, first=first, recent=recent, sequences=B, lists=H, positions=L, entries=entries)
     _check(_lib.msa_kv_select(B, H, at, step[0], step[1], L, address(who, "seq_len", seq_len, INT32, B, dev),
-                              address(who, "keep", keep, INT32, B, dev), int(first), int(recent), index.shape[2], to,
+                              address(who, "keep", keep, INT32, B, dev), first, recent, entries, to,
                               to_step[0], to_step[1], address(who, "count", count, INT32, B, dev), _stream(stream)))
 
 
@@ -97,6 +100,8 @@ def msa_kv_compact(shape: msa_shape, base, index, count, block_table, k_cache, v
     else:
         at, (per_seq, per_head, _) = _lists(who, "index", index, INT32, B, shape.num_kv_heads, 0, dev)
         entries = index.shape[2]
+    if entries >> 31:
+        refuse_large(who, entries=entries)
     _check(_lib.msa_kv_compact(ctypes.byref(shape), address(who, "base", base, INT32, B, dev), at, per_seq, per_head,
                                entries, address(who, "count", count, INT32, B, dev),
                                address(who, "block_table", block_table, INT32, B * shape.max_blocks_per_seq, dev),

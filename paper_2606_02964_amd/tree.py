@@ -134,11 +134,20 @@ def workspace_of(who: str, workspace, given: int, dev: int):
     return workspace.data_ptr(), int(given) or have
 
 
+def refuse_large(who: str, **sizes: int) -> None:
+    """Refuses sizes that the library's 32-bit arguments do not hold (ctypes would cut them off)."""
+    for name, x in sizes.items():
+        if not -1 << 31 <= x < 1 << 31:
+            raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {name} {x} does not fit 32 bits")
+
+
 def sizes_of(plan: Plan):
     """(entries of the plan's block table, of its lse)."""
     sizes = getattr(plan, "sizes", None)
     if sizes is None:
         sh = plan.shape
+        if not plan.handle or sh is None:  # no plan: the library reports that
+            return 0, 0
         sizes = plan.sizes = (sh.num_seqs * sh.max_blocks_per_seq, msa_plan_info(plan)["total_q"] * sh.num_q_heads)
     return sizes
 
@@ -213,6 +222,7 @@ def msa_tree_forward(plan: Plan, q, k_cache, v_cache, block_table, mask, o, lse=
 def msa_tree_verify_workspace(plan: Plan, vocab: int) -> int:
     """Bytes of workspace that ``msa_tree_verify`` needs."""
     out = ctypes.c_size_t()
+    refuse_large("msa_tree_verify_workspace", vocab=int(vocab))
     _check(_lib.msa_tree_verify_workspace(plan.handle, int(vocab), ctypes.byref(out)))
     return out.value
 
@@ -227,6 +237,8 @@ def msa_tree_verify(plan: Plan, target, tokens, parents, u_accept, u_sample, pat
     if not hasattr(target, "stride") or target.dim() != 2:
         raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: target is not a 2-D tensor")
     vocab, kind = target.shape[1], target.dtype
+    if vocab >> 31:
+        refuse_large(who, vocab=vocab)
     p, p_step = rows_address(who, "target", target, _PROB, vocab, rows, dev)
     q, q_step = (None, 0) if draft is None else rows_address(who, "draft", draft, (kind,), vocab, rows, dev)
     at, step = rows_address(who, "path", path, INT32, slots, trees, dev)

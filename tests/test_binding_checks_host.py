@@ -218,3 +218,30 @@ def test_a_row_stride_other_than_the_tensors(device0, trees):
     refused("3 elements from row to row, not 100", msa.msa_tree_mask, plan=trees, parents=OnDevice(120), mask=mask, mask_stride=100)
     refused("HOST_ONLY", msa.msa_tree_mask, plan=trees, parents=OnDevice(120), mask=mask, mask_stride=3)
     refused("HOST_ONLY", msa.msa_tree_mask, plan=trees, parents=OnDevice(120), mask=P, mask_stride=100)
+
+
+@pytest.mark.parametrize("size", [1 << 31, (1 << 32) + 5, 1 << 40])
+def test_sizes_that_do_not_fit_the_librarys_arguments(device0, plan, trees, size):
+    call = calls(plan, trees)
+    refused(f"first {size}", call["select"], **args("select", first=size))
+    refused(f"recent {size}", call["select"], **args("select", recent=size))
+    refused("recent -2147483649", call["select"], **args("select", recent=-(1 << 31) - 1))
+    refused("sizes", call["select"], **args("select", recent=-1))
+    refused(f"positions {size}", call["select"], **args("select", scores=OnDevice(2, 0, size, dtype=F32)))
+    refused(f"entries {size}", call["select"], **args("select", index=OnDevice(2, 0, size)))
+    refused(f"entries {size}", call["compact"], **args("compact", index=OnDevice(2, size)))
+    refused(f"entries {size}", call["compact"], **args("compact", index=OnDevice(2, 2, size)))
+    wide = OnDevice(120, size, dtype=F32)
+    refused(f"vocab {size}", call["verify"], **args("verify", target=wide, draft=wide))
+    refused(f"vocab {size}", msa.msa_tree_verify_workspace, plan=trees, vocab=size)
+
+
+def test_a_closed_plan(device0):
+    for make, call in ((msa.msa_plan, "weights"), (msa.msa_plan_tree, "forward"), (msa.msa_plan_tree, "verify")):
+        p = make(SHAPE, *LAYOUT, flags=msa.MSA_PLAN_HOST_ONLY)
+        p.close()
+        a = {"weights": (P, P, P, P, OnDevice(2, 2, 640, dtype=F32)), "forward": (P, P, P, P, P, P),
+             "verify": (OnDevice(120, 50, dtype=F32), P, P, P, P, P, P, P)}[call]
+        fn = {"weights": msa.msa_kv_weights, "forward": msa.msa_tree_forward, "verify": msa.msa_tree_verify}[call]
+        with pytest.raises(msa.MsaError, match="null plan"):
+            fn(p, *a)
