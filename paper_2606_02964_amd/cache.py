@@ -10,9 +10,9 @@ from __future__ import annotations
 
 import ctypes
 
-from . import MSA_ERR_INVALID_ARG, MsaError, Plan, _bind, _check, _i32, _i64, _lib, _P, _stream, msa_shape
-from .tree import (FLOAT32, INT32, address, refuse_large, refuse_tensor, rows_address, sizes_of, this_device,
-                   values_address, workspace_of)
+from . import MSA_ERR_INVALID_ARG, MsaError, Plan, _bind, _check, _i32, _i64, _lib, _P, msa_shape
+from .tree import (FLOAT32, INT32, address, here, refuse_large, refuse_tensor, rows_address, sizes_of, values_address,
+                   workspace_of)
 
 __all__ = ["msa_kv_weights", "msa_kv_weights_workspace", "msa_kv_select", "msa_kv_compact"]
 
@@ -30,16 +30,19 @@ def _refuse(who: str, what: str) -> None:
 
 def _lists(who: str, name: str, x, dtypes, a: int, b: int, c: int, dev: int):
     """(address, strides) of a tensor [sequences, lists, entries] of at least (a, b, c), its entries contiguous."""
-    if not hasattr(x, "stride") or len(x.shape) != 3:
+    try:
+        have, step = x.shape, x.stride()
+        if x.dtype in dtypes and x.get_device() == dev and have[0] >= a and have[1] >= b and have[2] >= c \
+                and (step[2] == 1 or have[2] <= 1) and len(have) == 3:
+            return x.data_ptr(), step
+    except (AttributeError, IndexError):
         _refuse(who, f"{name} is not a tensor [sequences, lists, entries]")
-    have, step = x.shape, x.stride()
-    if x.dtype not in dtypes or x.get_device() != dev:
-        refuse_tensor(who, name, x, dtypes, None, dev)
+    if len(have) != 3:
+        _refuse(who, f"{name} is not a tensor [sequences, lists, entries]")
+    refuse_tensor(who, name, x, dtypes, None, dev)
     if have[0] < a or have[1] < b or have[2] < c:
         _refuse(who, f"{name} has shape {tuple(have)}, {(a, b, c)} is needed")
-    if step[2] != 1 and have[2] > 1:
-        _refuse(who, f"{name} is not contiguous along its last dimension")
-    return x.data_ptr(), step
+    _refuse(who, f"{name} is not contiguous along its last dimension")
 
 
 def msa_kv_weights_workspace(plan: Plan) -> int:
@@ -53,26 +56,24 @@ def msa_kv_weights(plan: Plan, q, k_cache, block_table, lse, weights, workspace=
                    stream=None, workspace_bytes: int = 0) -> None:
     """Enqueue the sum of the plan's softmax weights by key into the tensor ``weights`` float32 [sequences, KV heads,
     positions]; ``accumulate`` adds to what is there.  ``lse`` float32 [total_q, query heads] is that of msa_forward."""
-    who, sh, dev = "msa_kv_weights", plan.shape, this_device()
-    need = getattr(plan, "positions", None)
-    if need is None:  # the most positions a sequence may have
-        need = plan.positions = sh.max_blocks_per_seq * sh.block_size
-        plan.heads = (sh.num_seqs, sh.num_kv_heads)
-    entries, lses = sizes_of(plan)
-    at, step = _lists(who, "weights", weights, FLOAT32, *plan.heads, need, dev)
+    who = "msa_kv_weights"
+    dev, stream = here(stream)
+    entries, lses, seqs, heads, positions = sizes_of(plan)
+    at, step = _lists(who, "weights", weights, FLOAT32, seqs, heads, positions, dev)
     ws, ws_bytes = workspace_of(who, workspace, workspace_bytes, dev)
     _check(_lib.msa_kv_weights(plan.handle, values_address(who, "q", q, dev),
                                values_address(who, "k_cache", k_cache, dev),
                                address(who, "block_table", block_table, INT32, entries, dev),
                                address(who, "lse", lse, FLOAT32, lses, dev), at, step[0], step[1], int(accumulate),
-                               ws, ws_bytes, _stream(stream)))
+                               ws, ws_bytes, stream))
 
 
 def msa_kv_select(scores, seq_len, keep, index, count, first: int = 0, recent: int = 0, stream=None) -> None:
     """Enqueue the choice of the positions that stay: tensors ``scores`` float32 [sequences, lists, positions] and
     ``index`` int32 [sequences, lists, entries]; ``seq_len`` and ``keep`` int32 [sequences].  ``index`` and ``count``
     int32 [sequences] are written."""
-    who, dev = "msa_kv_select", this_device()
+    who = "msa_kv_select"
+    dev, stream = here(stream)
     if len(getattr(scores, "shape", ())) != 3:
         _refuse(who, "scores is not a tensor [sequences, lists, positions]")
     B, H, L = scores.shape
@@ -83,14 +84,15 @@ def msa_kv_select(scores, seq_len, keep, index, count, first: int = 0, recent: i
         refuse_large(who, first=first, recent=recent, sequences=B, lists=H, positions=L, entries=entries)
     _check(_lib.msa_kv_select(B, H, at, step[0], step[1], L, address(who, "seq_len", seq_len, INT32, B, dev),
                               address(who, "keep", keep, INT32, B, dev), first, recent, entries, to,
-                              to_step[0], to_step[1], address(who, "count", count, INT32, B, dev), _stream(stream)))
+                              to_step[0], to_step[1], address(who, "count", count, INT32, B, dev), stream))
 
 
 def msa_kv_compact(shape: msa_shape, base, index, count, block_table, k_cache, v_cache, stream=None) -> None:
     """Enqueue the moves of K and V at ``base[b] + index[b, (head,) i]`` to ``base[b] + i``, i < ``count[b]``.
     ``index`` is an int32 tensor [sequences, entries], the same for all heads, or [sequences, KV heads, entries];
     ``base`` (or None: 0) and ``count`` int32 [sequences], ``block_table`` int32 [sequences, max_blocks_per_seq]."""
-    who, B, dev = "msa_kv_compact", shape.num_seqs, this_device()
+    who, B = "msa_kv_compact", shape.num_seqs
+    dev, stream = here(stream)
     if not hasattr(index, "stride"):
         _refuse(who, "index is not a tensor")
     if index.dim() == 2:
@@ -106,4 +108,4 @@ def msa_kv_compact(shape: msa_shape, base, index, count, block_table, k_cache, v
                                entries, address(who, "count", count, INT32, B, dev),
                                address(who, "block_table", block_table, INT32, B * shape.max_blocks_per_seq, dev),
                                values_address(who, "k_cache", k_cache, dev),
-                               values_address(who, "v_cache", v_cache, dev), _stream(stream)))
+                               values_address(who, "v_cache", v_cache, dev), stream))

@@ -18,8 +18,9 @@ try:
     Tensor = torch.Tensor
     INT32, FLOAT32, MASK = (torch.int32,), (torch.float32,), (torch.int64, torch.uint64)
     BF16 = (torch.bfloat16, torch.int16, torch.uint16)  # or its bits
-    # torch's own lookup takes 0.15 us, the public call 0.26
+    # torch's own lookups take 0.15 us, the public calls 0.26 and 2.9
     _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _raw_stream, _ready = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.is_initialized
     _PROB = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # MSA_PROB_*
 except ImportError:  # the package itself does without; then nothing here is a tensor
     Tensor = None
@@ -53,12 +54,14 @@ _bind("msa_tree_verify", [_P, _i32, _i32, _P, _i64, _P, _i64, _P, _P, _P, _P, _P
 _bind("msa_tree_verify_workspace", [_P, _i32, ctypes.POINTER(ctypes.c_size_t)])
 
 
-def this_device() -> int:
-    """The current device, -1 (a host tensor's) or an exception's -2 where there is none."""
+def here(stream):
+    """(current device, handle of ``stream`` or of the device's current one); device -2, which no tensor is on, where
+    there is none."""
     try:
-        return _device()
+        dev = _device()
     except (NameError, RuntimeError):
-        return -2
+        return -2, _stream(stream)
+    return dev, _raw_stream(dev) if stream is None and _raw_stream and _ready() else _stream(stream)
 
 
 def refuse_tensor(who: str, name: str, x, dtypes, need: Optional[int], dev: int, rows: Optional[int] = None) -> None:
@@ -124,7 +127,7 @@ def workspace_of(who: str, workspace, given: int, dev: int):
     """(address, bytes) of a workspace: a tensor, whose bytes are taken from it unless given, or an address."""
     if workspace is None:
         return None, int(given)
-    if not hasattr(workspace, "stride"):
+    if type(workspace) is not Tensor and not hasattr(workspace, "stride"):
         if not given:
             raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: workspace_bytes is needed with a workspace's address")
         return _addr(workspace), int(given)
@@ -142,14 +145,16 @@ def refuse_large(who: str, **sizes: int) -> None:
 
 
 def sizes_of(plan: Plan):
-    """(entries of the plan's block table, of its lse)."""
-    sizes = getattr(plan, "sizes", None)
-    if sizes is None:
+    """(entries of the plan's block table, of its lse, its sequences, its KV heads, the most positions of a sequence)."""
+    try:
+        return plan.sizes
+    except AttributeError:
         sh = plan.shape
         if not plan.handle or sh is None:  # no plan: the library reports that
-            return 0, 0
-        sizes = plan.sizes = (sh.num_seqs * sh.max_blocks_per_seq, msa_plan_info(plan)["total_q"] * sh.num_q_heads)
-    return sizes
+            return 0, 0, 0, 0, 0
+        plan.sizes = (sh.num_seqs * sh.max_blocks_per_seq, msa_plan_info(plan)["total_q"] * sh.num_q_heads, sh.num_seqs,
+                      sh.num_kv_heads, sh.max_blocks_per_seq * sh.block_size)
+        return plan.sizes
 
 
 def _row_stride(x, width: int) -> int:
@@ -195,10 +200,10 @@ def msa_tree_mask(plan: Plan, parents, mask, mask_stride: Optional[int] = None, 
     """Enqueue the trees' ancestor masks: ``parents`` int32 [tree_rows] to ``mask`` int64 or uint64
     [tree_rows, >= mask_words]."""
     _, rows, _, words = _figures(plan)
-    dev = this_device()
+    dev, stream = here(stream)
     up = address("msa_tree_mask", "parents", parents, INT32, rows, dev)
     at, step = rows_address("msa_tree_mask", "mask", mask, MASK, words, rows, dev, mask_stride)
-    _check(_lib.msa_tree_mask(plan.handle, up, at, step, _stream(stream)))
+    _check(_lib.msa_tree_mask(plan.handle, up, at, step, stream))
 
 
 def msa_tree_forward(plan: Plan, q, k_cache, v_cache, block_table, mask, o, lse=None, workspace=None,
@@ -206,8 +211,9 @@ def msa_tree_forward(plan: Plan, q, k_cache, v_cache, block_table, mask, o, lse=
     """Enqueue the attention of a plan with trees for one layer; ``mask`` as of ``msa_tree_mask`` (None if the plan
     has no tree), ``block_table`` int32 [sequences, max_blocks_per_seq], ``lse`` float32 [total_q, query heads], the rest
     as of ``msa_forward``."""
-    who, dev = "msa_tree_forward", this_device()
-    entries, lses = sizes_of(plan)
+    who = "msa_tree_forward"
+    dev, stream = here(stream)
+    entries, lses = sizes_of(plan)[:2]
     _, rows, _, words = _figures(plan)
     at, step = rows_address(who, "mask", mask, MASK, words, rows, dev, mask_stride)
     ws, ws_bytes = workspace_of(who, workspace, workspace_bytes, dev)
@@ -216,7 +222,8 @@ def msa_tree_forward(plan: Plan, q, k_cache, v_cache, block_table, mask, o, lse=
                                  values_address(who, "v_cache", v_cache, dev),
                                  address(who, "block_table", block_table, INT32, entries, dev), at, step,
                                  values_address(who, "o", o, dev),
-                                 None if lse is None else address(who, "lse", lse, FLOAT32, lses, dev), ws, ws_bytes, _stream(stream)))
+                                 None if lse is None else address(who, "lse", lse, FLOAT32, lses, dev), ws, ws_bytes,
+                                 stream))
 
 
 def msa_tree_verify_workspace(plan: Plan, vocab: int) -> int:
@@ -232,7 +239,8 @@ def msa_tree_verify(plan: Plan, target, tokens, parents, u_accept, u_sample, pat
     """Enqueue the verification of the plan's trees.  ``target`` (and ``draft``, or None) are tensors
     [tree_rows, vocab] of float32, bfloat16 or float16; ``path`` int32 [trees, >= max_slots], ``path_len`` and
     ``next_token`` int32 [trees] are written."""
-    who, dev = "msa_tree_verify", this_device()
+    who = "msa_tree_verify"
+    dev, stream = here(stream)
     trees, rows, slots, _ = _figures(plan)
     if not hasattr(target, "stride") or target.dim() != 2:
         raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: target is not a 2-D tensor")
@@ -250,4 +258,4 @@ def msa_tree_verify(plan: Plan, target, tokens, parents, u_accept, u_sample, pat
                                 address(who, "u_sample", u_sample, FLOAT32, trees, dev), at, step,
                                 address(who, "path_len", path_len, INT32, trees, dev),
                                 address(who, "next_token", next_token, INT32, trees, dev), ws, ws_bytes,
-                                _stream(stream)))
+                                stream))

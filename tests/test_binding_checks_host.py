@@ -125,6 +125,7 @@ class OnDevice:
 @pytest.fixture
 def device0(monkeypatch):
     monkeypatch.setattr("paper_2606_02964_amd.tree._device", lambda: 0)
+    monkeypatch.setattr("paper_2606_02964_amd.tree._raw_stream", lambda dev: None)
 
 
 F32, BF16 = torch.float32, torch.bfloat16
