@@ -9,8 +9,9 @@
 // neighbouring positions: it counts what it keeps, learns from the other
 // waves' counts where its own begin, and writes them in order.
 // A list in a buffer of up to 64K scores is read once, into registers (32 or 64 keys
-// a thread); others are read again by every pass.  One list of 9001 takes 8.5 us,
-// 256 of 2K to 16K with half kept 16.8, one of 200 6.4: that is passes and barriers.
+// a thread); others are read again by every pass.  One list of 9001 takes 9.0 us,
+// 256 of 2K to 16K with half kept 16.6, one of 200 6.4: that is passes and barriers
+// (waves wait 63% of the time; LDS is busy 15%, a third of it with conflicts).
 // Reading is the smaller part: one instruction for each of 16K keys takes a CU 256
 // cycles (16 waves, 16 keys a lane), so time goes by instructions per key.  (With the window and the list's end
 // tested by position in every loop, and lanes that share a bin added up first, a

@@ -6,9 +6,9 @@
 // of the segment's own slots, so nothing but the masked steps differs, of which
 // a tree has one to three of its row's dozens or hundreds.  The merge of
 // split tiles is msa_merge as it is.  Bound as those are: 48 trees of 16 slots over
-// up to 6K keys each (32 query, 8 KV heads, d = 128) read K/V at 4.9 TB/s (150 us);
+// up to 6K keys each (32 query, 8 KV heads, d = 128) read K/V at 4.9 TB/s (154 us);
 // 16 of 64 slots, each beside a chunk of 128 rows, over up to 30K keys (64 query heads)
-// run at 920 TFLOP/s (600 us); one of 61 slots over 8K 21.6 us with its merge.
+// run at 934 TFLOP/s (599 us); one of 61 slots over 8K 21.4 us with its merge.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -79,7 +79,7 @@ int launch_tree(const TreeAttnParams& p, int item_rows, int num_wg, hipStream_t 
 // its ancestors: each thread follows the parents of its slots up to the root
 // through LDS, setting bits of one word at a time (a parent is a lower slot, so
 // the walk ends, and it enters the words in descending order).
-// A step's masks are a few KB; the launch is all there is to it (1.8 us).
+// A step's masks are a few KB; the launch is all there is to it (1.6 us).
 __global__ __launch_bounds__(256) void msa_tree_mask_kernel(const TreeSpan* trees, const int32_t* parents,
                                                             uint64_t* mask, int64_t stride, int words) {
   __shared__ int16_t up[MSA_TREE_MAX_SLOTS];

@@ -22,7 +22,8 @@
 // that write back an XCD's whole L2, for every workgroup, 32 trees took 80 us.
 // Bound by reading one or two rows of the vocabulary per tree, and for few trees by
 // the chains of dependent reads in walk and pick (32 trees, two rows of 131072 fp32
-// each: 16.8 us; the rows' 34 MB alone take 6.1 us).
+// each: 16.5 us; the rows' 34 MB alone take 6.1 us; 32 trees of drawn slots over
+// 128000, whose walks sum rows too: 46.5 us, 37 of them the walk).
 // Sums are in 64 bits: with 10^5 tokens the borders between neighbouring tokens
 // are about 10^-5 of the mass apart and a 32-bit running sum would pick a
 // neighbour once in some hundred draws; and the tests' products (24 + 24 bits)
