@@ -40,7 +40,7 @@ class Budget:
         ws = torch.empty(max(1, plan.info()["workspace_bytes"]), dtype=torch.uint8, device="cuda")
         msa.msa_kv_append(plan, k, v, self.table, self.k, self.v)
         msa.msa_forward(plan, q, self.k, self.v, self.table, o, lse, ws)
-        exec(example("msa_kv_weights("), dict(msa=msa, torch=torch, plan=plan, layers=range(1), q=q, k_cache=self.k,
+        exec(example("msa_kv_weights(plan"), dict(msa=msa, torch=torch, plan=plan, layers=range(1), q=q, k_cache=self.k,
                                               block_table=self.table, lse=lse, weights=self.weights))
         torch.cuda.synchronize()
         self.calls += 1
