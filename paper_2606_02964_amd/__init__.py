@@ -8,7 +8,8 @@ fallback: importing this package without a built library raises.
 Functions carry the C names: ``msa_plan``, ``msa_plan_info``,
 ``msa_forward``, ``msa_kv_append``, ``msa_plan_destroy``,
 ``msa_last_error``, ``msa_plan_export``, ``msa_check_block_table``,
-``msa_forward_noalloc``; those of ``tree.py`` and ``cache.py`` are re-exported.
+``msa_forward_noalloc``; those of ``tree.py``, ``cache.py``, ``window.py``,
+``rope.py`` and ``fp8.py`` are re-exported.
 Device buffers are passed as objects with a
 ``data_ptr()`` method (e.g. torch tensors) or as integer addresses; streams
 as ``hipStream_t`` integers or objects with ``cuda_stream`` (torch streams).
@@ -391,8 +392,14 @@ class Evictor:
         return out
 
 
-# the entry points of msa_tree.h and msa_cache.h
+# the entry points of msa_tree.h, msa_cache.h, msa_window.h, msa_rope.h and msa_fp8.h
 from .tree import *  # noqa: E402,F401,F403
 from .tree import EXPORTED_TREE  # noqa: E402,F401
 from .cache import *  # noqa: E402,F401,F403
 from .cache import EXPORTED_CACHE  # noqa: E402,F401
+from .window import *  # noqa: E402,F401,F403
+from .window import EXPORTED_WINDOW  # noqa: E402,F401
+from .rope import *  # noqa: E402,F401,F403
+from .rope import EXPORTED_ROPE  # noqa: E402,F401
+from .fp8 import *  # noqa: E402,F401,F403
+from .fp8 import EXPORTED_FP8  # noqa: E402,F401

@@ -14,6 +14,7 @@
 #include "forward.h"
 #include "msa_internal.h"
 #include "msa_tree.h"
+#include "msa_window.h"
 #include "plan_handle.h"
 
 namespace {
@@ -96,6 +97,15 @@ msa_status msa::launched(const char* who, const char* what, int rc) {
                    std::string(who) + ": " + what + " launch failed: " + hipGetErrorString((hipError_t)rc));
 }
 
+msa::WindowAttnParams msa::window_params(msa_plan_t plan, const AttnParams& base) {
+  msa::WindowAttnParams p{};
+  static_cast<msa::AttnParams&>(p) = base;
+  p.window = plan->hp.window;
+  p.sinks = plan->hp.sinks;
+  p.head = msa::sink_keys(plan->hp.sinks);
+  return p;
+}
+
 msa_status msa::merge_splits(const char* who, msa_plan_t plan, void* o, float* lse, void* workspace,
                              void* hip_stream) {
   const msa::HostPlan& hp = plan->hp;
@@ -124,7 +134,10 @@ msa_status msa::forward_impl(const char* who, msa_plan_t plan, const void* q, co
   msa_status st = forward_params(who, plan, q, k_cache, v_cache, block_table, o, lse, workspace, workspace_bytes, &p);
   if (st != MSA_OK || plan->hp.work.empty()) return st;
   const msa::HostPlan& hp = plan->hp;
-  st = launched(who, "attention", msa::launch_attn(p, hp.shape.head_dim, hp.item_rows, hp.num_workgroups(), hip_stream));
+  const msa::WindowAttnParams wp = hp.window > 0 ? window_params(plan, p) : msa::WindowAttnParams{};
+  const msa::AttnParams* params = &p;
+  if (hp.window > 0) params = &wp;
+  st = launched(who, "attention", msa::launch_attn(*params, hp.shape.head_dim, hp.item_rows, hp.num_workgroups(), hip_stream));
   return st != MSA_OK ? st : merge_splits(who, plan, o, lse, workspace, hip_stream);
 }
 
@@ -140,7 +153,7 @@ namespace {
 
 msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
                      const int32_t* seg_start, const int32_t* seg_len, bool with_trees, const int32_t* seg_tree,
-                     const msa_plan_opts* opts, void* hip_stream, msa_plan_t* out) {
+                     int32_t window, int32_t sinks, const msa_plan_opts* opts, void* hip_stream, msa_plan_t* out) {
   const std::string w(who);
   if (!out) return set_error(MSA_ERR_INVALID_ARG, w + ": out must be non-null");
   *out = nullptr;
@@ -150,7 +163,7 @@ msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq
   msa_status st;
   try {
     st = msa::build_plan(shape, seq_kv_len, seg_indptr, seg_start, seg_len, opts, with_trees, seg_tree,
-                         &plan->hp, &err);
+                         window, sinks, &plan->hp, &err);
   } catch (const std::bad_alloc&) {
     st = MSA_ERR_OUT_OF_MEMORY;
     err = "host allocation failed while planning";
@@ -191,7 +204,15 @@ msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq
       return set_error(MSA_ERR_OUT_OF_MEMORY, w + ": host allocation failed");
     }
     if (n_row) std::memcpy(plan->staging.data(), hp.row_pos.data(), n_row);
-    if (n_work) std::memcpy(plan->staging.data() + off_work, hp.work.data(), n_work);
+    // (with a window, an item's last number says on the device where its first row's window starts)
+    auto device_item = [&](msa::WorkItem w) {
+      if (hp.window > 0) w.wg = msa::window_start(hp.row_pos[(size_t)w.row0], hp.window);
+      return w;
+    };
+    for (size_t i = 0; i < hp.work.size(); ++i) {
+      const msa::WorkItem w = device_item(hp.work[i]);
+      std::memcpy(plan->staging.data() + off_work + i * sizeof(w), &w, sizeof(w));
+    }
     if (n_merge) std::memcpy(plan->staging.data() + off_merge, hp.merge.data(), n_merge);
     if (n_append) std::memcpy(plan->staging.data() + off_append, hp.append.data(), n_append);
     if (n_seq) std::memcpy(plan->staging.data() + off_seq, hp.seq_row0.data(), n_seq);
@@ -203,7 +224,7 @@ msa_status make_plan(const char* who, const msa_shape* shape, const int32_t* seq
     for (size_t i = 0; i < n_wg; ++i) {
       msa::WgHead h{};
       const int32_t first = hp.wg_ptr[i], end = hp.wg_ptr[i + 1];
-      if (first < end) h.first = hp.work[(size_t)first];
+      if (first < end) h.first = device_item(hp.work[(size_t)first]);
       h.rest = std::min(first + 1, end);
       h.end = end;
       std::memcpy(plan->staging.data() + off_heads + i * sizeof(h), &h, sizeof(h));
@@ -250,15 +271,25 @@ extern "C" {
 msa_status msa_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
                     const int32_t* seg_start, const int32_t* seg_len, const msa_plan_opts* opts,
                     void* hip_stream, msa_plan_t* out) {
-  return make_plan("msa_plan", shape, seq_kv_len, seg_indptr, seg_start, seg_len, false, nullptr, opts, hip_stream,
-                   out);
+  return make_plan("msa_plan", shape, seq_kv_len, seg_indptr, seg_start, seg_len, false, nullptr, 0, 0, opts,
+                   hip_stream, out);
+}
+
+msa_status msa_plan_window(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
+                           const int32_t* seg_start, const int32_t* seg_len, int32_t window, int32_t sinks,
+                           const msa_plan_opts* opts, void* hip_stream, msa_plan_t* out) {
+  if (out) *out = nullptr;
+  if (window < 1) return set_error(MSA_ERR_INVALID_ARG, "msa_plan_window: window must be >= 1");
+  if (sinks < 0) return set_error(MSA_ERR_INVALID_ARG, "msa_plan_window: sinks must be >= 0");
+  return make_plan("msa_plan_window", shape, seq_kv_len, seg_indptr, seg_start, seg_len, false, nullptr, window, sinks,
+                   opts, hip_stream, out);
 }
 
 msa_status msa_plan_tree(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
                          const int32_t* seg_start, const int32_t* seg_len, const int32_t* seg_tree,
                          const msa_plan_opts* opts, void* hip_stream, msa_plan_t* out) {
-  return make_plan("msa_plan_tree", shape, seq_kv_len, seg_indptr, seg_start, seg_len, true, seg_tree, opts,
-                   hip_stream, out);
+  return make_plan("msa_plan_tree", shape, seq_kv_len, seg_indptr, seg_start, seg_len, true, seg_tree, 0, 0,
+                   opts, hip_stream, out);
 }
 
 msa_status msa_plan_tree_info(msa_plan_t plan, msa_tree_info_t* info) {
@@ -352,12 +383,20 @@ msa_status msa_check_block_table(msa_plan_t plan, const int32_t* block_table, in
   const int64_t row_stride = location == MSA_TABLE_DEVICE ? width : s.max_blocks_per_seq;
   for (int32_t b = 0; b < s.num_seqs; ++b) {
     const int32_t* row = table + (int64_t)b * row_stride;
-    for (int32_t i = 0; i < hp.seq_blocks[(size_t)b]; ++i)
+    // a window's blocks start at its first row's; before them the sinks' are read
+    int32_t sink_blocks = 0, first_block = 0;
+    if (hp.window > 0 && hp.seq_blocks[(size_t)b] > 0) {
+      sink_blocks = (int32_t)(((int64_t)hp.sinks + s.block_size - 1) / s.block_size);
+      first_block = msa::window_start(hp.row_pos[(size_t)hp.seq_row0[(size_t)b]], hp.window) / s.block_size;
+    }
+    for (int32_t i = 0; i < hp.seq_blocks[(size_t)b]; ++i) {
+      if (i >= sink_blocks && i < first_block) continue;
       if (row[i] < 0 || row[i] >= s.num_blocks)
-        return set_error(MSA_ERR_INVALID_ARG,
+          return set_error(MSA_ERR_INVALID_ARG,
                          "msa_check_block_table: sequence " + std::to_string(b) + ", logical block " +
-                             std::to_string(i) + " maps to physical block " + std::to_string(row[i]) +
-                             ", outside [0, " + std::to_string(s.num_blocks) + ")");
+                               std::to_string(i) + " maps to physical block " + std::to_string(row[i]) +
+                               ", outside [0, " + std::to_string(s.num_blocks) + ")");
+    }
   }
   return MSA_OK;
 }

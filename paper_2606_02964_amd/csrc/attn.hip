@@ -145,6 +145,7 @@ int launch_attn_form(const AttnParams& p, int head_dim, int item_rows, int num_w
 int launch_attn(const AttnParams& p, int head_dim, int item_rows, int num_wg, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (num_wg <= 0) return 0;
+  if (p.window > 0) return launch_window(static_cast<const WindowAttnParams&>(p), head_dim, item_rows, num_wg, stream);
   return p.precise ? launch_attn_form<true>(p, head_dim, item_rows, num_wg, s)
                    : launch_attn_form<false>(p, head_dim, item_rows, num_wg, s);
 }

@@ -1,0 +1,222 @@
+// attn8_device.h -- work items of up to 32 rows over an 8-bit cache, read straight
+// into registers (decode_item of attn_device.h, which has the mathematics, over bytes).
+//
+// The four waves of a workgroup hold the same rows and take 32-key half-steps in
+// turn.  What differs is how keys and channels lie in the operands, so that every
+// load is 16 bytes:
+//   * QK: lane half hl holds channels 32 i + 16 hl .. + 15 of its key (and of Q): a
+//     product does not mind the order of its terms.  A key's power of two goes into
+//     the conversion to bf16, which is exact.
+//   * PV: a V chunk is 16 tokens of a channel, so lane half hl takes the tokens of
+//     block hl of the half-step's two.  K's rows are ordered such that the lane's 16
+//     scores are these tokens' too, in order: weights meet V without a move.  A
+//     token's power of two multiplies its weight (exactly), not its d values.
+// Half the bytes of the bf16 form leave registers for both K and V of the next
+// half-step while one is computed.
+#pragma once
+
+#include "attn_device.h"
+
+namespace msa {
+namespace {
+
+__device__ __forceinline__ bf16x8 fp8_octet(uint32_t lo, uint32_t hi, float scale) {
+  return __builtin_bit_cast(bf16x8, make_uint4(fp8_pair<false>(lo, scale), fp8_pair<true>(lo, scale),
+                                               fp8_pair<false>(hi, scale), fp8_pair<true>(hi, scale)));
+}
+
+template <int D, bool kPrecise, class P>
+__device__ __forceinline__ void decode8_item(const P& p, const WorkItem w, DecodeLds<D>& lds) {
+  constexpr int kWaves = DecodeLds<D>::kWaves, kHalf = 32;
+  if (w.nrows == 0) return;  // (uniform over the workgroup)
+
+  // (an opaque copy of the thread id: lane-dependent set-up is computed per item)
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, hl = lane >> 5, ln = lane & 31;
+  const int G = p.group;
+  const int t = div_group(ln, p), hh = ln - t * G;  // tile row ln <-> token t, head hh of the group
+  const bool valid = t < w.nrows;
+  const int tok = w.row0 + t;
+  const int head = w.kv_head * G + hh;
+  const auto axis = key_axis(p, w);
+
+  // the two blocks of half-step h, as in decode_item
+  const int32_t* bt = p.block_table + (int64_t)w.seq * p.max_blocks;
+  const int nh = (w.kv_hi - w.kv_lo + kHalf - 1) / kHalf;
+  auto table_blocks = [&](int h, int32_t& id0, int32_t& id1) {
+    const int k0 = w.kv_lo + h * kHalf;
+    id0 = bt[axis.block(k0)];
+    id1 = k0 + kBlockSize < w.kv_hi ? bt[axis.next_block(k0)] : id0;
+  };
+  int32_t idv0 = 0, idv1 = 0;
+  if (wave + kWaves * lane < nh) table_blocks(wave + kWaves * lane, idv0, idv1);
+
+  const auto row_of = row_view(p, valid, tok);
+  const int pos = row_of.pos;
+  constexpr int kQk = D / 16;  // QK MFMAs per half-step
+  bf16x8 qf[kQk];
+  {
+    const uint16_t* qrow = p.q + (int64_t)tok * p.q_st + (int64_t)head * p.q_sh + hl * 16;
+#pragma unroll
+    for (int kk = 0; kk < kQk; ++kk) {
+      if (valid) {
+        qf[kk] = *reinterpret_cast<const bf16x8*>(qrow + (kk >> 1) * 32 + (kk & 1) * 8);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) qf[kk][j] = (__bf16)0.0f;
+      }
+    }
+  }
+
+  // MFMA row m of K is token (m bits 4, 3, 1, 0) of block (m bit 2), so that lane half hl gets the
+  // scores of block hl, register e those of token e
+  const int kblk = (ln >> 2) & 1, ktok = ((ln >> 3) & 3) * 4 + (ln & 3);
+  const char* kbase = reinterpret_cast<const char*>(p.k) + (int64_t)w.kv_head * p.k_sh;
+  const char* vbase = reinterpret_cast<const char*>(p.v) + (int64_t)w.kv_head * p.v_sh;
+  const uint32_t koff = (uint32_t)(ktok * p.k_st + hl * 16);
+  const uint32_t voff = (uint32_t)(ln * p.v_sd);
+  const uint32_t vdt = (uint32_t)(32 * p.v_sd);
+  const uint8_t* ksb = p.k_scale + w.kv_head * kBlockSize + ktok;
+  const uint8_t* vsb = p.v_scale + w.kv_head * kBlockSize;
+  const int64_t scales = (int64_t)p.num_kv_heads * kBlockSize;  // of a block
+
+  auto blocks = [&](int h, int64_t& id0, int64_t& id1) __attribute__((always_inline)) {
+    const int i = (h - wave) / kWaves;  // wave-uniform
+    if (i < 64) {
+      id0 = __builtin_amdgcn_readlane(idv0, i);
+      id1 = __builtin_amdgcn_readlane(idv1, i);
+    } else {
+      int32_t a, b;
+      table_blocks(h, a, b);
+      id0 = a;
+      id1 = b;
+    }
+  };
+  constexpr int kChunks = D / 32;  // 16-byte chunks of a lane, of K and of V
+  uint4 ka[2][kChunks], va[2][kChunks], vs[2];
+  uint32_t ks[2];
+  auto load = [&](auto bsel, int h) __attribute__((always_inline)) {
+    constexpr int b = decltype(bsel)::value;
+    int64_t id0, id1;
+    blocks(h, id0, id1);
+    const int64_t kid = kblk ? id1 : id0, vid = hl ? id1 : id0;
+    const char* kp = kbase + kid * p.k_sb + koff;
+    const char* vp = vbase + vid * p.v_sb + voff;
+    ks[b] = ksb[kid * scales];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) ka[b][i] = *reinterpret_cast<const uint4*>(kp + i * 32);
+    vs[b] = *reinterpret_cast<const uint4*>(vsb + vid * scales);
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) va[b][i] = *reinterpret_cast<const uint4*>(vp + i * vdt);
+  };
+
+  const float c = p.scale_log2;
+  float m_ref = -__builtin_inff(), l_run = 0.0f;
+  f32x16 oacc[D / 32];
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.0f;
+
+  int pmin = 0, pmax = 0;  // positions of the tile's first and last row (set below, once loads are under way)
+  auto half = [&](auto bsel, int h) __attribute__((always_inline)) {
+    constexpr int b = decltype(bsel)::value;
+    if (h + kWaves < nh) load(std::integral_constant<int, 1 - b>{}, h + kWaves);
+    const float kf = __uint_as_float(ks[b] << 23);
+    f32x16 sc = {};
+#pragma unroll
+    for (int kk = 0; kk < kQk; ++kk) {
+      const uint4& x = ka[b][kk >> 1];
+      const bf16x8 a = kk & 1 ? fp8_octet(x.z, x.w, kf) : fp8_octet(x.x, x.y, kf);
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kk], sc, 0, 0, 0);
+    }
+    // score e of a lane is token e of block hl
+    const int k0 = axis.key(w.kv_lo + h * kHalf);
+    const bool masked = k0 + kHalf - 1 >= pmin || before_window(p, k0, kHalf, pmax);
+    const bool split = (k0 | (kKvStep - 1)) >= pmin || kPrecise;  // lo terms of the weights, as in decode_item
+    if (masked) {
+      const int lim = pos - k0 - hl * 16;
+      if constexpr (P::kWindow) {
+        const int low = lim - p.window, sink = p.sinks - k0 - hl * 16;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = e <= lim && (e > low || e < sink) ? sc[e] : -__builtin_inff();
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[e] = e <= lim ? sc[e] : -__builtin_inff();
+      }
+    }
+    // weights and their sum; wv: times V's powers of two
+    float wv[16], ls;
+    auto weights = [&]() {
+      const float nm = m_ref == -__builtin_inff() ? 0.0f : -m_ref;
+      ls = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        wv[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e], c, nm));
+        wv[e + 1] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e + 1], c, nm));
+        ls += wv[e] + wv[e + 1];
+      }
+    };
+    weights();
+    if (__any(!(ls < kSettleSum) || m_ref == -__builtin_inff())) {  // the lazy reference max
+      float mx = -__builtin_inff();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, sc[e]);
+      const float m_blk = pair_max(mx) * c;
+      const bool grow = m_blk > m_ref + kRescaleLog2;
+      if (__any(grow)) {
+        const float alpha = grow ? __builtin_amdgcn_exp2f(m_ref - m_blk) : 1.0f;
+        m_ref = grow ? m_blk : m_ref;
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) oacc[dt] *= alpha;
+        weights();
+      }
+    }
+    l_run += ls;
+    const uint32_t sv[4] = {vs[b].x, vs[b].y, vs[b].z, vs[b].w};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) wv[e] *= __uint_as_float((sv[e >> 2] >> (8 * (e & 3)) & 0xff) << 23);
+    uint32_t pk[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) pk[u] = pack_bf16x2(wv[2 * u], wv[2 * u + 1]);
+    const bool own = (row_of.first | (kKvStep - 1)) <= (k0 | (kKvStep - 1)) &&
+                     (k0 | (kKvStep - 1)) <= (pos | (kKvStep - 1));
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const bf16x8 ph = __builtin_bit_cast(bf16x8, make_uint4(pk[4 * ks], pk[4 * ks + 1], pk[4 * ks + 2], pk[4 * ks + 3]));
+      bf16x8 a[D / 32];
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt) {
+        a[dt] = ks ? fp8_octet(va[b][dt].z, va[b][dt].w, 1.0f) : fp8_octet(va[b][dt].x, va[b][dt].y, 1.0f);
+        oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[dt], ph, oacc[dt], 0, 0, 0);
+      }
+      if (split) {
+        uint32_t lo[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const bf16x2 hv = __builtin_bit_cast(bf16x2, pk[4 * ks + u]);
+          const uint32_t x = pack_bf16x2(wv[8 * ks + 2 * u] - (float)hv[0], wv[8 * ks + 2 * u + 1] - (float)hv[1]);
+          lo[u] = kPrecise || own ? x : 0u;
+        }
+        const bf16x8 pl = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+          oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[dt], pl, oacc[dt], 0, 0, 0);
+      }
+    }
+  };
+  if (wave < nh) load(std::integral_constant<int, 0>{}, wave);
+  pmin = __builtin_amdgcn_readfirstlane(row_of.first);
+  pmax = __builtin_amdgcn_readlane(pos, w.nrows * G - 1);
+  for (int h = wave; h < nh; h += 2 * kWaves) {
+    half(std::integral_constant<int, 0>{}, h);
+    if (h + kWaves < nh) half(std::integral_constant<int, 1>{}, h + kWaves);
+  }
+  merge_waves<D>(p, w, lds, tid, wave, hl, ln, oacc, m_ref, l_run);
+}
+
+}  // namespace
+}  // namespace msa

@@ -50,6 +50,10 @@
 // some of the latest keys taken out, so plan, tiles and steps stay as they
 // are; only the masked steps begin at the tree's first slot, where a row's
 // few latest keys may be spread over several steps, all with hi + lo terms.
+// Windows (WindowAttnParams): a row sees its latest positions and the first few.
+// A tile's keys then lie on an axis that leaves out what none of its rows sees
+// (KeyAxis), a work item's key range counts along it, and steps that hold a window's
+// start or a part of the sinks are masked too; they come first, and run without overlap.
 // Both kernels also come in a precise-weights form (kPrecise, selected by
 // the plan): every step, or half-step, carries every row's weights as
 // hi + lo terms.
@@ -87,6 +91,10 @@ struct Tile {
   static constexpr int kBytesV = kKvStep * D * 2;
   static constexpr int kPage = kBlockSize * D * 2;  // bytes of one block of K or V
   static constexpr int kDmaPerPage = kPage / 1024;  // 1 KB per wave-wide 16-byte copy
+  // LDS of a workgroup: K ring (2 steps), V ring (2 steps); an 8-bit cache: the next step's pages as they
+  // are (at d = 128 80 KB in all, so that two workgroups still fit a CU)
+  template <class P>
+  static constexpr int lds_bytes() { return 2 * (kBytesK + kBytesV) + (P::kFp8 ? kKvStep * D * 2 : 0); }
 };
 
 __device__ __forceinline__ int swap_bits23(int m) {
@@ -107,6 +115,18 @@ __device__ __forceinline__ float pair_sum(float x) {
 __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
   const bf16x2 v = {(__bf16)a, (__bf16)b};
   return __builtin_bit_cast(uint32_t, v);
+}
+
+// two e4m3 numbers of a register times a power of two as a bf16 pair (exact): its lower or upper two ...
+template <bool kUpper>
+__device__ __forceinline__ uint32_t fp8_pair(uint32_t x, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, kUpper));
+}
+// ... and numbers i and i + 1 with a power each (bits of floats)
+template <int i>
+__device__ __forceinline__ uint32_t fp8_pair2(uint32_t x, uint32_t scale0, uint32_t scale1) {
+  return pack_bf16x2(__builtin_amdgcn_cvt_scalef32_f32_fp8(x, __uint_as_float(scale0), i),
+                     __builtin_amdgcn_cvt_scalef32_f32_fp8(x, __uint_as_float(scale1), i + 1));
 }
 
 typedef __attribute__((address_space(3))) void lds_void_t;
@@ -186,6 +206,39 @@ __device__ __forceinline__ TreeRowView row_view(const TreeAttnParams& p, bool va
   return v;
 }
 
+// The positions that a work item's key range stands for.  Without a window the range
+// is the positions; with one see WindowAttnParams and window_skip.
+struct PlainAxis {
+  __device__ __forceinline__ int key(int v) const { return v; }
+  __device__ __forceinline__ int at(int key) const { return key; }
+  __device__ __forceinline__ int block(int v) const { return v >> 4; }
+  __device__ __forceinline__ int next_block(int v) const { return (v >> 4) + 1; }  // of the half-step at v
+};
+struct WindowAxis {
+  int head, skip;
+  int sink_blocks, first_block;  // blocks from sink_blocks to before first_block hold no visible key
+
+  __device__ __forceinline__ int key(int v) const { return v < head ? v : v + skip; }
+  __device__ __forceinline__ int at(int key) const { return key - skip; }  // of a position behind the part left out
+  // The logical block of key v's tokens.  A step may hold blocks without a visible key, before a
+  // window's start or behind the sinks: their table entries need not be valid, so the first block of the
+  // window stands in (all its keys are hidden there).
+  __device__ __forceinline__ int block(int v) const {
+    const int b = key(v) >> 4;
+    return b >= sink_blocks && b < first_block ? first_block : b;
+  }
+  __device__ __forceinline__ int next_block(int v) const { return block(v + kBlockSize); }
+};
+__device__ __forceinline__ PlainAxis key_axis(const AttnParams&, const WorkItem&) { return {}; }
+__device__ __forceinline__ WindowAxis key_axis(const WindowAttnParams& p, const WorkItem& w) {
+  return {p.head, window_skip(w.wg, p.head), (p.sinks >> 4) + ((p.sinks & 15) != 0), w.wg >> 4};
+}
+// Whether keys k0 .. k0 + n - 1 hold one that a window hides from the row at `pos`
+__device__ __forceinline__ bool before_window(const AttnParams&, int, int, int) { return false; }
+__device__ __forceinline__ bool before_window(const WindowAttnParams& p, int k0, int n, int pos) {
+  return max(k0, p.sinks) <= min(k0 + n - 1, pos - p.window);
+}
+
 // r / G for a tile row r < 256 (r * (G * group_inv - 2^16) < 2^16, so exact)
 __device__ __forceinline__ int div_group(int r, const AttnParams& p) {
   return (int)((uint32_t)r * (uint32_t)p.group_inv >> 16);
@@ -197,7 +250,7 @@ __device__ __forceinline__ int div_group(int r, const AttnParams& p) {
 // refill the rings at once.
 template <int D, int W, bool kPrecise, bool kHelp, class P>
 __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* smem) {
-  constexpr bool kTree = P::kTree;
+  constexpr bool kTree = P::kTree, kFp8 = P::kFp8;
   using T = Tile<D>;
   constexpr int kRows = 32 * W;  // tile rows
   if (w.nrows == 0) return;  // (uniform over the workgroup)
@@ -214,6 +267,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   const bool valid = t < w.nrows;
   const int tok = w.row0 + t;
   const int head = w.kv_head * G + hh;
+  const auto axis = key_axis(p, w);
 
   // Block ids: every page a wave copies belongs to block slot wave & 3 of
   // its step, so a wave needs one id per step.  Lane i of idv holds the id of
@@ -225,7 +279,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   auto load_ids = [&](int s0) -> int32_t {
     const int st = s0 + lane;
     const int kb = w.kv_lo + st * kKvStep + bslot * kBlockSize;
-    return (st < n && kb < w.kv_hi) ? bt[kb >> 4] : 0;
+    return (st < n && kb < w.kv_hi) ? bt[axis.block(kb)] : 0;
   };
   int32_t idv = load_ids(0), idv_next = n > 64 ? load_ids(64) : 0;
 
@@ -264,9 +318,11 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   // by 32 channels (bit 3 of the channel, hence the half swap, is unchanged)
   const uint32_t vgo0 = (uint32_t)((lane >> 1) * p.v_sd + (((lane & 1) ^ ((lane >> 4) & 1)) * 8)) * 2u;
   const uint32_t vgq = (uint32_t)(32 * p.v_sd) * 2u;
-  const int64_t ksb = p.k_sb * 2, vsb = p.v_sb * 2;  // bytes per block
-  const char* kbase = reinterpret_cast<const char*>(p.k + (int64_t)w.kv_head * p.k_sh);
-  const char* vbase = reinterpret_cast<const char*>(p.v + (int64_t)w.kv_head * p.v_sh);
+  constexpr int kSize = kFp8 ? 1 : 2;  // bytes of a number in the cache
+  const int64_t ksb = p.k_sb * kSize, vsb = p.v_sb * kSize;  // bytes per block
+  typedef typename std::conditional<kFp8, const uint8_t*, const uint16_t*>::type cache_t;
+  const char* kbase = reinterpret_cast<const char*>((cache_t)p.k + (int64_t)w.kv_head * p.k_sh);
+  const char* vbase = reinterpret_cast<const char*>((cache_t)p.v + (int64_t)w.kv_head * p.v_sh);
   auto kbuf = [&](int s) -> char* { return smem + __builtin_amdgcn_readfirstlane((s & 1) * T::kBytesK); };
   auto vbuf = [&](int s) -> char* {
     return smem + __builtin_amdgcn_readfirstlane(2 * T::kBytesK + (s & 1) * T::kBytesV);
@@ -285,6 +341,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   // values: those keys are masked by selection, so never meet arithmetic).
   const bool copier = wave >= 4 || (W == 4 && !kHelp);  // wave-uniform
   const char *kpage, *vpage;  // pages of the next copies
+  const uint8_t *kspage, *vspage;  // 8-bit caches: their powers of two
   int32_t id_cur = 0;
   // Reads the ids of K step s and V step s - 1 and takes their page
   // addresses; called for s = 0, 1, 2, ... in turn, one iteration before the
@@ -300,6 +357,11 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
     kpage = kbase + (int64_t)id_cur * ksb;
     vpage = vbase + (int64_t)id_prev * vsb;
     asm volatile("" : "+s"(kpage), "+s"(vpage));
+    if constexpr (kFp8) {
+      kspage = p.k_scale + ((int64_t)id_cur * p.num_kv_heads + w.kv_head) * kBlockSize;
+      vspage = p.v_scale + ((int64_t)id_prev * p.num_kv_heads + w.kv_head) * kBlockSize;
+      asm volatile("" : "+s"(kspage), "+s"(vspage));
+    }
   };
   // before next_pages(s) at multiples of 64: the next 64 ids move in
   auto move_ids = [&](int s) __attribute__((always_inline)) {
@@ -318,14 +380,111 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
 #pragma unroll
     for (int q = 0; q < T::kDmaPerPage; ++q) dma16(src + q * vgq, vgo0, vd + q * 1024);
   };
+  // An 8-bit cache's pages go through LDS as they are (raw) and are turned into bf16 in the rings, once
+  // for all waves, so that everything behind the rings is as for a bf16 cache: the numbers are exact in
+  // bf16.  In iteration j a wave turns what it has copied, K of step j+2 and V of step j+1, into the
+  // rings, then copies K of step j+3 and V of step j+2 to the same places: a wave reads what it wrote
+  // alone, so no barrier is added, and a copy has an iteration to arrive.  Registers would hold as
+  // much, but the pipelined step leaves too few.  A K chunk (16 channels of a token) has one power of two,
+  // which the conversion applies; a V chunk (16 tokens of a channel) has 16, the same for all lanes.
+  // Four waves share the pages' 1 KB pieces by block slot; of eight computing waves both groups of four
+  // take half of them (d = 64: K and V, whose pages are one piece); helpers take all of them.
+  constexpr int kPieces = D / 64;  // of a page
+  constexpr bool kHalved = kFp8 && W == 8 && !kHelp;
+  constexpr int kMine = kHalved && kPieces == 2 ? 1 : kPieces;  // of a page, that a wave takes
+  char* raw = smem + 2 * (T::kBytesK + T::kBytesV) + bslot * (2 * kPieces * 1024);
+  uint32_t kgo8[kMine], vgo8[kMine];  // byte offsets inside a block
+  uint32_t ksc[kMine], vsc = 0;       // powers of two of what is in raw: the K chunks' tokens, lanes 0-3: V
+  auto piece = [&](int i) { return kHalved && kPieces == 2 ? (wave >> 2) : i; };
+  const bool takes_k = !kHalved || kPieces == 2 || wave < 4, takes_v = !kHalved || kPieces == 2 || wave >= 4;
+  auto k_token = [&](int i) { return (piece(i) * 64 + lane) / (D / 16); };
+  if constexpr (kFp8) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      kgo8[i] = (uint32_t)(k_token(i) * p.k_st + (lane % (D / 16)) * 16);
+      vgo8[i] = (uint32_t)((piece(i) * 64 + lane) * p.v_sd);
+    }
+  }
+  // chunk i of a page of step s into the ring
+  auto put_k = [&](int s, int i, const uint4& x, uint32_t scale) __attribute__((always_inline)) {
+    const int t = k_token(i), c = 2 * (lane % (D / 16));
+    char* to = kbuf(s) + bslot * T::kPage + t * (2 * D);
+    const float f = __uint_as_float(scale << 23);
+    *reinterpret_cast<uint4*>(to + ((c ^ kswz(t)) * 16)) = make_uint4(
+        fp8_pair<false>(x.x, f), fp8_pair<true>(x.x, f), fp8_pair<false>(x.y, f), fp8_pair<true>(x.y, f));
+    *reinterpret_cast<uint4*>(to + (((c + 1) ^ kswz(t)) * 16)) = make_uint4(
+        fp8_pair<false>(x.z, f), fp8_pair<true>(x.z, f), fp8_pair<false>(x.w, f), fp8_pair<true>(x.w, f));
+  };
+  auto put_v = [&](int s, int i, const uint4& x, uint32_t scales) __attribute__((always_inline)) {
+    const int c = piece(i) * 64 + lane;
+    char* to = vbuf(s) + bslot * T::kPage + c * 32;
+    const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+    uint32_t y[8];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const uint32_t f = __builtin_amdgcn_readlane(scales, d);
+      y[2 * d] = fp8_pair2<0>(u[d], (f & 0xff) << 23, (f >> 8 & 0xff) << 23);
+      y[2 * d + 1] = fp8_pair2<2>(u[d], (f >> 16 & 0xff) << 23, f >> 24 << 23);
+    }
+    const int swap = (c >> 3) & 1;
+    *reinterpret_cast<uint4*>(to + swap * 16) = make_uint4(y[0], y[1], y[2], y[3]);
+    *reinterpret_cast<uint4*>(to + (swap ^ 1) * 16) = make_uint4(y[4], y[5], y[6], y[7]);
+  };
+  auto has = [&](int s) { return w.kv_lo + bslot * kBlockSize + s * kKvStep < w.kv_hi; };  // a block of step s
+  // (a block at or past kv_hi is not read, as above)
+  auto convert = [&](int sk, int sv) __attribute__((always_inline)) {
+    if (kHelp && !copier) return;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (takes_k && has(sk)) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i)
+        put_k(sk, i, *reinterpret_cast<const uint4*>(raw + piece(i) * 1024 + lane * 16), ksc[i]);
+    }
+    if (takes_v && sv < n) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        if (has(sv)) {
+          put_v(sv, i, *reinterpret_cast<const uint4*>(raw + (kPieces + piece(i)) * 1024 + lane * 16), vsc);
+        } else {
+          char* to = vbuf(sv) + bslot * T::kPage + piece(i) * 2048 + lane * 32;
+          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<uint4*>(to + 16) = make_uint4(0, 0, 0, 0);
+        }
+      }
+    }
+  };
+  auto fetch = [&](int sk, int sv) __attribute__((always_inline)) {
+    if (kHelp && !copier) return;
+    if (takes_k && has(sk)) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        dma16(kpage, kgo8[i], raw + piece(i) * 1024);
+        ksc[i] = kspage[k_token(i)];
+      }
+    }
+    if (takes_v && has(sv)) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) dma16(vpage, vgo8[i], raw + (kPieces + piece(i)) * 1024);
+      vsc = reinterpret_cast<const uint32_t*>(vspage)[lane & 3];
+    }
+  };
   // copies of iteration j, both steps whole
   auto copy_whole = [&](int j) __attribute__((always_inline)) {
+    if constexpr (kFp8) {
+      convert(j + 2, j + 1);
+      fetch(j + 3, j + 2);
+      return;
+    }
     if (!copier) return;
     copy_k(kpage, j + 2);
     copy_v(vpage, j + 1);
   };
   // K of step sk and V of step sv where either may end inside the step or lie past the end
   auto copy_any = [&](const char* ksrc, int sk, const char* vsrc, int sv) {
+    if constexpr (kFp8) {
+      convert(sk, sv);
+      fetch(sk + 1, sv + 1);
+      return;
+    }
     if (!copier) return;
     const int kb = w.kv_lo + bslot * kBlockSize;
     if (kb + sk * kKvStep < w.kv_hi) copy_k(ksrc, sk);
@@ -403,7 +562,17 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
       }
       return;
     }
-    const int lim = pos - (w.kv_lo + s * kKvStep) - hl * 8;
+    const int lim = pos - axis.key(w.kv_lo + s * kKvStep) - hl * 8;
+    if constexpr (P::kWindow) {
+      const int low = lim - p.window, sink = p.sinks - axis.key(w.kv_lo + s * kKvStep) - hl * 8;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const int at = (e >> 4) * 32 + ((e & 15) >> 3) * 16 + (e & 7);
+        const float x = sbuf[b][e >> 4][e & 15];
+        sbuf[b][e >> 4][e & 15] = at <= lim && (at > low || at < sink) ? x : -__builtin_inff();
+      }
+      return;
+    }
 #pragma unroll
     for (int e = 0; e < 32; ++e) {
       const float x = sbuf[b][e >> 4][e & 15];
@@ -609,11 +778,48 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   // barrier that ended iteration j-1 (the buffers' previous contents K_j and
   // V_{j-1} were last read before it) and waited for before the barrier that
   // ends iteration j.
+  constexpr int kLead = kFp8 ? 4 : 3;  // iteration j takes the page addresses of K step j + kLead
   next_pages(0);
-  copy_any(kbase + (int64_t)id_cur * ksb, 0, vbase + (int64_t)id_cur * vsb, 0);
-  next_pages(1);
-  copy_any(kpage, 1, vbase, n);
-  next_pages(2);
+  if constexpr (kFp8) {
+    // the first pages straight to the rings: K of steps 0 and 1, V of step 0
+    if (!kHelp || copier) {
+      uint4 k0[kMine] = {}, k1[kMine] = {}, v0[kMine] = {};
+      uint32_t s0[kMine] = {}, s1[kMine] = {}, sv = 0;
+      const uint8_t* vs = p.v_scale + ((int64_t)id_cur * p.num_kv_heads + w.kv_head) * kBlockSize;
+      const char* vp = vbase + (int64_t)id_cur * vsb;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        if (takes_k && has(0)) {
+          k0[i] = *reinterpret_cast<const uint4*>(kpage + kgo8[i]);
+          s0[i] = kspage[k_token(i)];
+        }
+        if (takes_v && has(0)) v0[i] = *reinterpret_cast<const uint4*>(vp + vgo8[i]);
+      }
+      if (takes_v && has(0)) sv = reinterpret_cast<const uint32_t*>(vs)[lane & 3];
+      next_pages(1);
+#pragma unroll
+      for (int i = 0; i < kMine; ++i)
+        if (takes_k && has(1)) {
+          k1[i] = *reinterpret_cast<const uint4*>(kpage + kgo8[i]);
+          s1[i] = kspage[k_token(i)];
+        }
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        if (takes_k) put_k(0, i, k0[i], s0[i]), put_k(1, i, k1[i], s1[i]);
+        if (takes_v) put_v(0, i, v0[i], sv);
+      }
+    } else {
+      next_pages(1);
+    }
+    next_pages(2);
+    fetch(2, 1);
+    next_pages(3);
+  } else {
+    copy_any(kbase + (int64_t)id_cur * ksb, 0, vbase + (int64_t)id_cur * vsb, 0);
+    next_pages(1);
+    copy_any(kpage, 1, vbase, n);
+    next_pages(2);
+  }
   // wave-wide smallest and largest causal limit: a tile's rows are in
   // ascending position, so those of its first and last row
   const int nvalid = __builtin_popcountll(__ballot(valid)) >> 1;  // rows (both lane halves hold them)
@@ -622,11 +828,16 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   const int pmax = nvalid > 0 ? __builtin_amdgcn_readlane(pos, nvalid - 1) : -1;
   // (>=: a step whose last key is some row's position counts too, so that
   // every row's diagonal step runs through the masked path)
-  auto need_mask = [&](int s) { return w.kv_lo + s * kKvStep + kKvStep - 1 >= pmin; };
+  auto past_first = [&](int s) { return axis.key(w.kv_lo + s * kKvStep) + kKvStep - 1 >= pmin; };
+  auto need_mask = [&](int s) {
+    if constexpr (P::kWindow) return past_first(s) || before_window(p, axis.key(w.kv_lo + s * kKvStep), kKvStep, pmax);
+    return past_first(s);
+  };
   // steps this wave computes: keys up to its largest position.  A wave past
   // them still copies its share of every step and meets every barrier.
-  const int nw = pmax >= w.kv_lo ? min(n, (pmax - w.kv_lo) / kKvStep + 1) : 0;
-  wait_dma<0>();
+  const int vmax = axis.at(pmax);
+  const int nw = vmax >= w.kv_lo ? min(n, (vmax - w.kv_lo) / kKvStep + 1) : 0;
+  if constexpr (!kFp8) wait_dma<0>();
   lds_barrier();
   if (nw > 0) {
     qk_plain(0, 0);
@@ -644,43 +855,9 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   // steps differently between the parts; every step still ends with exactly
   // one barrier.
   auto tail = [&]() {
-    wait_dma<0>();
+    if constexpr (!kFp8) wait_dma<0>();
     lds_barrier();
   };
-  int j = 0;
-  const int whole = (w.kv_hi - w.kv_lo) / kKvStep;  // steps without a missing block
-  for (; j + 2 < nw && !need_mask(j + 2); j += 2) {
-    copy_whole(j);  // step j+2 is not masked, hence whole
-    fused(std::integral_constant<int, 0>{}, [&]() { next_pages(j + 3); });
-    tail();
-    if (j + 3 < whole) copy_whole(j + 1);
-    else copy_any(kpage, j + 3, vpage, j + 2);
-    move_ids(j + 4);
-    fused(std::integral_constant<int, 1>{}, [&]() { next_pages(j + 4); });
-    tail();
-  }
-  // One or two steps without a mask may remain before the diagonal ones: the
-  // same, with the next step's mask after its scores.  (With precise weights
-  // the pipelined step takes the next step's row max, so that one must need no
-  // mask either.)  A 3-step item of a helped workgroup 9.9 -> 8.9 us.
-  if (j + 1 < nw && !need_mask(kPrecise ? j + 1 : j)) {
-    copy_any(kpage, j + 2, vpage, j + 1);
-    fused(std::integral_constant<int, 0>{}, [&]() { next_pages(j + 3); });
-    if (!kPrecise && need_mask(j + 1)) mask_plain(1, j + 1);
-    tail();
-    ++j;
-    if (!kPrecise && j + 1 < nw && !need_mask(j)) {
-      copy_any(kpage, j + 2, vpage, j + 1);
-      move_ids(j + 3);
-      fused(std::integral_constant<int, 1>{}, [&]() { next_pages(j + 3); });
-      if (need_mask(j + 1)) mask_plain(0, j + 1);
-      tail();
-      ++j;
-    } else {
-      sbuf[0][0] = sbuf[1][0];
-      sbuf[0][1] = sbuf[1][1];
-    }
-  }
   // Remaining steps (the diagonal ones and the last) run without overlap:
   // weights of step j, PV of step j, then QK + mask of step j+1 into the
   // same score registers.  Same copy schedule as the pipelined loop.
@@ -726,7 +903,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
     };
     weigh();
     settle(0, ls, weigh);
-    const int s_lo = w.kv_lo + jj * kKvStep;
+    const int s_lo = axis.key(w.kv_lo + jj * kKvStep);
     // this is the row's diagonal step, or one of those that hold its tree's slots
     const bool own = pos >= s_lo && row.first < s_lo + kKvStep;
     l_run += ls;
@@ -752,16 +929,62 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
       if (need_mask(jj + 1)) mask_plain(0, jj + 1);
     }
   };
-  for (; j < n; ++j) {
-    copy_any(kpage, j + 2, vpage, j + 1);
-    move_ids(j + 3);
-    next_pages(j + 3);
-    if (j < nw) {
-      if constexpr (kPrecise) plain_precise(j);
-      else plain(j, need_mask(j));
+  // One step without overlap; waves past their last step still copy.
+  auto step = [&](int jj) __attribute__((always_inline)) {
+    copy_any(kpage, jj + 2, vpage, jj + 1);
+    move_ids(jj + kLead);
+    next_pages(jj + kLead);
+    if (jj < nw) {
+      if constexpr (kPrecise) plain_precise(jj);
+      else plain(jj, past_first(jj));
     }
     tail();
+  };
+  int j = 0;
+  if constexpr (P::kWindow) {
+    // the steps that hold a hidden key before some row's window (an even number: the paired loop
+    // takes its ring stages from that), and those of the sinks before them
+    const int hidden = pmax - p.window;  // the last such key
+    const int v = hidden >= axis.head + axis.skip ? axis.at(hidden) : min(hidden, axis.head - 1);
+    const int lead = v < w.kv_lo ? 0 : ((v - w.kv_lo) / kKvStep + 2) & ~1;
+    for (; j < lead && j < n; ++j) step(j);
   }
+  const int whole = (w.kv_hi - w.kv_lo) / kKvStep;  // steps without a missing block
+  for (; j + 2 < nw && !need_mask(j + 2); j += 2) {
+    copy_whole(j);  // step j+2 is not masked, hence whole
+    if constexpr (kFp8) move_ids(j + 4);  // (an odd step is none that ids move in at)
+    fused(std::integral_constant<int, 0>{}, [&]() { next_pages(j + kLead); });
+    tail();
+    if (j + 3 < whole) copy_whole(j + 1);
+    else copy_any(kpage, j + 3, vpage, j + 2);
+    if constexpr (!kFp8) move_ids(j + 4);
+    fused(std::integral_constant<int, 1>{}, [&]() { next_pages(j + 1 + kLead); });
+    tail();
+  }
+  // One or two steps without a mask may remain before the diagonal ones: the
+  // same, with the next step's mask after its scores.  (With precise weights
+  // the pipelined step takes the next step's row max, so that one must need no
+  // mask either.)  A 3-step item of a helped workgroup 9.9 -> 8.9 us.
+  if (j + 1 < nw && !need_mask(kPrecise ? j + 1 : j)) {
+    copy_any(kpage, j + 2, vpage, j + 1);
+    if constexpr (kFp8) move_ids(j + 4);
+    fused(std::integral_constant<int, 0>{}, [&]() { next_pages(j + kLead); });
+    if (!kPrecise && need_mask(j + 1)) mask_plain(1, j + 1);
+    tail();
+    ++j;
+    if (!kPrecise && j + 1 < nw && !need_mask(j)) {
+      copy_any(kpage, j + 2, vpage, j + 1);
+      if constexpr (!kFp8) move_ids(j + 3);
+      fused(std::integral_constant<int, 1>{}, [&]() { next_pages(j + kLead); });
+      if (need_mask(j + 1)) mask_plain(0, j + 1);
+      tail();
+      ++j;
+    } else {
+      sbuf[0][0] = sbuf[1][0];
+      sbuf[0][1] = sbuf[1][1];
+    }
+  }
+  for (; j < n; ++j) step(j);
 
   // epilogue: lane (hl, ln) holds row r, channels dt*32 + (i/4)*8 + hl*4 + i%4
   const float l_tot = pair_sum(l_run);
@@ -818,15 +1041,84 @@ struct DecodeLds {
   float mm[kWaves][32], ml[kWaves][32];
 };
 
+// Merges the waves' partial states of an item of up to 32 rows and writes its rows'
+// output: lane (hl, ln) holds row ln, channels dt*32 + (i/4)*8 + hl*4 + i%4.
+template <int D, class P>
+__device__ __forceinline__ void merge_waves(const P& p, const WorkItem& w, DecodeLds<D>& lds, int tid, int wave,
+                                            int hl, int ln, const f32x16 (&oacc)[D / 32], float m_ref, float l_run) {
+  constexpr bool kTree = P::kTree;
+  constexpr int kWaves = DecodeLds<D>::kWaves;
+  auto& mo = lds.mo;
+  auto& mm = lds.mm;
+  auto& ml = lds.ml;
+  const int G = p.group;
+  const float l_tot = pair_sum(l_run);
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+      f32x4 v;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = oacc[dt][g4 * 4 + q];
+      *reinterpret_cast<f32x4*>(&mo[wave][ln][dt * 32 + g4 * 8 + hl * 4]) = v;
+    }
+  if (hl == 0) {
+    mm[wave][ln] = m_ref;
+    ml[wave][ln] = l_tot;
+  }
+  __syncthreads();
+  constexpr int kCh = D / 8;  // channels per thread: 32 rows x 8 threads
+  const int row = tid >> 3, c0 = (tid & 7) * kCh;
+  const int rt = div_group(row, p), rh = row - rt * G;
+  if (rt >= w.nrows) return;
+  float M = -__builtin_inff();
+#pragma unroll
+  for (int u = 0; u < kWaves; ++u) M = fmaxf(M, mm[u][row]);
+  float L = 0.0f, acc[kCh];
+#pragma unroll
+  for (int q = 0; q < kCh; ++q) acc[q] = 0.0f;
+#pragma unroll
+  for (int u = 0; u < kWaves; ++u) {
+    const float f = mm[u][row] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mm[u][row] - M);
+    L += f * ml[u][row];
+#pragma unroll
+    for (int q = 0; q < kCh; q += 4) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(&mo[u][row][c0 + q]);
+#pragma unroll
+      for (int z = 0; z < 4; ++z) acc[q + z] += f * v[z];
+    }
+  }
+  const int otok = w.row0 + rt, ohead = w.kv_head * G + rh;
+  if (w.out_slot < 0) {
+    const float inv = kTree && L == 0.0f ? 0.0f : 1.0f / L;
+    uint16_t* orow = p.o + (int64_t)otok * p.o_st + (int64_t)ohead * p.o_sh + c0;
+#pragma unroll
+    for (int q = 0; q < kCh; q += 4)
+      *reinterpret_cast<uint2*>(orow + q) = make_uint2(pack_bf16x2(acc[q] * inv, acc[q + 1] * inv),
+                                                       pack_bf16x2(acc[q + 2] * inv, acc[q + 3] * inv));
+    if (p.lse && c0 == 0) p.lse[(int64_t)otok * p.num_q_heads + ohead] = (M + __log2f(L)) * kLn2;
+  } else {
+    const int R = p.slot_rows;
+    float* slot = p.ws + (int64_t)w.out_slot * R * (D + 1);
+    const bool empty = kTree ? L == 0.0f : !(L > 0.0f);  // no visible key in this split
+    const float inv = empty ? 0.0f : 1.0f / L;
+#pragma unroll
+    for (int q = 0; q < kCh; q += 4) {
+      f32x4 v;
+#pragma unroll
+      for (int z = 0; z < 4; ++z) v[z] = acc[q + z] * inv;
+      *reinterpret_cast<f32x4*>(slot + row * D + c0 + q) = v;
+    }
+    if (c0 == 0) slot[(int64_t)R * D + row] = empty ? -__builtin_inff() : (M + __log2f(L)) * kLn2;
+  }
+}
+
 // One work item of msa_decode; the LDS merge area is reused by the next item
 // only after the barrier the caller places between items.
 template <int D, bool kPrecise, class P>
 __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, DecodeLds<D>& lds) {
   constexpr bool kTree = P::kTree;
   constexpr int kWaves = DecodeLds<D>::kWaves, kHalf = 32;
-  auto& mo = lds.mo;
-  auto& mm = lds.mm;
-  auto& ml = lds.ml;
   if (w.nrows == 0) return;  // (uniform over the workgroup)
 
   // lane-dependent set-up is computed per item (an opaque copy of the
@@ -840,6 +1132,7 @@ __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, Decode
   const bool valid = t < w.nrows;
   const int tok = w.row0 + t;
   const int head = w.kv_head * G + hh;
+  const auto axis = key_axis(p, w);
 
   // The two blocks of half-step h.  The second one is only read when it
   // holds a key of the range; otherwise the first one stands in (its keys
@@ -852,8 +1145,8 @@ __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, Decode
   const int nh = (w.kv_hi - w.kv_lo + kHalf - 1) / kHalf;  // (an item's keys end at its last row's position or before)
   auto table_blocks = [&](int h, int32_t& id0, int32_t& id1) {
     const int k0 = w.kv_lo + h * kHalf;
-    id0 = bt[k0 >> 4];
-    id1 = k0 + kBlockSize < w.kv_hi ? bt[(k0 >> 4) + 1] : id0;
+    id0 = bt[axis.block(k0)];
+    id1 = k0 + kBlockSize < w.kv_hi ? bt[axis.next_block(k0)] : id0;
   };
   int32_t idv0 = 0, idv1 = 0;
   if (wave + kWaves * lane < nh) table_blocks(wave + kWaves * lane, idv0, idv1);
@@ -926,6 +1219,7 @@ __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, Decode
     for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.0f;
 
   int pmin = 0;  // position (or tree start) of the tile's first row, the smallest (set below, once loads are under way)
+  int pmax = 0;  // position of its last row (windows)
   // one half-step h of this wave, its K in buffer b
   auto half = [&](auto bsel, int h) __attribute__((always_inline)) {
     constexpr int b = decltype(bsel)::value;
@@ -935,18 +1229,27 @@ __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, Decode
 #pragma unroll
     for (int kk = 0; kk < kQk; ++kk) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[b][kk], qf[kk], sc, 0, 0, 0);
     // score e (0..15) of a lane is key (e / 8) * 16 + hl * 8 + e % 8 of the half-step
-    const int k0 = w.kv_lo + h * kHalf;
+    const int k0 = axis.key(w.kv_lo + h * kHalf);
     // On the two half-steps of a row's diagonal 64-key step (split) the row
     // also enters its weights' bf16 lo terms, as in the main kernel: a
     // second PV pass on them follows (with precise weights: on every
     // half-step, for every row).
-    const bool masked = k0 + kHalf - 1 >= pmin;  // holds some row's position, or passes one
+    const bool masked = k0 + kHalf - 1 >= pmin || before_window(p, k0, kHalf, pmax);  // some row does not see all of it
     const bool split = (k0 | (kKvStep - 1)) >= pmin || kPrecise;
     if (masked && kTree) {
       if constexpr (kTree) {
         const uint32_t seen = (uint32_t)row_of.visible(k0) >> (hl * 8);
 #pragma unroll
         for (int e = 0; e < 16; ++e) sc[e] = (seen >> ((e >> 3) * 16 + (e & 7))) & 1 ? sc[e] : -__builtin_inff();
+      }
+    } else if (masked && P::kWindow) {
+      if constexpr (P::kWindow) {
+        const int lim = pos - k0 - hl * 8, low = lim - p.window, sink = p.sinks - k0 - hl * 8;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int at = (e >> 3) * 16 + (e & 7);
+          sc[e] = at <= lim && (at > low || at < sink) ? sc[e] : -__builtin_inff();
+        }
       }
     } else if (masked) {
       const int lim = pos - k0 - hl * 8;
@@ -1024,72 +1327,13 @@ __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, Decode
   };
   if (wave < nh) load_k(std::integral_constant<int, 0>{}, wave);
   pmin = __builtin_amdgcn_readfirstlane(row_of.first);
+  if constexpr (P::kWindow) pmax = __builtin_amdgcn_readlane(pos, w.nrows * G - 1);
   for (int h = wave; h < nh; h += 2 * kWaves) {
     half(std::integral_constant<int, 0>{}, h);
     if (h + kWaves < nh) half(std::integral_constant<int, 1>{}, h + kWaves);
   }
 
-  // merge the waves' partial states: lane (hl, ln) holds row ln, channels
-  // dt*32 + (i/4)*8 + hl*4 + i%4
-  const float l_tot = pair_sum(l_run);
-#pragma unroll
-  for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-    for (int g4 = 0; g4 < 4; ++g4) {
-      f32x4 v;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = oacc[dt][g4 * 4 + q];
-      *reinterpret_cast<f32x4*>(&mo[wave][ln][dt * 32 + g4 * 8 + hl * 4]) = v;
-    }
-  if (hl == 0) {
-    mm[wave][ln] = m_ref;
-    ml[wave][ln] = l_tot;
-  }
-  __syncthreads();
-  constexpr int kCh = D / 8;  // channels per thread: 32 rows x 8 threads
-  const int row = tid >> 3, c0 = (tid & 7) * kCh;
-  const int rt = div_group(row, p), rh = row - rt * G;
-  if (rt >= w.nrows) return;
-  float M = -__builtin_inff();
-#pragma unroll
-  for (int u = 0; u < kWaves; ++u) M = fmaxf(M, mm[u][row]);
-  float L = 0.0f, acc[kCh];
-#pragma unroll
-  for (int q = 0; q < kCh; ++q) acc[q] = 0.0f;
-#pragma unroll
-  for (int u = 0; u < kWaves; ++u) {
-    const float f = mm[u][row] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mm[u][row] - M);
-    L += f * ml[u][row];
-#pragma unroll
-    for (int q = 0; q < kCh; q += 4) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(&mo[u][row][c0 + q]);
-#pragma unroll
-      for (int z = 0; z < 4; ++z) acc[q + z] += f * v[z];
-    }
-  }
-  const int otok = w.row0 + rt, ohead = w.kv_head * G + rh;
-  if (w.out_slot < 0) {
-    const float inv = kTree && L == 0.0f ? 0.0f : 1.0f / L;
-    uint16_t* orow = p.o + (int64_t)otok * p.o_st + (int64_t)ohead * p.o_sh + c0;
-#pragma unroll
-    for (int q = 0; q < kCh; q += 4)
-      *reinterpret_cast<uint2*>(orow + q) = make_uint2(pack_bf16x2(acc[q] * inv, acc[q + 1] * inv),
-                                                       pack_bf16x2(acc[q + 2] * inv, acc[q + 3] * inv));
-    if (p.lse && c0 == 0) p.lse[(int64_t)otok * p.num_q_heads + ohead] = (M + __log2f(L)) * kLn2;
-  } else {
-    const int R = p.slot_rows;
-    float* slot = p.ws + (int64_t)w.out_slot * R * (D + 1);
-    const bool empty = kTree ? L == 0.0f : !(L > 0.0f);  // no visible key in this split
-    const float inv = empty ? 0.0f : 1.0f / L;
-#pragma unroll
-    for (int q = 0; q < kCh; q += 4) {
-      f32x4 v;
-#pragma unroll
-      for (int z = 0; z < 4; ++z) v[z] = acc[q + z] * inv;
-      *reinterpret_cast<f32x4*>(slot + row * D + c0 + q) = v;
-    }
-    if (c0 == 0) slot[(int64_t)R * D + row] = empty ? -__builtin_inff() : (M + __log2f(L)) * kLn2;
-  }
+  merge_waves<D>(p, w, lds, tid, wave, hl, ln, oacc, m_ref, l_run);
 }
 
 }  // namespace

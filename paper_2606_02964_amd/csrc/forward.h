@@ -21,6 +21,9 @@ msa_status forward_params(const char* who, msa_plan_t plan, const void* q, const
                           const void* v_cache, const int32_t* block_table, void* o, float* lse,
                           void* workspace, size_t workspace_bytes, AttnParams* out);
 
+// The same with the plan's window (hp.window > 0).
+WindowAttnParams window_params(msa_plan_t plan, const AttnParams& base);
+
 // The merge launch of the plan's split tiles, if it has any.
 msa_status merge_splits(const char* who, msa_plan_t plan, void* o, float* lse, void* workspace,
                         void* hip_stream);

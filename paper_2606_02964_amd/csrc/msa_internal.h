@@ -36,7 +36,8 @@ struct WorkItem {
   int32_t kv_lo;     // first key (multiple of kKvStep)
   int32_t kv_hi;     // one past the last key
   int32_t out_slot;  // -1: final output; >= 0: workspace slot of a partial
-  int32_t wg;        // the workgroup (blockIdx.x) that runs it
+  int32_t wg;        // the workgroup (blockIdx.x) that runs it; on the device, in plans with a window,
+                     // the first position that its first row's window holds
 };
 static_assert(sizeof(WorkItem) == 32, "WorkItem is exported as 8 int32");
 
@@ -77,9 +78,23 @@ struct TreeSpan {
   int32_t n;
 };
 
+// Keys of a tile in a plan with a window (msa_window.h) lie on an axis of their own:
+// the positions below `head` (the sinks rounded up to whole key steps), then those from
+// head + skip on.  A work item's kv_lo and kv_hi count along it.
+// (at most the largest multiple of kKvStep that 32 bits hold: no window starts past it)
+constexpr int32_t sink_keys(int32_t sinks) {
+  return sinks > INT32_MAX - kKvStep ? INT32_MAX / kKvStep * kKvStep : (sinks + kKvStep - 1) / kKvStep * kKvStep;
+}
+constexpr int32_t window_start(int32_t pos, int32_t window) { return pos < window ? 0 : pos - window + 1; }
+// positions left out between the two parts, a multiple of kKvStep; first: the first row's window_start
+constexpr int32_t window_skip(int32_t first, int32_t head) {
+  const int32_t whole = first / kKvStep * kKvStep;
+  return whole > head ? whole - head : 0;
+}
+
 // Arguments of the attention kernel.
 struct AttnParams {
-  static constexpr bool kTree = false;
+  static constexpr bool kTree = false, kWindow = false, kFp8 = false;
   const uint16_t* q;
   const uint16_t* k;
   const uint16_t* v;
@@ -100,6 +115,7 @@ struct AttnParams {
   int32_t slot_rows; // rows of a workspace slot
   float scale_log2;  // scale * log2(e)
   int32_t precise;   // nonzero: every step carries hi + lo weights (MSA_PLAN_PRECISE_WEIGHTS)
+  int32_t window;    // positions that a row sees up to its own; 0: all, else this is a WindowAttnParams
 };
 
 struct TreeAttnParams : AttnParams {
@@ -107,6 +123,20 @@ struct TreeAttnParams : AttnParams {
   const RowTree* row_tree;  // [rows]
   const uint64_t* mask;     // [tree rows][mask_stride]
   int64_t mask_stride;      // words
+};
+
+struct WindowAttnParams : AttnParams {
+  static constexpr bool kWindow = true;
+  int32_t sinks, head;  // head: sink_keys(sinks)
+};
+
+// The same over an 8-bit cache (k and v point to bytes).
+template <class Base>
+struct Fp8Params : Base {
+  static constexpr bool kFp8 = true;
+  const uint8_t* k_scale;  // [blocks][KV heads][16]
+  const uint8_t* v_scale;
+  int32_t num_kv_heads;
 };
 
 struct MergeParams {
@@ -121,9 +151,11 @@ struct MergeParams {
   int32_t max_rows;   // rows (tokens x G) of the largest split tile
 };
 
-// Launchers (attn.hip).  Return a hipError_t value as int.
+// Launchers (attn.hip, window.hip).  Return a hipError_t value as int.
 // item_rows: rows of the widest work item (32, 128 or 256), which selects the kernel.
+// launch_attn hands parameters with a window to launch_window.
 int launch_attn(const AttnParams& p, int head_dim, int item_rows, int num_wg, void* stream);
+int launch_window(const WindowAttnParams& p, int head_dim, int item_rows, int num_wg, void* stream);
 int launch_merge(const MergeParams& p, int head_dim, int num_merge, void* stream);
 
 }  // namespace msa

@@ -267,7 +267,8 @@ msa_status check_shape(const msa_shape& s, std::string* err) {
 
 msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
                       const int32_t* seg_start, const int32_t* seg_len, const msa_plan_opts* opts,
-                      bool with_trees, const int32_t* seg_tree, HostPlan* out, std::string* err) {
+                      bool with_trees, const int32_t* seg_tree, int32_t window, int32_t sinks, HostPlan* out,
+                      std::string* err) {
   if (!shape || !out) return fail(err, MSA_ERR_INVALID_ARG, "shape and out must be non-null");
   const msa_shape& s = *shape;
   msa_plan_opts o{};
@@ -316,6 +317,13 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
   P.shape = s;
   P.group = G;
   P.precise_weights = (o.flags & MSA_PLAN_PRECISE_WEIGHTS) != 0;
+  // keys that the row at position p sees, and the keys of a tile of rows first .. last on its axis
+  auto seen = [&](int64_t p) {
+    return window == 0 || p < window ? p + 1 : window + std::min<int64_t>(sinks, p - window + 1);
+  };
+  auto axis_keys = [&](int32_t first, int32_t last) {
+    return last + 1 - (window == 0 ? 0 : window_skip(window_start(first, window), sink_keys(sinks)));
+  };
   std::vector<int64_t> seq_row0(B + 1, 0);
   std::vector<int32_t> seq_maxpos(B, -1);
   int64_t total = 0, num_trees = 0;
@@ -362,6 +370,13 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
       for (int32_t k = seg_indptr[b]; k < seg_indptr[b + 1]; ++k)
         for (int32_t t = 0; t < seg_len[k]; ++t) P.row_pos[(size_t)r++] = seg_start[k] + t;
   }
+  // (no more than there are positions: sums of them stay within 32 bits)
+  if (window > 0) {
+    int32_t top = 1;
+    for (int32_t b = 0; b < B; ++b) top = std::max(top, seq_maxpos[b] + 1);
+    P.window = window = std::min(window, top);
+    P.sinks = sinks = std::min(sinks, top);
+  }
   P.seq_row0.assign(seq_row0.begin(), seq_row0.end());
   P.has_trees = with_trees;
   if (with_trees) {
@@ -387,20 +402,20 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
       int64_t i = lo;
       while (i < hi) {
         const int64_t first = i;
-        double useful = (double)P.row_pos[(size_t)i] + 1.0, waste = 0.0;
+        double useful = (double)seen(P.row_pos[(size_t)i]), waste = 0.0;
         int32_t cnt = 1;
         ++i;
         while (i < hi && cnt < tt) {
           const double step = (double)P.row_pos[(size_t)i] - (double)P.row_pos[(size_t)(i - 1)];
           const double nw = waste + cnt * step;
-          const double nu = useful + (double)P.row_pos[(size_t)i] + 1.0;
+          const double nu = useful + (double)seen(P.row_pos[(size_t)i]);
           if (nw > kWasteFrac * nu && nw > (double)kKvStep * tt) break;
           waste = nw;
           useful = nu;
           ++cnt;
           ++i;
         }
-        const int32_t kv_hi = P.row_pos[(size_t)(first + cnt - 1)] + 1;
+        const int32_t kv_hi = axis_keys(P.row_pos[(size_t)first], P.row_pos[(size_t)(first + cnt - 1)]);
         for (int32_t g = 0; g < s.num_kv_heads; ++g) units.push_back(Unit{b, g, (int32_t)first, cnt, kv_hi});
       }
     }
@@ -827,11 +842,11 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
     }
   }
 
-  if (!with_trees) plan_weights(&P);
+  if (!with_trees && window == 0) plan_weights(&P);
 
   // figures
   const double hq = s.num_q_heads;
-  for (int64_t r = 0; r < total; ++r) P.useful_flops += 4.0 * d * hq * ((double)P.row_pos[(size_t)r] + 1);
+  for (int64_t r = 0; r < total; ++r) P.useful_flops += 4.0 * d * hq * (double)seen(P.row_pos[(size_t)r]);
   const double qo_bytes = 2.0 * 2.0 * (double)total * hq * d;  // Q read + O write, bf16
   P.planned_bytes = qo_bytes;
   for (const WorkItem& w : P.work) {
@@ -845,8 +860,22 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
     P.tile_flops += 4.0 * d * rows * (double)((w.kv_hi - w.kv_lo + gran - 1) / gran * gran);
   }
   P.min_bytes = qo_bytes;
-  for (int32_t b = 0; b < B; ++b)
-    if (seq_maxpos[b] >= 0) P.min_bytes += (double)(seq_maxpos[b] + 1) * d * 2.0 * 2.0 * Hkv;
+  for (int32_t b = 0; b < B; ++b) {
+    if (seq_maxpos[b] < 0) continue;
+    double keys = (double)seq_maxpos[b] + 1;
+    if (window > 0) {  // those in some row's window, and the sinks before them
+      int64_t first = -1, end = 0;
+      keys = 0;
+      for (int32_t k = seg_indptr[b]; k < seg_indptr[b + 1]; ++k) {
+        const int64_t lo = std::max<int64_t>(window_start(seg_start[k], window), end);
+        end = (int64_t)seg_start[k] + seg_len[k];
+        keys += (double)(end - lo);
+        if (first < 0) first = lo;
+      }
+      keys += (double)std::min<int64_t>(sinks, first);
+    }
+    P.min_bytes += keys * d * 2.0 * 2.0 * Hkv;
+  }
   return MSA_OK;
 }
 

@@ -35,6 +35,8 @@ struct HostPlan {
   std::vector<TreeSpan> trees;    // one per tree segment
   int32_t tree_rows = 0;          // rows of all trees
   int32_t max_slots = 0;          // rows of the largest one
+  int32_t window = 0;             // positions that a row sees up to its own, 0: all (plans of msa_plan_window: >= 1)
+  int32_t sinks = 0;              // first positions that every row sees, with a window
   int64_t num_tiles = 0;          // tiles x kv heads before splitting
   int64_t max_splits = 1;
   int32_t max_merge_rows = 0;     // rows (tokens x G) of the largest split tile
@@ -49,9 +51,11 @@ msa_status check_shape(const msa_shape& shape, std::string* err);
 
 // Validates the inputs and fills *out.  On error returns the status and a
 // message in *err; *out is then unspecified.  with_trees: a plan of
-// msa_plan_tree, seg_tree as there (null: every segment is a tree).
+// msa_plan_tree, seg_tree as there (null: every segment is a tree).  window:
+// 0, or that of a plan of msa_plan_window, with its sinks.
 msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const int32_t* seg_indptr,
                       const int32_t* seg_start, const int32_t* seg_len, const msa_plan_opts* opts,
-                      bool with_trees, const int32_t* seg_tree, HostPlan* out, std::string* err);
+                      bool with_trees, const int32_t* seg_tree, int32_t window, int32_t sinks, HostPlan* out,
+                      std::string* err);
 
 }  // namespace msa

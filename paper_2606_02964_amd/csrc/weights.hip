@@ -472,6 +472,7 @@ extern "C" msa_status msa_kv_weights(msa_plan_t plan, const void* q, const void*
   const auto invalid = [&](const std::string& msg) { return msa::fail(who, MSA_ERR_INVALID_ARG, msg); };
   if (!plan) return invalid("null plan");
   if (plan->hp.has_trees) return msa::fail(who, MSA_ERR_UNSUPPORTED, "the plan was built by msa_plan_tree");
+  if (plan->hp.window > 0) return msa::fail(who, MSA_ERR_UNSUPPORTED, "the plan was built by msa_plan_window");
   if (stride_seq < 0 || stride_head < 0) return invalid("strides must be >= 0");
   if (accumulate != 0 && accumulate != 1) return invalid("accumulate must be 0 or 1");
   if (plan->host_only) return invalid("plan was built with MSA_PLAN_HOST_ONLY");
