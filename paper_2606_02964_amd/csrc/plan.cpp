@@ -78,6 +78,7 @@ constexpr double kItemStepsDecode = 1.0;
 constexpr double kHomeSlack = 0.03;
 constexpr double kHomeSlackSmall = 0.15;
 constexpr double kOneRoundFactor = 1.1;  // one piece per workgroup preferred up to this times the packed load
+constexpr int64_t kFewKeys = 128;        // keys that a window and its sinks hold, up to which all weights are hi + lo
 constexpr double kCutSlack = 0.02;       // a workgroup's load over the mean before a unit is cut
 
 msa_status fail(std::string* err, msa_status st, const std::string& msg) {
@@ -376,6 +377,11 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
     for (int32_t b = 0; b < B; ++b) top = std::max(top, seq_maxpos[b] + 1);
     P.window = window = std::min(window, top);
     P.sinks = sinks = std::min(sinks, top);
+    // Rows of few keys carry all their weights as hi + lo terms.  A causal row of up to 64 does anyway, as
+    // they are in the step that holds its own position, but a window's keys start in the step before, and
+    // sinks are in another: with two keys, half the weight would be off by 2^-9.  Past 128 keys at
+    // least 64 share what is rounded, as in longer causal rows.
+    if ((int64_t)window + sinks <= kFewKeys) P.precise_weights = true;
   }
   P.seq_row0.assign(seq_row0.begin(), seq_row0.end());
   P.has_trees = with_trees;
@@ -863,16 +869,15 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
   for (int32_t b = 0; b < B; ++b) {
     if (seq_maxpos[b] < 0) continue;
     double keys = (double)seq_maxpos[b] + 1;
-    if (window > 0) {  // those in some row's window, and the sinks before them
-      int64_t first = -1, end = 0;
+    if (window > 0) {  // those in some row's window, and the sinks outside of all
+      int64_t end = 0;
       keys = 0;
       for (int32_t k = seg_indptr[b]; k < seg_indptr[b + 1]; ++k) {
         const int64_t lo = std::max<int64_t>(window_start(seg_start[k], window), end);
+        keys += (double)std::max<int64_t>(std::min<int64_t>(sinks, lo) - end, 0);
         end = (int64_t)seg_start[k] + seg_len[k];
         keys += (double)(end - lo);
-        if (first < 0) first = lo;
       }
-      keys += (double)std::min<int64_t>(sinks, first);
     }
     P.min_bytes += keys * d * 2.0 * 2.0 * Hkv;
   }

@@ -1,0 +1,238 @@
+"""Rotary positions with the cache write (msa_rope_append) against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_02964_amd as msa
+from serve_ref import BS, Layout, exponent, normal, pow2, quantise, rotate
+
+pytestmark = pytest.mark.gpu
+
+SEQS = {"one": [(1, [(0, 1)])],
+        "tokens": [(L, [(L - 1, 1)]) for L in (1, 16, 17, 33, 300)],
+        "chunks": [(100, [(3, 1), (20, 40), (64, 16)]), (50, []), (900, [(0, 29), (431, 100)]), (48, [(0, 48)])]}
+
+
+def freqs(R):
+    return torch.from_numpy(msa.msa_rope_freqs(R, 10000.0)[0]).cuda()
+
+
+def setup(seqs, heads, seed, fp8):
+    lay = Layout(SEQS[seqs], *heads, seed=seed)
+    hq, hkv, d = heads
+    qkv = normal(seed, lay.rows, hq + 2 * hkv, d)
+    if fp8:
+        k = torch.randint(0, 100, (lay.num_blocks, hkv, BS, d), dtype=torch.uint8, device="cuda")
+        v = torch.randint(0, 100, (lay.num_blocks, hkv, d, BS), dtype=torch.uint8, device="cuda")
+        ks, vs = (torch.randint(100, 140, (lay.num_blocks, hkv, BS), dtype=torch.uint8, device="cuda") for _ in range(2))
+    else:
+        k, v = normal(seed + 1, lay.num_blocks, hkv, BS, d), normal(seed + 2, lay.num_blocks, hkv, d, BS)
+        ks = vs = None
+    return lay, qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], k, v, ks, vs
+
+
+# A rotated number in 32 bits: the angle's remainder is off by 2^-25 turns (2^-22.3 radians), sine and cosine by
+# 2^-23 each, their products, the amplitude's and the sum by 2^-24 each: below 2^-21 (|x0| + |x1|) together.
+# Rounded to bf16: 2^-8 of itself more.  An angle of t radians has its own rounding in 64 bits, 2^-52 t (up to 2^31: 2^-21).
+def slack(x, freq, pairs, amplitude, far=False):
+    R = 2 * freq.shape[0]
+    m = torch.zeros_like(x, dtype=torch.float64)
+    a, b = (slice(0, R // 2), slice(R // 2, R)) if pairs == 0 else (slice(0, R, 2), slice(1, R, 2))
+    s = (x[..., a].double().abs() + x[..., b].double().abs()) * abs(amplitude) * 2.0 ** (-20 if far else -21)
+    m[..., a], m[..., b] = s, s
+    return m
+
+
+def check_bf16(got, x, pos, freq, pairs, amplitude, far=False):
+    want, far = rotate(x, pos, freq, pairs, amplitude), slack(x, freq, pairs, amplitude, far)
+    R = 2 * freq.shape[0]
+    assert torch.equal(got[..., R:], x[..., R:])
+    assert ((got.double() - want).abs() <= far + 2.0 ** -8 * want.abs()).all()
+
+
+@pytest.mark.parametrize("seqs", SEQS)
+@pytest.mark.parametrize("heads,R", [((8, 2, 128), 128), ((8, 2, 128), 16), ((32, 8, 128), 96), ((4, 4, 64), 64),
+                                     ((5, 5, 64), 32), ((15, 3, 64), 48), ((256, 1, 128), 128)], ids=str)
+@pytest.mark.parametrize("pairs", [0, 1])
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
+def test_definition(seqs, heads, R, pairs, fp8):
+    lay, q, k_new, v_new, k, v, ks, vs = setup(seqs, heads, R + pairs, fp8)
+    freq, amplitude = freqs(R), 1.25
+    before = [None if x is None else x.clone() for x in (k, v, ks, vs)]
+    q_out = torch.full((lay.rows + 1, lay.hq, lay.d), 7.0, dtype=torch.bfloat16, device="cuda")
+    msa.msa_rope_append(lay.plan(msa), msa.make_rope(freq, pairs, amplitude), q, q_out[:lay.rows], k_new, v_new, lay.table, k, v, ks, vs)
+    torch.cuda.synchronize()
+    assert (q_out[lay.rows] == 7.0).all()
+    check_bf16(q_out[:lay.rows], q, lay.pos, freq, pairs, amplitude)
+    blk, at = lay.places()
+    if not fp8:
+        check_bf16(k[blk, :, at], k_new, lay.pos, freq, pairs, amplitude)
+        assert torch.equal(v[blk, :, :, at], v_new)
+    else:
+        want, far = rotate(k_new, lay.pos, freq, pairs, amplitude), slack(k_new, freq, pairs, amplitude)
+        s = ks[blk, :, at].long() - 127
+        # next to a border the power may be the other one's; the largest number then says so
+        top = want.abs().amax(-1)
+        edge = ((top / pow2(exponent(want)) - 448.0).abs() < 1e-3) | ((top / pow2(exponent(want)) - 224.0).abs() < 1e-3)
+        assert ((s == exponent(want)) | edge).all()
+        got = k[blk, :, at].view(torch.float8_e4m3fn).double() * pow2(s)[..., None]
+        bound = torch.maximum(2.0 ** -4 * want.abs(), 2.0 ** -10 * pow2(s)[..., None])  # half a step of e4m3
+        assert ((got - want).abs() <= bound * 1.0000001 + 2 * far).all()
+        vq, vb = quantise(v_new)
+        assert torch.equal(vs[blk, :, at], vb)
+        assert torch.equal(v[blk, :, :, at].view(torch.float8_e4m3fn).double() * pow2(vb.long() - 127)[..., None], vq)
+    # nothing else is written
+    kw = torch.zeros(lay.num_blocks, BS, dtype=torch.bool, device="cuda")
+    kw[blk, at] = True
+    assert torch.equal(k.permute(0, 2, 1, 3)[~kw], before[0].permute(0, 2, 1, 3)[~kw])
+    assert torch.equal(v.permute(0, 3, 1, 2)[~kw], before[1].permute(0, 3, 1, 2)[~kw])
+    if fp8:
+        assert torch.equal(ks.permute(0, 2, 1)[~kw], before[2].permute(0, 2, 1)[~kw])
+        assert torch.equal(vs.permute(0, 2, 1)[~kw], before[3].permute(0, 2, 1)[~kw])
+
+
+@pytest.mark.parametrize("fp8", [False, True], ids=["bf16", "fp8"])
+def test_far_and_given_positions(fp8):
+    """Positions of their own, negative and up to 2^31 - 1: angles keep 64 bits."""
+    lay, q, k_new, v_new, k, v, ks, vs = setup("chunks", (8, 2, 128), 3, fp8)
+    pos = torch.randint(0, 1 << 20, (lay.rows,), dtype=torch.int32, device="cuda")
+    pos[:4] = torch.tensor([(1 << 31) - 1, -5, 0, -(1 << 31)], dtype=torch.int32)
+    freq = freqs(128)
+    q_out = torch.empty(lay.rows, 8, 128, dtype=torch.bfloat16, device="cuda")
+    msa.msa_rope_append(lay.plan(msa), msa.make_rope(freq), q, q_out, k_new, v_new, lay.table, k, v, ks, vs, pos)
+    check_bf16(q_out, q, pos, freq, 0, 1.0, far=True)
+    if not fp8:
+        blk, at = lay.places()
+        check_bf16(k[blk, :, at], k_new, pos, freq, 0, 1.0, far=True)
+
+
+def test_in_place_without_q_and_strided():
+    lay, q, k_new, v_new, k, v, _, _ = setup("chunks", (8, 2, 128), 4, False)
+    rope, plan = msa.make_rope(freqs(128), 1), lay.plan(msa)
+    q_out = torch.empty(lay.rows, 8, 128, dtype=torch.bfloat16, device="cuda")
+    msa.msa_rope_append(plan, rope, q, q_out, k_new, v_new, lay.table, k, v)
+    k1, v1 = torch.zeros_like(k), torch.zeros_like(v)
+    msa.msa_rope_append(plan, rope, None, None, k_new, v_new, lay.table, k1, v1)  # keys alone
+    blk, at = lay.places()
+    assert torch.equal(k1[blk, :, at], k[blk, :, at]) and torch.equal(v1[blk, :, :, at], v[blk, :, :, at])
+    spare = k_new.clone()
+    msa.msa_rope_append(plan, rope, q, q, k_new, v_new, lay.table, k1, v1)  # in place, inside the fused projection
+    assert torch.equal(q, q_out) and torch.equal(k_new, spare)
+
+
+def test_zero_rows_and_bad_entries():
+    lay = Layout([(40, [])], 8, 2, 128)
+    rope = msa.make_rope(freqs(128))
+    none = torch.empty(0, 8, 128, dtype=torch.bfloat16, device="cuda")
+    kv = torch.empty(0, 2, 128, dtype=torch.bfloat16, device="cuda")
+    cache = torch.zeros(lay.num_blocks, 2, BS, 128, dtype=torch.bfloat16, device="cuda")
+    msa.msa_rope_append(lay.plan(msa), rope, none, none, kv, kv, lay.table, cache, cache)
+    lay, q, k_new, v_new, k, v, ks, vs = setup("chunks", (8, 2, 128), 5, True)
+    table = lay.table.clone()
+    table[0, 0], table[2, 30] = -1, lay.num_blocks
+    q_out = torch.empty(lay.rows, 8, 128, dtype=torch.bfloat16, device="cuda")
+    before = k.clone(), v.clone(), ks.clone(), vs.clone()
+    msa.msa_rope_append(lay.plan(msa), rope, q, q_out, k_new, v_new, table, k, v, ks, vs)
+    check_bf16(q_out, q, lay.pos, freqs(128), 0, 1.0)  # q of the skipped rows too
+    for b, i in ((0, 0), (2, 30)):
+        blk = int(lay.table[b, i])
+        assert all(torch.equal(x[blk], y[blk]) for x, y in zip((k, v, ks, vs), before))
+
+
+def test_values_of_every_size():
+    """Rows of zeros, of one large number, of the smallest and the largest bf16 numbers."""
+    lay = Layout([(64, [(0, 64)])], 1, 1, 64, seed=6)
+    x = normal(7, 64, 1, 64)
+    x[0] = 0.0
+    x[1, 0, 1:] = 0.0
+    x[2] *= 2.0 ** -126
+    x[3] = 2.0 ** -133  # the smallest bf16 number
+    x[4] *= 2.0 ** 120
+    x[5, 0, 3] = 3.3895e38  # the largest
+    x[6] = 448.0
+    x[7] = 450.0
+    x[8, 0, 0] = -0.0
+    for i in range(40):
+        x[10 + i] *= 2.0 ** (i - 20)
+    k = torch.zeros(lay.num_blocks, 1, BS, 64, dtype=torch.uint8, device="cuda")
+    v = torch.zeros(lay.num_blocks, 1, 64, BS, dtype=torch.uint8, device="cuda")
+    ks, vs = (torch.zeros(lay.num_blocks, 1, BS, dtype=torch.uint8, device="cuda") for _ in range(2))
+    msa.msa_fp8_append(lay.plan(msa), x, x, lay.table, k, v, ks, vs)
+    blk, at = lay.places()
+    want, b = quantise(x)
+    assert torch.equal(ks[blk, :, at], b) and torch.equal(vs[blk, :, at], b)
+    assert int(b.min()) == 17 and int(b.max()) == 247
+    for got in (k[blk, :, at], v[blk, :, :, at]):
+        assert torch.equal(got.view(torch.float8_e4m3fn).double() * pow2(b.long() - 127)[..., None], want)
+
+
+def test_graph_and_stream():
+    lay, q, k_new, v_new, k, v, ks, vs = setup("chunks", (8, 2, 128), 8, True)
+    rope, plan = msa.make_rope(freqs(128)), lay.plan(msa)
+    q_out = torch.zeros(lay.rows, 8, 128, dtype=torch.bfloat16, device="cuda")
+    args = (plan, rope, q, q_out, k_new, v_new, lay.table, k, v, ks, vs)
+    msa.msa_rope_append(*args)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        msa.msa_rope_append(*args)
+    for seed in (1, 2, 3):
+        q.copy_(normal(seed, *q.shape))
+        k_new.copy_(normal(seed + 9, *k_new.shape))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (q_out, k, v, ks, vs)]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        msa.msa_rope_append(*args, stream=side)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (q_out, k, v, ks, vs)))
+
+
+def test_binding_refuses():
+    lay, q, k_new, v_new, k, v, ks, vs = setup("chunks", (8, 2, 128), 9, True)
+    rope, plan = msa.make_rope(freqs(128)), lay.plan(msa)
+    q_out = torch.empty(lay.rows, 8, 128, dtype=torch.bfloat16, device="cuda")
+
+    def refused(text, status=msa.MSA_ERR_INVALID_ARG, **kw):
+        a = dict(rope=rope, q=q, q_out=q_out, k_new=k_new, v_new=v_new, block_table=lay.table, k_cache=k, v_cache=v, k_scale=ks, v_scale=vs)
+        a.update(kw)
+        with pytest.raises(msa.MsaError, match=text) as e:
+            msa.msa_rope_append(plan, **a)
+        assert e.value.status == status
+    refused("q has shape", q=q[1:])
+    refused("q_out has shape", q_out=q_out[:, :4])
+    refused("k_new has shape", k_new=k_new[..., :64])
+    refused("v_new has type", v_new=v_new.float())
+    refused("not contiguous along", q=torch.empty(lay.rows, 8, 256, dtype=torch.bfloat16, device="cuda")[..., ::2])
+    refused("strides must be positive multiples of 8", q=torch.empty(lay.rows, 8, 132, dtype=torch.bfloat16, device="cuda")[..., :128])
+    refused("16-byte aligned", v_new=torch.empty(lay.rows * 256 + 8, dtype=torch.bfloat16, device="cuda")[4:4 + lay.rows * 256].view(lay.rows, 2, 128))
+    refused("go together", k_scale=None)
+    refused("k_cache has type", k_cache=torch.zeros(9, device="cuda"))
+    refused("k_cache has type", k_scale=None, v_scale=None)  # bytes where a bf16 cache is taken
+    refused("k_scale has", k_scale=ks[:-1])
+    refused("positions has type", positions=lay.pos)
+    refused("positions has", positions=torch.zeros(lay.rows - 1, dtype=torch.int32, device="cuda"))
+    refused("block_table", block_table=lay.table.cpu())
+    refused("null is not|must be non-null", q_out=None)
+    refused("is not an msa_rope", rope=None)
+    for field, value, text, st in (("rotary_dim", 130, "rotary_dim", 1), ("rotary_dim", 24, "multiple of 16", 2), ("rotary_dim", 0, "rotary_dim", 1),
+                                   ("pairs", 2, "pairs", 1), ("reserved", 1, "reserved", 1), ("amplitude", float("nan"), "amplitude", 1),
+                                   ("inv_freq", None, "non-null", 1)):
+        r = msa.make_rope(freqs(128))
+        setattr(r, field, value)
+        refused(text, st, rope=r)
+    with pytest.raises(msa.MsaError, match="inv_freq"):
+        msa.make_rope(freqs(128).float())
+    with pytest.raises(msa.MsaError, match="inv_freq"):
+        msa.make_rope(freqs(128).cpu())
+
+
+def test_frequencies_on_the_card():
+    """A stretched table as msa_rope_freqs gives it, used as it comes."""
+    f, a = msa.msa_rope_freqs(128, 500000.0, msa.MSA_ROPE_SCALE_PAIRS, 8.0, 8192.0, 1.0, 32.0)
+    lay, q, k_new, v_new, k, v, _, _ = setup("tokens", (8, 2, 128), 10, False)
+    freq = torch.from_numpy(np.asarray(f)).cuda()
+    q_out = torch.empty(lay.rows, 8, 128, dtype=torch.bfloat16, device="cuda")
+    msa.msa_rope_append(lay.plan(msa), msa.make_rope(freq, 0, a), q, q_out, k_new, v_new, lay.table, k, v)
+    check_bf16(q_out, q, lay.pos, freq, 0, a)

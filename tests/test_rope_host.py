@@ -1,0 +1,99 @@
+"""Frequency tables of rotary positions, and what the calls refuse, on the host."""
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+
+import paper_2606_02964_amd as msa
+
+INCLUDE = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+
+
+@pytest.mark.parametrize("header,names", [("msa_rope.h", msa.EXPORTED_ROPE), ("msa_fp8.h", msa.EXPORTED_FP8)])
+def test_names(header, names):
+    text = open(os.path.join(INCLUDE, header)).read()
+    assert set(re.findall(r"^msa_status (msa_\w+)\(", text, re.M)) == set(names)
+
+
+def plain(R, base):
+    return np.array([base ** (-2.0 * i / R) for i in range(R // 2)])
+
+
+@pytest.mark.parametrize("R,base", [(2, 10000.0), (16, 10000.0), (128, 500000.0), (96, 1e6)])
+def test_kinds(R, base):
+    f = plain(R, base)
+    close = dict(rtol=1e-14, atol=0)  # a power in 64 bits, and a few products
+    got, a = msa.msa_rope_freqs(R, base)
+    assert got.dtype == np.float64 and got.shape == (R // 2,) and a == 1.0
+    np.testing.assert_allclose(got, f, **close)
+    np.testing.assert_allclose(msa.msa_rope_freqs(R, base, msa.MSA_ROPE_SCALE_LINEAR, 4.0)[0], f / 4.0, **close)
+    if R > 2:
+        got = msa.msa_rope_freqs(R, base, msa.MSA_ROPE_SCALE_BASE, 4.0)[0]
+        np.testing.assert_allclose(got, plain(R, base * 4.0 ** (R / (R - 2))), **close)
+        np.testing.assert_allclose((got[0], got[-1]), (1.0, f[-1] / 4.0), rtol=1e-13)
+    got, a = msa.msa_rope_freqs(R, base, msa.MSA_ROPE_SCALE_TURNS, 8.0, 8192.0, 1.0, 4.0)
+    assert a == 1.0
+    for i, x in enumerate(f):
+        turns = 8192.0 * x / (2 * math.pi)
+        s = min(1.0, max(0.0, (turns - 1.0) / 3.0))
+        assert got[i] == pytest.approx(s * x + (1 - s) * x / 8.0, rel=1e-13)
+    got, a = msa.msa_rope_freqs(R, base, msa.MSA_ROPE_SCALE_PAIRS, 16.0, 4096.0, 1.0, 32.0)
+    assert a == np.float32(0.1 * math.log(16.0) + 1.0)
+    pair = lambda n: R * math.log(4096.0 / (2 * math.pi * n)) / (2 * math.log(base))  # noqa: E731
+    lo, hi = max(math.floor(pair(32.0)), 0), min(math.ceil(pair(1.0)), R - 1)
+    hi = hi if hi > lo else lo + 0.001
+    for i, x in enumerate(f):
+        s = 1.0 - min(1.0, max(0.0, (i - lo) / (hi - lo)))
+        assert got[i] == pytest.approx(s * x + (1 - s) * x / 16.0, rel=1e-13)
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(rotary_dim=0), "rotary_dim"), (dict(rotary_dim=7), "rotary_dim"), (dict(rotary_dim=-2), "rotary_dim"), (dict(kind=9), "kind"),
+    (dict(base=0.0), "base"), (dict(base=float("nan")), "base"), (dict(kind=1, factor=0.0), "factor"), (dict(kind=1, factor=float("inf")), "factor"),
+    (dict(kind=2, rotary_dim=2, factor=2.0), "rotary_dim > 2"), (dict(kind=3, factor=2.0), "original_len"),
+    (dict(kind=3, factor=2.0, original_len=10.0, low=4.0, high=4.0), "low < high"), (dict(kind=4, factor=2.0, original_len=10.0, low=0.0, high=4.0), "kind PAIRS"),
+    (dict(kind=4, factor=2.0, original_len=10.0, base=1.0), "kind PAIRS"), (dict(rotary_dim=1 << 31), "32 bits")])
+def test_freqs_refuse(kw, text):
+    with pytest.raises(msa.MsaError, match=text) as e:
+        msa.msa_rope_freqs(**dict(dict(rotary_dim=64), **kw))
+    assert e.value.status == msa.MSA_ERR_INVALID_ARG
+
+
+def test_calls_refuse_before_the_device():
+    """Integer addresses that are never read: every call ends in a check."""
+    P, SHAPE = 4096, msa.make_shape(1, 8, 2, 128, 100, 100, 0.1)
+    plan = msa.msa_plan(SHAPE, [50], [0, 1], [3], [9], flags=msa.MSA_PLAN_HOST_ONLY)
+    rope = msa.msa_rope(P, 128, 0, 1.0, 0)
+    with pytest.raises(msa.MsaError, match="HOST_ONLY"):
+        msa.msa_rope_append(plan, rope, P, P, P, P, P, P, P)
+    with pytest.raises(msa.MsaError, match="HOST_ONLY"):
+        msa.msa_fp8_append(plan, P, P, P, P, P, P, P)
+    with pytest.raises(msa.MsaError, match="HOST_ONLY"):
+        msa.msa_fp8_forward(plan, P, P, P, P, P, P, P)
+    with pytest.raises(msa.MsaError, match="non-null"):
+        msa.msa_fp8_append(plan, P, P, P, P, P, None, None)
+
+    def read(shape=SHAPE, to=SHAPE, max_len=50, end=P, **kw):
+        a = dict(start=None, end=end, max_len=max_len, block_table=P, k_cache=P, v_cache=P, k_scale=P, v_scale=P, to=to, to_table=P, k_out=P, v_out=P)
+        a.update(kw)
+        msa.msa_fp8_read(shape, **a)
+
+    def refused(text, **kw):
+        with pytest.raises(msa.MsaError, match=text) as e:
+            read(**kw)
+        return e.value.status
+    assert refused("max_len", max_len=-1) == msa.MSA_ERR_INVALID_ARG
+    refused("32 bits", max_len=1 << 31)
+    refused("must agree", to=msa.make_shape(1, 8, 4, 128, 100, 100, 0.1))
+    refused("must agree", to=msa.make_shape(2, 8, 2, 128, 100, 100, 0.1))
+    refused("must agree", to=msa.make_shape(1, 8, 2, 64, 100, 100, 0.1))
+    refused("multiples of 16", shape=msa.make_shape(1, 8, 2, 128, 100, 100, 0.1, k_strides=(4096, 2048, 136)))
+    refused("non-null", end=None)
+    refused("non-null", k_scale=None)
+    refused("16-byte", k_out=P + 8)
+    refused("4-byte", to_table=P + 2)
+    big = msa.make_shape(1 << 20, 8, 2, 128, 1000, 1000, 0.1)
+    assert refused("2\\^23", shape=big, to=big, max_len=16000) == msa.MSA_ERR_UNSUPPORTED
+    read(max_len=0)  # nothing to do

@@ -1,0 +1,119 @@
+"""Plans of msa_plan_window on the host: which keys and blocks the work items cover, the figures,
+and the refusals."""
+import os
+import random
+import re
+
+import numpy as np
+import pytest
+
+import paper_2606_02964_amd as msa
+
+HOST = msa.MSA_PLAN_HOST_ONLY
+INCLUDE = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+
+
+def test_names():
+    text = open(os.path.join(INCLUDE, "msa_window.h")).read()
+    assert set(re.findall(r"^msa_status (msa_\w+)\(", text, re.M)) == set(msa.EXPORTED_WINDOW)
+
+
+def seen(p, window, sinks):
+    return set(range(max(0, p - window + 1), p + 1)) | set(range(min(sinks, p + 1)))
+
+
+def random_layout(r):
+    lens, indptr, start, length = [], [0], [], []
+    for _ in range(r.randint(1, 4)):
+        at = r.choice((0, 0, 1, 17, 300, 2000))
+        for _ in range(r.randint(0, 3)):
+            n = r.choice((1, 1, 2, 16, 63, 64, 65, 200))
+            start.append(at)
+            length.append(n)
+            at += n + r.choice((0, 1, 40, 700))
+        lens.append(at + r.randint(0, 5))
+        indptr.append(len(start))
+    return lens, indptr, start, length
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_items_cover_what_rows_see(seed):
+    r = random.Random(seed)
+    for _ in range(12):
+        lens, indptr, start, length = random_layout(r)
+        hq, hkv, d = r.choice(((8, 2, 128), (4, 4, 64), (64, 1, 64), (32, 8, 128)))
+        window, sinks = r.choice((1, 2, 40, 64, 100, 700, 5000)), r.choice((0, 1, 4, 64, 65, 130, 9000))
+        blocks = max([1] + [-(-x // 16) for x in lens])
+        shape = msa.make_shape(len(lens), hq, hkv, d, blocks, max(1, blocks * len(lens)), 0.1)
+        split = r.choice((0, 0, 64, 128))
+        plan = msa.msa_plan_window(shape, lens, indptr, start, length, window, sinks, kv_split_tokens=split, flags=HOST)
+        pos, work, merge = msa.msa_plan_export(plan)
+        covered = {}
+        for seq, g, row0, nrows, lo, hi, slot, wg in work.tolist():
+            first = max(0, int(pos[row0]) - window + 1)
+            head = -(-sinks // 64) * 64
+            skip = max(0, first // 64 * 64 - head)
+            keys = {v if v < head else v + skip for v in range(lo, hi)}
+            assert lo % 64 == 0 and hi > lo
+            for row in range(row0, row0 + nrows):
+                mine = keys & seen(int(pos[row]), window, sinks)
+                at = covered.setdefault((row, g), set())
+                assert not at & mine
+                at |= mine
+        for row in range(len(pos)):
+            for g in range(hkv):
+                assert covered[row, g] == seen(int(pos[row]), window, sinks)
+        flops = sum(len(seen(int(p), window, sinks)) for p in pos) * 4.0 * d * hq
+        info = plan.info()
+        assert info["useful_flops"] == flops
+        keys = sum(len(set().union(*[seen(p, window, sinks) for k in range(indptr[b], indptr[b + 1])
+                                     for p in range(start[k], start[k] + length[k])] or [set()]))
+                   for b in range(len(lens)))
+        assert info["min_bytes"] == 4.0 * len(pos) * hq * d + 4.0 * keys * d * hkv
+
+
+def test_short_windows_make_short_plans():
+    shape = msa.make_shape(4, 32, 8, 128, 8192, 4 * 8192, 0.1)
+    layout = ([131072] * 4, [0, 1, 2, 3, 4], [131071] * 4, [1] * 4)
+    full = msa.msa_plan(shape, *layout, flags=HOST).info()
+    part = msa.msa_plan_window(shape, *layout, 1000, 4, flags=HOST).info()
+    assert part["planned_bytes"] < full["planned_bytes"] / 100
+
+
+def test_wide_window_is_the_causal_plan():
+    r = random.Random(5)
+    for _ in range(20):
+        lens, indptr, start, length = random_layout(r)
+        blocks = max([1] + [-(-x // 16) for x in lens])
+        shape = msa.make_shape(len(lens), 8, 2, 128, blocks, max(1, blocks * len(lens)), 0.1)
+        a = msa.msa_plan_export(msa.msa_plan(shape, lens, indptr, start, length, flags=HOST))
+        b = msa.msa_plan_export(msa.msa_plan_window(shape, lens, indptr, start, length, max(lens) + 1, 3, flags=HOST))
+        assert all(np.array_equal(x, y) for x, y in zip(a, b))
+
+
+def test_check_block_table():
+    shape = msa.make_shape(1, 8, 2, 128, 100, 100, 0.1)
+    plan = msa.msa_plan_window(shape, [1600], [0, 2], [1000, 1500], [10, 100], 50, 20, flags=HOST)
+    table = np.arange(100, dtype=np.int32)[None, :].copy()
+    table[0, 2:59] = -1  # behind the sinks (blocks 0, 1), before the first row's window (951, in block 59)
+    msa.msa_check_block_table(plan, table)
+    for bad in (0, 1, 59, 75, 99):
+        t = table.copy()
+        t[0, bad] = 100
+        with pytest.raises(msa.MsaError, match=f"logical block {bad} "):
+            msa.msa_check_block_table(plan, t)
+    # rows without the sinks' second block
+    plan = msa.msa_plan_window(shape, [1600], [0, 1], [3], [4], 2, 20, flags=HOST)
+    table[0, 1:] = -1
+    msa.msa_check_block_table(plan, table)
+
+
+def test_refusals():
+    shape = msa.make_shape(1, 8, 2, 128, 100, 100, 0.1)
+    for window, sinks, text in ((0, 0, "window"), (-1, 0, "window"), (1, -1, "sinks"), (1 << 31, 0, "32 bits"), (1, 1 << 31, "32 bits")):
+        with pytest.raises(msa.MsaError, match=text) as e:
+            msa.msa_plan_window(shape, [1600], [0, 1], [3], [4], window, sinks, flags=HOST)
+        assert e.value.status == msa.MSA_ERR_INVALID_ARG
+    with pytest.raises(msa.MsaError, match="past seq_kv_len"):
+        msa.msa_plan_window(shape, [1600], [0, 1], [1599], [4], 5, 0, flags=HOST)
+    assert msa.msa_plan_window(shape, [0], [0, 0], [], [], 5, 0, flags=HOST).info()["num_work"] == 0
