@@ -432,25 +432,34 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   };
   auto has = [&](int s) { return w.kv_lo + bslot * kBlockSize + s * kKvStep < w.kv_hi; };  // a block of step s
   // (a block at or past kv_hi is not read, as above)
+  uint4 raw_k[kMine], raw_v[kMine];
+  auto read_raw = [&]() __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      raw_k[i] = *reinterpret_cast<const uint4*>(raw + piece(i) * 1024 + lane * 16);
+      raw_v[i] = *reinterpret_cast<const uint4*>(raw + (kPieces + piece(i)) * 1024 + lane * 16);
+    }
+  };
+  auto turn_k = [&](int s, int i) __attribute__((always_inline)) {
+    if (takes_k && has(s)) put_k(s, i, raw_k[i], ksc[i]);
+  };
+  auto turn_v = [&](int s, int i) __attribute__((always_inline)) {
+    if (!takes_v || s >= n) return;
+    if (has(s)) {
+      put_v(s, i, raw_v[i], vsc);
+    } else {
+      char* to = vbuf(s) + bslot * T::kPage + piece(i) * 2048 + lane * 32;
+      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<uint4*>(to + 16) = make_uint4(0, 0, 0, 0);
+    }
+  };
   auto convert = [&](int sk, int sv) __attribute__((always_inline)) {
     if (kHelp && !copier) return;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if (takes_k && has(sk)) {
+    read_raw();
 #pragma unroll
-      for (int i = 0; i < kMine; ++i)
-        put_k(sk, i, *reinterpret_cast<const uint4*>(raw + piece(i) * 1024 + lane * 16), ksc[i]);
-    }
-    if (takes_v && sv < n) {
+    for (int i = 0; i < kMine; ++i) turn_k(sk, i);
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        if (has(sv)) {
-          put_v(sv, i, *reinterpret_cast<const uint4*>(raw + (kPieces + piece(i)) * 1024 + lane * 16), vsc);
-        } else {
-          char* to = vbuf(sv) + bslot * T::kPage + piece(i) * 2048 + lane * 32;
-          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<uint4*>(to + 16) = make_uint4(0, 0, 0, 0);
-        }
-      }
-    }
+    for (int i = 0; i < kMine; ++i) turn_v(sv, i);
   };
   auto fetch = [&](int sk, int sv) __attribute__((always_inline)) {
     if (kHelp && !copier) return;
@@ -469,11 +478,6 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   };
   // copies of iteration j, both steps whole
   auto copy_whole = [&](int j) __attribute__((always_inline)) {
-    if constexpr (kFp8) {
-      convert(j + 2, j + 1);
-      fetch(j + 3, j + 2);
-      return;
-    }
     if (!copier) return;
     copy_k(kpage, j + 2);
     copy_v(vpage, j + 1);
@@ -676,7 +680,8 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   // meanwhile).  Against unpipelined steps with a second pass over V: the
   // 8 x 8192 workload 2042 -> 1947 us, 32-token segments at 4K 1510 -> 1408 us;
   // at d = 64, where vector instructions bound the step, 299 -> 298 us.
-  auto fused = [&](auto bsel, auto&& addresses) {
+  // beside(i) runs behind MFMA i of block 2.
+  auto fused = [&](auto bsel, auto&& beside) {
     constexpr int B = decltype(bsel)::value, NB = 1 - B;
     const float nm = m_ref == -__builtin_inff() ? 0.0f : -m_ref;
     uint32_t pk[16];
@@ -767,7 +772,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
 #pragma unroll
         for (int e = i * kElPerPv; e < (i + 1) * kElPerPv; ++e) mx = fmaxf(mx, sbuf[NB][e >> 4][e & 15]);
       }
-      if (i == 0) addresses();
+      beside(i);
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (kPrecise) move_reference(mx);
@@ -929,6 +934,25 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
       if (need_mask(jj + 1)) mask_plain(0, jj + 1);
     }
   };
+  // What a pipelined step j does beside its PV MFMAs: the page addresses of the next copies and, for an
+  // 8-bit cache, the whole of its turning and copying (its vector work is what the MFMAs leave room for).
+  auto beside = [&](int jj) {
+    return [&, jj]([[maybe_unused]] int i) __attribute__((always_inline)) {
+      (void)jj;
+      if constexpr (!kFp8) {
+        if (i == 0) next_pages(jj + kLead);
+      } else if constexpr (!kHelp) {
+        if (i == 0) read_raw();
+#pragma unroll
+        for (int u = 0; u < kMine; ++u) {
+          if (i == 1 + u) turn_k(jj + 2, u);
+          if (i == 3 + u * (kPv / 4)) turn_v(jj + 1, u);
+        }
+        if (i == kPv - 2) fetch(jj + 3, jj + 2);
+        if (i == kPv - 1) next_pages(jj + kLead);
+      }
+    };
+  };
   // One step without overlap; waves past their last step still copy.
   auto step = [&](int jj) __attribute__((always_inline)) {
     copy_any(kpage, jj + 2, vpage, jj + 1);
@@ -941,41 +965,53 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
     tail();
   };
   int j = 0;
-  if constexpr (P::kWindow) {
-    // the steps that hold a hidden key before some row's window (an even number: the paired loop
-    // takes its ring stages from that), and those of the sinks before them
+  // Keys before a window are masked behind the pipelined step that takes their scores; with precise
+  // weights, which take a row max there, the steps that hold any run without overlap (an even number:
+  // the paired loop takes its ring stages from that), and those of the sinks before them.
+  auto mask_window = [&](int b, int jj) {
+    if constexpr (P::kWindow && !kPrecise) {
+      if (before_window(p, axis.key(w.kv_lo + jj * kKvStep), kKvStep, pmax)) mask_plain(b, jj);
+    }
+  };
+  if constexpr (P::kWindow && kPrecise) {
     const int hidden = pmax - p.window;  // the last such key
     const int v = hidden >= axis.head + axis.skip ? axis.at(hidden) : min(hidden, axis.head - 1);
     const int lead = v < w.kv_lo ? 0 : ((v - w.kv_lo) / kKvStep + 2) & ~1;
     for (; j < lead && j < n; ++j) step(j);
   }
   const int whole = (w.kv_hi - w.kv_lo) / kKvStep;  // steps without a missing block
-  for (; j + 2 < nw && !need_mask(j + 2); j += 2) {
-    copy_whole(j);  // step j+2 is not masked, hence whole
+  for (; j + 2 < nw && !past_first(j + 2); j += 2) {
+    if constexpr (!kFp8) copy_whole(j);  // step j+2 is not masked, hence whole
     if constexpr (kFp8) move_ids(j + 4);  // (an odd step is none that ids move in at)
-    fused(std::integral_constant<int, 0>{}, [&]() { next_pages(j + kLead); });
+    fused(std::integral_constant<int, 0>{}, beside(j));
+    mask_window(1, j + 1);
     tail();
-    if (j + 3 < whole) copy_whole(j + 1);
-    else copy_any(kpage, j + 3, vpage, j + 2);
-    if constexpr (!kFp8) move_ids(j + 4);
-    fused(std::integral_constant<int, 1>{}, [&]() { next_pages(j + 1 + kLead); });
+    if constexpr (!kFp8) {
+      if (j + 3 < whole) copy_whole(j + 1);
+      else copy_any(kpage, j + 3, vpage, j + 2);
+      move_ids(j + 4);
+    }
+    fused(std::integral_constant<int, 1>{}, beside(j + 1));
+    mask_window(0, j + 2);
     tail();
   }
   // One or two steps without a mask may remain before the diagonal ones: the
   // same, with the next step's mask after its scores.  (With precise weights
   // the pipelined step takes the next step's row max, so that one must need no
   // mask either.)  A 3-step item of a helped workgroup 9.9 -> 8.9 us.
-  if (j + 1 < nw && !need_mask(kPrecise ? j + 1 : j)) {
-    copy_any(kpage, j + 2, vpage, j + 1);
+  if (j + 1 < nw && !past_first(kPrecise ? j + 1 : j)) {
     if constexpr (kFp8) move_ids(j + 4);
-    fused(std::integral_constant<int, 0>{}, [&]() { next_pages(j + kLead); });
+    else copy_any(kpage, j + 2, vpage, j + 1);
+    fused(std::integral_constant<int, 0>{}, beside(j));
     if (!kPrecise && need_mask(j + 1)) mask_plain(1, j + 1);
     tail();
     ++j;
-    if (!kPrecise && j + 1 < nw && !need_mask(j)) {
-      copy_any(kpage, j + 2, vpage, j + 1);
-      if constexpr (!kFp8) move_ids(j + 3);
-      fused(std::integral_constant<int, 1>{}, [&]() { next_pages(j + kLead); });
+    if (!kPrecise && j + 1 < nw && !past_first(j)) {
+      if constexpr (!kFp8) {
+        copy_any(kpage, j + 2, vpage, j + 1);
+        move_ids(j + 3);
+      }
+      fused(std::integral_constant<int, 1>{}, beside(j));
       if (need_mask(j + 1)) mask_plain(0, j + 1);
       tail();
       ++j;

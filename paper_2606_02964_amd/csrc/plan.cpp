@@ -62,6 +62,10 @@ constexpr int64_t kWideMinTiles64 = 1024;  // narrow tiles, head_dim 64
 // takes a whole workgroup's step however wide (45 of 60 sequences decoding:
 // fill 0.82 1296 / 1313, 0.57 566 / 621; 24 of 32: 0.94 1645 / 1605)
 constexpr double kWideMinFill = 0.9;
+// ... and, with a window, the steps of a tile: short tiles' start and end, 8.5 us of a workgroup, run beside
+// another's steps where a CU has two (windows of 200 keys 804 / 717, 512 633 / 625, 1024 916 / 941, 2048
+// 1401 / 1419 as wide / narrow; 4 prompts of 6000, 64 heads)
+constexpr double kWideMinUnitSteps = 16.0;
 constexpr double kWasteFrac = 0.125;     // masked keys allowed per tile, relative
 constexpr int64_t kMinSplitKeys = 1024;  // never split below this many keys
 constexpr int64_t kMinSplitSteps = kMinSplitKeys / kKvStep;
@@ -468,6 +472,7 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
         else if (steps >= (late ? kWideMinStepsPerSlot64 : kWideMinStepsPerSlot) * 2.0 * kCUs &&
                  (given || row_steps >= kWideMinFill * steps * narrow_tokens) &&
                  (!late || (int64_t)narrow_units.size() >= kWideMinTiles64) &&
+                 (window == 0 || steps >= kWideMinUnitSteps * (double)narrow_units.size()) &&
                  (!(o.flags & MSA_PLAN_NO_AUTO_SPLIT) || (int64_t)narrow_units.size() > kCUs))
           rows = kTileRowsWide;
       }

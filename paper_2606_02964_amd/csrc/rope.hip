@@ -19,6 +19,7 @@
 // Bound by HBM: each number is read once and written once.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -57,6 +58,7 @@ struct RopeParams {
   int32_t num_blocks;
   int32_t half;         // pairs of a head: rotary_dim / 2
   int32_t head_groups;  // workgroups that share a slice's heads
+  int32_t total_q;      // rows of all slices (launch_rope's choice of head_groups)
   float amplitude;
 };
 
@@ -282,9 +284,17 @@ __global__ __launch_bounds__(256) void msa_rope_kernel(RopeParams p) {
 
 template <int D>
 int launch_rope(RopeParams p, int pairs, bool fp8, int num_items, hipStream_t s) {
-  const int passes = p.num_kv_heads / 2 + p.num_kv_heads % 2;
-  const int most = (1 << 23) / num_items;
-  p.head_groups = most < 1 ? 1 : passes <= most ? passes : most;
+  // Workgroups that share a slice's heads: four passes each, since a workgroup's look-ups and angles cost as much as a
+  // pass, but some 1024 in all where there is work for a pass each (32 query, 8 KV heads, d = 128, bf16, us, with
+  // two KV heads and their queries each / by this rule: 1 row of 512 sequences 13.0 / 10.2, of 2048 46.4 / 33.3; 1024 rows
+  // of 8 47.2 / 46.9; into 8 bits 13.7 / 9.5, 44.3 / 23.6, 42.1 / 46; d = 64, 16 heads: 2048 rows 64 / 23).
+  // (Stores past the caches take a twentieth off this launch, and add as much to the attention behind it,
+  // which then finds no q in them: 8 x 1024 rows 44.5 / 46.9, with msa_forward 225.3 / 223.2.)
+  const int64_t passes = ((int64_t)p.total_q * (p.num_q_heads + p.num_kv_heads) * (D / 16) / num_items + 255) / 256;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>((1 << 23) / num_items, p.num_kv_heads));
+  const int64_t groups = std::max<int64_t>(passes / 4, std::min<int64_t>(passes, 1024 / num_items));
+  p.head_groups = (int32_t)std::max<int64_t>(1, std::min(groups, most));
+  while (p.num_kv_heads % p.head_groups != 0) --p.head_groups;  // as many each (8 heads of 8 x 1024 rows, 8 bits: in 5 parts 46 us)
   const dim3 grid((uint32_t)num_items * (uint32_t)p.head_groups), block(256);
   if (fp8) {
     if (pairs == kNoPairs) hipLaunchKernelGGL((msa_rope_kernel<D, kNoPairs, true>), grid, block, 0, s, p);
@@ -361,6 +371,7 @@ msa_status write_rows(const char* who, msa_plan_t plan, const msa_rope* rope, co
   p.num_kv_heads = s.num_kv_heads;
   p.max_blocks = s.max_blocks_per_seq;
   p.num_blocks = s.num_blocks;
+  p.total_q = (int32_t)hp.total_q;
   int pairs = kNoPairs;
   if (rope) {
     p.inv_freq = rope->inv_freq;
