@@ -341,8 +341,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   // values: those keys are masked by selection, so never meet arithmetic).
   const bool copier = wave >= 4 || (W == 4 && !kHelp);  // wave-uniform
   const char *kpage, *vpage;  // pages of the next copies
-  const uint8_t *kspage, *vspage;  // 8-bit caches: their powers of two
-  int32_t id_cur = 0;
+  int32_t id_cur = 0, id_last = 0;
   // Reads the ids of K step s and V step s - 1 and takes their page
   // addresses; called for s = 0, 1, 2, ... in turn, one iteration before the
   // copies, where the address arithmetic runs beside MFMAs.  (Taken at the
@@ -352,16 +351,15 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   auto next_pages = [&](int s) __attribute__((always_inline)) {
     const int32_t id_prev = id_cur;
     id_cur = __builtin_amdgcn_readlane(idv, s & 63);
+    if constexpr (kFp8) {  // (8-bit caches: the addresses follow at the copies, which are beside MFMAs themselves)
+      id_last = id_prev;
+      return;
+    }
     // pinned to scalar registers here: left to itself the compiler moves the
     // products to the copies and spills 130 vector registers
     kpage = kbase + (int64_t)id_cur * ksb;
     vpage = vbase + (int64_t)id_prev * vsb;
     asm volatile("" : "+s"(kpage), "+s"(vpage));
-    if constexpr (kFp8) {
-      kspage = p.k_scale + ((int64_t)id_cur * p.num_kv_heads + w.kv_head) * kBlockSize;
-      vspage = p.v_scale + ((int64_t)id_prev * p.num_kv_heads + w.kv_head) * kBlockSize;
-      asm volatile("" : "+s"(kspage), "+s"(vspage));
-    }
   };
   // before next_pages(s) at multiples of 64: the next 64 ids move in
   auto move_ids = [&](int s) __attribute__((always_inline)) {
@@ -407,7 +405,9 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   }
   // chunk i of a page of step s into the ring
   auto put_k = [&](int s, int i, const uint4& x, uint32_t scale) __attribute__((always_inline)) {
-    const int t = k_token(i), c = 2 * (lane % (D / 16));
+    int l = lane;
+    if (D == 128) asm volatile("" : "+v"(l));  // (the places in LDS are worked out anew: no registers are left to keep them)
+    const int t = (piece(i) * 64 + l) / (D / 16), c = 2 * (l % (D / 16));
     char* to = kbuf(s) + bslot * T::kPage + t * (2 * D);
     const float f = __uint_as_float(scale << 23);
     *reinterpret_cast<uint4*>(to + ((c ^ kswz(t)) * 16)) = make_uint4(
@@ -416,7 +416,9 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
         fp8_pair<false>(x.z, f), fp8_pair<true>(x.z, f), fp8_pair<false>(x.w, f), fp8_pair<true>(x.w, f));
   };
   auto put_v = [&](int s, int i, const uint4& x, uint32_t scales) __attribute__((always_inline)) {
-    const int c = piece(i) * 64 + lane;
+    int l = lane;
+    if (D == 128) asm volatile("" : "+v"(l));
+    const int c = piece(i) * 64 + l;
     char* to = vbuf(s) + bslot * T::kPage + c * 32;
     const uint32_t u[4] = {x.x, x.y, x.z, x.w};
     uint32_t y[8];
@@ -432,48 +434,51 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   };
   auto has = [&](int s) { return w.kv_lo + bslot * kBlockSize + s * kKvStep < w.kv_hi; };  // a block of step s
   // (a block at or past kv_hi is not read, as above)
-  uint4 raw_k[kMine], raw_v[kMine];
-  auto read_raw = [&]() __attribute__((always_inline)) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      raw_k[i] = *reinterpret_cast<const uint4*>(raw + piece(i) * 1024 + lane * 16);
-      raw_v[i] = *reinterpret_cast<const uint4*>(raw + (kPieces + piece(i)) * 1024 + lane * 16);
-    }
+  auto raw_chunk = [&](int t) {
+    int l = lane;
+    if (D == 128) asm volatile("" : "+v"(l));
+    return *reinterpret_cast<const uint4*>(raw + (t & 1 ? kPieces + piece(t / 2) : piece(t / 2)) * 1024 + l * 16);
   };
-  auto turn_k = [&](int s, int i) __attribute__((always_inline)) {
-    if (takes_k && has(s)) put_k(s, i, raw_k[i], ksc[i]);
-  };
-  auto turn_v = [&](int s, int i) __attribute__((always_inline)) {
-    if (!takes_v || s >= n) return;
-    if (has(s)) {
-      put_v(s, i, raw_v[i], vsc);
-    } else {
-      char* to = vbuf(s) + bslot * T::kPage + piece(i) * 2048 + lane * 32;
-      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<uint4*>(to + 16) = make_uint4(0, 0, 0, 0);
+  // chunk t of what is in raw into the rings: even t K of step sk, odd t V of step sv
+  auto turn = [&](int t, int sk, int sv, const uint4& x) __attribute__((always_inline)) {
+    const int i = t / 2;
+    if (t % 2 == 0) {
+      if (takes_k && has(sk)) put_k(sk, i, x, ksc[i]);
+    } else if (takes_v && sv < n) {
+      if (has(sv)) {
+        put_v(sv, i, x, vsc);
+      } else {
+        char* to = vbuf(sv) + bslot * T::kPage + piece(i) * 2048 + lane * 32;
+        *reinterpret_cast<uint4*>(to) = *reinterpret_cast<uint4*>(to + 16) = make_uint4(0, 0, 0, 0);
+      }
     }
   };
   auto convert = [&](int sk, int sv) __attribute__((always_inline)) {
-    if (kHelp && !copier) return;
-    read_raw();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) turn_k(sk, i);
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) turn_v(sv, i);
+    for (int t = 0; t < 2 * kMine; ++t) turn(t, sk, sv, raw_chunk(t));
   };
+  auto powers = [&](const uint8_t* base, int32_t id) {  // of a block
+    if constexpr (kFp8) base += ((int64_t)id * p.num_kv_heads + w.kv_head) * kBlockSize;
+    return base;
+  };
+  // copies of the last next_pages(sk): K of step sk, V of step sv = sk - 1
   auto fetch = [&](int sk, int sv) __attribute__((always_inline)) {
-    if (kHelp && !copier) return;
-    if (takes_k && has(sk)) {
+    if constexpr (kFp8) {
+      int l = lane;
+      if (D == 128) asm volatile("" : "+v"(l));
+      if (takes_k && has(sk)) {
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        dma16(kpage, kgo8[i], raw + piece(i) * 1024);
-        ksc[i] = kspage[k_token(i)];
+        for (int i = 0; i < kMine; ++i) {
+          dma16(kbase + (int64_t)id_cur * ksb, kgo8[i], raw + piece(i) * 1024);
+          ksc[i] = powers(p.k_scale, id_cur)[(piece(i) * 64 + l) / (D / 16)];
+        }
       }
-    }
-    if (takes_v && has(sv)) {
+      if (takes_v && has(sv)) {
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) dma16(vpage, vgo8[i], raw + (kPieces + piece(i)) * 1024);
-      vsc = reinterpret_cast<const uint32_t*>(vspage)[lane & 3];
+        for (int i = 0; i < kMine; ++i) dma16(vbase + (int64_t)id_last * vsb, vgo8[i], raw + (kPieces + piece(i)) * 1024);
+        vsc = reinterpret_cast<const uint32_t*>(powers(p.v_scale, id_last))[l & 3];
+      }
     }
   };
   // copies of iteration j, both steps whole
@@ -485,6 +490,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   // K of step sk and V of step sv where either may end inside the step or lie past the end
   auto copy_any = [&](const char* ksrc, int sk, const char* vsrc, int sv) {
     if constexpr (kFp8) {
+      if constexpr (kHelp) return;  // (the helpers have a loop of their own)
       convert(sk, sv);
       fetch(sk + 1, sv + 1);
       return;
@@ -790,23 +796,25 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
     if (!kHelp || copier) {
       uint4 k0[kMine] = {}, k1[kMine] = {}, v0[kMine] = {};
       uint32_t s0[kMine] = {}, s1[kMine] = {}, sv = 0;
-      const uint8_t* vs = p.v_scale + ((int64_t)id_cur * p.num_kv_heads + w.kv_head) * kBlockSize;
-      const char* vp = vbase + (int64_t)id_cur * vsb;
+      const char *kp = kbase + (int64_t)id_cur * ksb, *vp = vbase + (int64_t)id_cur * vsb;
+      const uint8_t* kps = powers(p.k_scale, id_cur);
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         if (takes_k && has(0)) {
-          k0[i] = *reinterpret_cast<const uint4*>(kpage + kgo8[i]);
-          s0[i] = kspage[k_token(i)];
+          k0[i] = *reinterpret_cast<const uint4*>(kp + kgo8[i]);
+          s0[i] = kps[k_token(i)];
         }
         if (takes_v && has(0)) v0[i] = *reinterpret_cast<const uint4*>(vp + vgo8[i]);
       }
-      if (takes_v && has(0)) sv = reinterpret_cast<const uint32_t*>(vs)[lane & 3];
+      if (takes_v && has(0)) sv = reinterpret_cast<const uint32_t*>(powers(p.v_scale, id_cur))[lane & 3];
       next_pages(1);
+      kp = kbase + (int64_t)id_cur * ksb;
+      kps = powers(p.k_scale, id_cur);
 #pragma unroll
       for (int i = 0; i < kMine; ++i)
         if (takes_k && has(1)) {
-          k1[i] = *reinterpret_cast<const uint4*>(kpage + kgo8[i]);
-          s1[i] = kspage[k_token(i)];
+          k1[i] = *reinterpret_cast<const uint4*>(kp + kgo8[i]);
+          s1[i] = kps[k_token(i)];
         }
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
@@ -817,7 +825,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
       next_pages(1);
     }
     next_pages(2);
-    fetch(2, 1);
+    if (!kHelp || copier) fetch(2, 1);
     next_pages(3);
   } else {
     copy_any(kbase + (int64_t)id_cur * ksb, 0, vbase + (int64_t)id_cur * vsb, 0);
@@ -844,6 +852,19 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   const int nw = vmax >= w.kv_lo ? min(n, (vmax - w.kv_lo) / kKvStep + 1) : 0;
   if constexpr (!kFp8) wait_dma<0>();
   lds_barrier();
+  if constexpr (kFp8 && kHelp) {
+    if (copier) {  // the helpers' steps
+      lds_barrier();
+      for (int s = 0; s < n; ++s) {
+        convert(s + 2, s + 1);
+        fetch(s + 3, s + 2);
+        move_ids(s + kLead);
+        next_pages(s + kLead);
+        lds_barrier();
+      }
+      return;
+    }
+  }
   if (nw > 0) {
     qk_plain(0, 0);
     if (need_mask(0)) mask_plain(0, 0);
@@ -936,28 +957,29 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   };
   // What a pipelined step j does beside its PV MFMAs: the page addresses of the next copies and, for an
   // 8-bit cache, the whole of its turning and copying (its vector work is what the MFMAs leave room for).
+  uint4 chunk;
   auto beside = [&](int jj) {
     return [&, jj]([[maybe_unused]] int i) __attribute__((always_inline)) {
-      (void)jj;
+      (void)jj, (void)chunk;
       if constexpr (!kFp8) {
         if (i == 0) next_pages(jj + kLead);
       } else if constexpr (!kHelp) {
-        if (i == 0) read_raw();
-#pragma unroll
-        for (int u = 0; u < kMine; ++u) {
-          if (i == 1 + u) turn_k(jj + 2, u);
-          if (i == 3 + u * (kPv / 4)) turn_v(jj + 1, u);
-        }
-        if (i == kPv - 2) fetch(jj + 3, jj + 2);
-        if (i == kPv - 1) next_pages(jj + kLead);
+        constexpr int kSpan = D == 128 ? 3 : 2, kDone = 2 * kMine * kSpan;  // MFMAs to a chunk, to all
+        if (i == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (i % kSpan == 0 && i < kDone) chunk = raw_chunk(i / kSpan);
+        if (i % kSpan == kSpan - 1 && i < kDone) turn(i / kSpan, jj + 2, jj + 1, chunk);
+        if (i == kDone) fetch(jj + 3, jj + 2);
+        if (i == kDone + 1) next_pages(jj + kLead);
       }
     };
   };
   // One step without overlap; waves past their last step still copy.
   auto step = [&](int jj) __attribute__((always_inline)) {
     copy_any(kpage, jj + 2, vpage, jj + 1);
-    move_ids(jj + kLead);
-    next_pages(jj + kLead);
+    if constexpr (!(kFp8 && kHelp)) {
+      move_ids(jj + kLead);
+      next_pages(jj + kLead);
+    }
     if (jj < nw) {
       if constexpr (kPrecise) plain_precise(jj);
       else plain(jj, past_first(jj));
@@ -982,7 +1004,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   const int whole = (w.kv_hi - w.kv_lo) / kKvStep;  // steps without a missing block
   for (; j + 2 < nw && !past_first(j + 2); j += 2) {
     if constexpr (!kFp8) copy_whole(j);  // step j+2 is not masked, hence whole
-    if constexpr (kFp8) move_ids(j + 4);  // (an odd step is none that ids move in at)
+    if constexpr (kFp8 && !kHelp) move_ids(j + 4);  // (an odd step is none that ids move in at)
     fused(std::integral_constant<int, 0>{}, beside(j));
     mask_window(1, j + 1);
     tail();
@@ -1000,8 +1022,8 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   // the pipelined step takes the next step's row max, so that one must need no
   // mask either.)  A 3-step item of a helped workgroup 9.9 -> 8.9 us.
   if (j + 1 < nw && !past_first(kPrecise ? j + 1 : j)) {
-    if constexpr (kFp8) move_ids(j + 4);
-    else copy_any(kpage, j + 2, vpage, j + 1);
+    if constexpr (!kFp8) copy_any(kpage, j + 2, vpage, j + 1);
+    else if constexpr (!kHelp) move_ids(j + 4);
     fused(std::integral_constant<int, 0>{}, beside(j));
     if (!kPrecise && need_mask(j + 1)) mask_plain(1, j + 1);
     tail();
