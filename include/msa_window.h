@@ -9,8 +9,10 @@
  * The window belongs to the plan: a plan of msa_plan_window goes wherever one of
  * msa_plan does (msa_forward, msa_forward_noalloc, msa_fp8_forward, msa_kv_append,
  * msa_rope_append, msa_fp8_append, msa_check_block_table, msa_plan_info, whose figures
- * count visible pairs and keys, msa_plan_export), but for msa_kv_weights.  A
- * model whose layers differ has a plan for each kind.
+ * count visible pairs and keys, msa_plan_export), but for msa_kv_weights, which
+ * refuses one that hides keys.  A model whose layers differ has a plan for each kind.
+ * Rows of up to 128 keys (window + sinks) carry their weights as with
+ * MSA_PLAN_PRECISE_WEIGHTS, as causal rows of up to 64 do.
  *
  * Blocks that are out of every window can be given to other sequences: of
  * sequence b, with its first and last query positions f and l, the kernels read
@@ -32,7 +34,7 @@ extern "C" {
 /*
  * msa_plan_window: msa_plan for rows that see a window and sinks.
  *
- *   window  >= 1; past the longest context it is the same as msa_plan
+ *   window  >= 1; where it hides nothing from any row, the plan is msa_plan's
  *   sinks   >= 0
  *
  * The other arguments and the statuses are those of msa_plan.  A work item's

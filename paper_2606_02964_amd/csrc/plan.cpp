@@ -63,9 +63,14 @@ constexpr int64_t kWideMinTiles64 = 1024;  // narrow tiles, head_dim 64
 // fill 0.82 1296 / 1313, 0.57 566 / 621; 24 of 32: 0.94 1645 / 1605)
 constexpr double kWideMinFill = 0.9;
 // ... and, with a window, the steps of a tile: short tiles' start and end, 8.5 us of a workgroup, run beside
-// another's steps where a CU has two (windows of 200 keys 804 / 717, 512 633 / 625, 1024 916 / 941, 2048
-// 1401 / 1419 as wide / narrow; 4 prompts of 6000, 64 heads)
-constexpr double kWideMinUnitSteps = 16.0;
+// another's steps where a CU has two (us, wide / narrow: a prompt of 12000 with 32 heads, windows of 512 keys
+// 168 / 157, 1024 248 / 237, 2048 388 / 393; 4 of 6000, 336 / 322, 475 / 467, 689 / 708)
+constexpr double kWideMinUnitSteps = 24.0;
+// uneven loads of a plan with a window, in key steps over the mean, up to which nothing is cut: its many short
+// items end nearly together, and partials and their merge launch cost more (us, whole / cut: the prompt of 12000
+// with 1024 keys, 8 steps over the mean, 237 / 251; 12 chunks of 256 rows, 1024 keys, 11 steps, 82.6 / 84.4,
+// 2048 keys, 20 steps, 135 / 128)
+constexpr double kWindowUnevenSteps = 14.0;
 constexpr double kWasteFrac = 0.125;     // masked keys allowed per tile, relative
 constexpr int64_t kMinSplitKeys = 1024;  // never split below this many keys
 constexpr int64_t kMinSplitSteps = kMinSplitKeys / kKvStep;
@@ -375,12 +380,14 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
       for (int32_t k = seg_indptr[b]; k < seg_indptr[b + 1]; ++k)
         for (int32_t t = 0; t < seg_len[k]; ++t) P.row_pos[(size_t)r++] = seg_start[k] + t;
   }
-  // (no more than there are positions: sums of them stay within 32 bits)
   if (window > 0) {
-    int32_t top = 1;
+    int32_t top = 1;  // the most positions that a row has up to its own
     for (int32_t b = 0; b < B; ++b) top = std::max(top, seq_maxpos[b] + 1);
-    P.window = window = std::min(window, top);
-    P.sinks = sinks = std::min(sinks, top);
+    if (window >= top) window = 0;  // nothing is hidden: a causal plan
+  }
+  if (window > 0) {
+    P.window = window;
+    P.sinks = sinks = std::min(sinks, *std::max_element(seq_maxpos.begin(), seq_maxpos.end()) + 1);  // (sums stay within 32 bits)
     // Rows of few keys carry all their weights as hi + lo terms.  A causal row of up to 64 does anyway, as
     // they are in the step that holds its own position, but a window's keys start in the step before, and
     // sinks are in another: with two keys, half the weight would be off by 2^-9.  Past 128 keys at
@@ -770,6 +777,18 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
         if ((double)lo + ov <= kOneRoundFactor * capacity) capacity = (double)lo + ov;
       }
       capacity = std::max(capacity, min_steps + ov);
+      if (window > 0) {
+        std::vector<double> heap((size_t)wgs_per_xcd, 0.0);
+        double most = 0.0;
+        for (const Part& part : px)
+          for (size_t qi = part.first; qi < part.last; ++qi) {
+            std::pop_heap(heap.begin(), heap.end(), std::greater<double>());
+            heap.back() += pcost(chunks[(size_t)qx[qi]]);
+            most = std::max(most, heap.back());
+            std::push_heap(heap.begin(), heap.end(), std::greater<double>());
+          }
+        if (most <= mean_load + kWindowUnevenSteps) capacity = std::max(capacity, most);
+      }
     }
     typedef std::pair<double, int> Slot;  // (load, workgroup of this XCD): least loaded first, then lowest
     std::vector<Slot> slots;  // heap of the workgroups in use; pieces take the idle ones first, in turn

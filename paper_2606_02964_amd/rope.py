@@ -84,17 +84,22 @@ def sizes(plan: Plan):
 
 def rows_of(who: str, name: str, x, rows: int, heads: int, d: int, dev: int):
     """(address, strides by row and head) of bfloat16 rows [rows, heads, d]; an address means contiguous ones."""
+    if type(x) is Tensor and x.dim() == 3:  # (the common case: a few reads, as in tree.py)
+        n, h, c = x.shape
+        by_row, by_head, by_channel = x.stride()
+        # (what a dimension of one entry says of its stride does not matter)
+        if c == d and h == heads and n >= rows and by_channel == 1 and x.get_device() == dev and x.dtype in BF16:
+            return x.data_ptr(), by_row if n > 1 else heads * d, by_head if h > 1 else d
     if x is None or type(x) is int or not hasattr(x, "stride"):
         return _addr(x), heads * d, d
     if x.dtype not in BF16 or x.get_device() != dev or not x.is_cuda:
         refuse_tensor(who, name, x, BF16, None, dev)
-    shape, step = x.shape, x.stride()
-    if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != d:
-        raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {name} has shape {tuple(shape)}, ({rows}, {heads}, {d}) is needed")
-    if step[2] != 1:
+    if x.dim() != 3 or x.shape[0] < rows or x.shape[1] != heads or x.shape[2] != d:
+        raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {name} has shape {tuple(x.shape)}, ({rows}, {heads}, {d}) is needed")
+    by_row, by_head, by_channel = x.stride()
+    if by_channel != 1:
         raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: {name} is not contiguous along its last dimension")
-    # (what a dimension of one entry says of its stride does not matter)
-    return x.data_ptr(), step[0] if shape[0] > 1 else heads * d, step[1] if heads > 1 else d
+    return x.data_ptr(), by_row if x.shape[0] > 1 else heads * d, by_head if heads > 1 else d
 
 
 def bytes_address(who: str, name: str, x, dev: int):

@@ -86,9 +86,17 @@ def test_wide_window_is_the_causal_plan():
         lens, indptr, start, length = random_layout(r)
         blocks = max([1] + [-(-x // 16) for x in lens])
         shape = msa.make_shape(len(lens), 8, 2, 128, blocks, max(1, blocks * len(lens)), 0.1)
-        a = msa.msa_plan_export(msa.msa_plan(shape, lens, indptr, start, length, flags=HOST))
-        b = msa.msa_plan_export(msa.msa_plan_window(shape, lens, indptr, start, length, max(lens) + 1, 3, flags=HOST))
-        assert all(np.array_equal(x, y) for x, y in zip(a, b))
+        a = msa.msa_plan(shape, lens, indptr, start, length, flags=HOST)
+        b = msa.msa_plan_window(shape, lens, indptr, start, length, max(lens) + 1, 3, flags=HOST)
+        assert all(np.array_equal(x, y) for x, y in zip(msa.msa_plan_export(a), msa.msa_plan_export(b)))
+        assert a.info() == b.info() and msa.msa_kv_weights_workspace(a) == msa.msa_kv_weights_workspace(b)
+    # a plan of many tiles, whose width and cuts go by other rules where keys are hidden
+    shape = msa.make_shape(3, 64, 8, 128, 700, 2100, 0.1)
+    layout = ([9000, 11000, 5000], [0, 1, 2, 3], [0, 0, 100], [9000, 11000, 4900])
+    a = msa.msa_plan_export(msa.msa_plan(shape, *layout, flags=HOST))
+    b = msa.msa_plan_export(msa.msa_plan_window(shape, *layout, 11000, 3, flags=HOST))
+    c = msa.msa_plan_export(msa.msa_plan_window(shape, *layout, 10999, 0, flags=HOST))
+    assert all(np.array_equal(x, y) for x, y in zip(a, b)) and len(c[1]) > 0
 
 
 def test_check_block_table():
