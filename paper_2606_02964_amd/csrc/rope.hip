@@ -176,12 +176,20 @@ __global__ __launch_bounds__(256) void msa_rope_kernel(RopeParams p) {
     }
   };
 
+  // the row's places (in vector registers: with all strides in scalar ones the loop spills them)
+  const uint16_t* q_row = p.q + r * p.q_st + q0 * p.q_sh;
+  uint16_t* qo_row = p.q_out + r * p.qo_st + q0 * p.qo_sh;
+  const uint16_t* k_row = p.k_new + r * p.kn_st + kv0 * p.kn_sh;
+  const uint16_t* v_row = p.v_new + r * p.vn_st + kv0 * p.vn_sh + 16 * lane;
+  cache_t* kc_row = static_cast<cache_t*>(p.k_cache) + (int64_t)blk * p.k_sb + kv0 * p.k_sh + (int64_t)(off0 + row) * p.k_st;
+  cache_t* vc = static_cast<cache_t*>(p.v_cache) + (int64_t)blk * p.v_sb + kv0 * p.v_sh;
+  const int64_t powers = ((int64_t)blk * p.num_kv_heads + kv0) * 16 + off0 + row;
   for (int h0 = 0; h0 < heads; h0 += per) {
     const int h = h0 + first;
     if (active && h < heads && h >= nkv) {
-      const int64_t g = q0 + h - nkv;
-      const uint16_t* src = p.q + r * p.q_st + g * p.q_sh;
-      uint16_t* dst = p.q_out + r * p.qo_st + g * p.qo_sh;
+      const int64_t g = h - nkv;
+      const uint16_t* src = q_row + g * p.q_sh;
+      uint16_t* dst = qo_row + g * p.qo_sh;
       const uint4 a = *reinterpret_cast<const uint4*>(src + ca), b = *reinterpret_cast<const uint4*>(src + cb);
       if (turned) {
         float x[16];
@@ -198,16 +206,16 @@ __global__ __launch_bounds__(256) void msa_rope_kernel(RopeParams p) {
     if (h0 >= nkv || !stored) continue;  // (uniform: no K/V head in this pass)
     const int ng = nkv - h0 < per ? nkv - h0 : per;  // K/V heads of the pass
     if (active && h < nkv) {
-      const int64_t g = kv0 + h;
-      const uint16_t* ks = p.k_new + r * p.kn_st + g * p.kn_sh;
-      const uint16_t* vs = p.v_new + r * p.vn_st + g * p.vn_sh + 16 * lane;
+      const int64_t g = h;
+      const uint16_t* ks = k_row + g * p.kn_sh;
+      const uint16_t* vs = v_row + g * p.vn_sh;
       const uint4 ka = *reinterpret_cast<const uint4*>(ks + ca), kb = *reinterpret_cast<const uint4*>(ks + cb);
       const uint4 va = *reinterpret_cast<const uint4*>(vs), vb = *reinterpret_cast<const uint4*>(vs + 8);
-      cache_t* kd = static_cast<cache_t*>(p.k_cache) + (int64_t)blk * p.k_sb + g * p.k_sh + (int64_t)(off0 + row) * p.k_st;
+      cache_t* kd = kc_row + g * p.k_sh;
       cache_t* sv = s_v[first * n + row] + 16 * lane;
       float x[16];
       if constexpr (kFp8) {
-        const int64_t at = ((int64_t)blk * p.num_kv_heads + g) * 16 + off0 + row;
+        const int64_t at = powers + g * 16;
         unpack(ka, x);
         unpack(kb, x + 8);
         turn(x);
@@ -245,13 +253,15 @@ __global__ __launch_bounds__(256) void msa_rope_kernel(RopeParams p) {
     }
     __syncthreads();
     // V out, one half block (8 tokens) at a time
-    cache_t* vd = static_cast<cache_t*>(p.v_cache) + (int64_t)blk * p.v_sb + (int64_t)(kv0 + h0) * p.v_sh;
+    cache_t* vd = vc + (int64_t)h0 * p.v_sh;
+#pragma unroll 1
     for (int hb = 0; hb < 2; ++hb) {
       const int lo = off0 > 8 * hb ? off0 : 8 * hb;
       const int hi = off0 + n < 8 * hb + 8 ? off0 + n : 8 * hb + 8;
       if (lo >= hi) continue;  // the slice misses this half
       const int w = hi - lo;
       if (w == 8) {
+#pragma unroll 1
         for (int idx = tid; idx < ng * D; idx += 256) {
           const int c = idx % D, g = idx / D;
           cache_t e[8];
@@ -272,6 +282,7 @@ __global__ __launch_bounds__(256) void msa_rope_kernel(RopeParams p) {
           }
         }
       } else {
+#pragma unroll 1
         for (int idx = tid; idx < ng * D * w; idx += 256) {
           const int t = lo + idx % w, c = (idx / w) % D, g = idx / (w * D);
           vd[(int64_t)g * p.v_sh + (int64_t)c * p.v_sd + t] = s_v[g * n + t - off0][c];
