@@ -459,7 +459,7 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
         double steps = 0, row_steps = 0;
         int64_t max_rows = 0;
         for (const Unit& u : narrow_units) {
-          const double st = (double)((u.kv_hi + kKvStep - 1) / kKvStep);
+          const double st = (double)(((int64_t)u.kv_hi + kKvStep - 1) / kKvStep);
           steps += st;
           row_steps += st * u.nrows;
           max_rows = std::max<int64_t>(max_rows, (int64_t)u.nrows * G);

@@ -35,8 +35,6 @@ def check(o, lse, ref, precise=False):
 @pytest.mark.parametrize("heads", [(4, 4, 64), (8, 2, 128), (32, 8, 128), (64, 1, 64), (256, 1, 128), (15, 3, 64)], ids=str)
 @pytest.mark.parametrize("seqs", LAYOUTS)
 def test_forward(heads, seqs):
-    if heads[0] > 60 and seqs == "prompt":
-        pytest.skip("a reference of minutes")
     lay = Layout(LAYOUTS[seqs], *heads, seed=1)
     cache = cache8(lay, 3)
     q = normal(4, lay.rows, lay.hq, lay.d)

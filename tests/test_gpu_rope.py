@@ -236,3 +236,36 @@ def test_frequencies_on_the_card():
     q_out = torch.empty(lay.rows, 8, 128, dtype=torch.bfloat16, device="cuda")
     msa.msa_rope_append(lay.plan(msa), msa.make_rope(freq, 0, a), q, q_out, k_new, v_new, lay.table, k, v)
     check_bf16(q_out, q, lay.pos, freq, 0, a)
+
+
+def test_tree_rows_turn_by_their_depth():
+    """A tree's slots are written at their places and turned by their depths; the attention of the tree then sees
+    them as a chain of that depth would have them."""
+    ctx, parents = 40, [-1, 0, 0, 1, 3, 2]
+    depth = [0]
+    for p in parents[1:]:
+        depth.append(depth[p] + 1)
+    lay = Layout([(ctx + 6, [(ctx, 6)])], 4, 2, 64, seed=20)
+    plan = msa.msa_plan_tree(lay.shape(msa), lay.lens, lay.indptr, lay.start, lay.length)
+    qkv, freq = normal(21, 6, 8, 64), freqs(64)
+    k, v = normal(22, lay.num_blocks, 2, BS, 64), normal(23, lay.num_blocks, 2, 64, BS)
+    pos = torch.tensor([ctx + x for x in depth], dtype=torch.int32, device="cuda")
+    q = torch.empty(6, 4, 64, dtype=torch.bfloat16, device="cuda")
+    msa.msa_rope_append(plan, msa.make_rope(freq), qkv[:, :4], q, qkv[:, 4:6], qkv[:, 6:], lay.table, k, v, positions=pos)
+    check_bf16(q, qkv[:, :4], pos, freq, 0, 1.0)
+    blk, at = lay.places()
+    check_bf16(k[blk, :, at], qkv[:, 4:6], pos, freq, 0, 1.0)
+    assert torch.equal(v[blk, :, :, at], qkv[:, 6:])
+    mask = torch.empty(6, 1, dtype=torch.int64, device="cuda")
+    msa.msa_tree_mask(plan, torch.tensor(parents, dtype=torch.int32, device="cuda"), mask)
+    o, lse = torch.empty_like(q), torch.empty(6, 4, device="cuda")
+    ws = torch.empty(max(1, plan.info()["workspace_bytes"]), dtype=torch.uint8, device="cuda")
+    msa.msa_tree_forward(plan, q, k, v, lay.table, mask, o, lse, ws)
+    kk, vv = lay.keys(0, k, False), lay.keys(0, v, True)
+    for i in range(6):
+        seen, t = list(range(ctx)), i
+        while t >= 0:
+            seen.append(ctx + t)
+            t = parents[t]
+        x = torch.stack([q[i, h].double() @ kk[seen, h // 2].T for h in range(4)]) * 64 ** -0.5
+        assert (torch.logsumexp(x, 1) - lse[i].double()).abs().max() <= 2.5e-4

@@ -97,3 +97,35 @@ def test_calls_refuse_before_the_device():
     big = msa.make_shape(1 << 20, 8, 2, 128, 1000, 1000, 0.1)
     assert refused("2\\^23", shape=big, to=big, max_len=16000) == msa.MSA_ERR_UNSUPPORTED
     read(max_len=0)  # nothing to do
+
+
+@pytest.mark.parametrize("header", ["msa_rope.h", "msa_fp8.h", "msa_window.h"])
+def test_headers_are_c(header, tmp_path):
+    import shutil
+    import subprocess
+    if not shutil.which("gcc"):
+        pytest.skip("no gcc")
+    src = tmp_path / "t.c"
+    src.write_text(f'#include "{header}"\nint main(void) {{ return 0; }}\n')
+    res = subprocess.run(["gcc", "-std=c99", "-Wall", "-Wextra", "-Werror", "-pedantic", "-fsyntax-only", "-I", INCLUDE, str(src)],
+                         capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+
+
+def test_structs_match_the_header(tmp_path):
+    """Sizes and offsets of the binding's structs, by the C compiler."""
+    import ctypes
+    import shutil
+    import subprocess
+    if not shutil.which("gcc"):
+        pytest.skip("no gcc")
+    fields = [(s, f) for s in (msa.msa_rope, msa.msa_rope_scaling) for f, _ in s._fields_]
+    lines = "".join(f'printf("%zu\\n", offsetof({s.__name__}, {f}));' for s, f in fields)
+    lines += "".join(f'printf("%zu\\n", sizeof({s.__name__}));' for s in (msa.msa_rope, msa.msa_rope_scaling))
+    src = tmp_path / "t.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "msa_rope.h"\nint main(void) {' + lines + "return 0; }\n")
+    exe = tmp_path / "t"
+    subprocess.run(["gcc", "-I", INCLUDE, str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    want = [getattr(s, f).offset for s, f in fields] + [ctypes.sizeof(s) for s in (msa.msa_rope, msa.msa_rope_scaling)]
+    assert got == want
