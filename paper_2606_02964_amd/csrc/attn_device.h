@@ -387,6 +387,11 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
   // which the conversion applies; a V chunk (16 tokens of a channel) has 16, the same for all lanes.
   // Four waves share the pages' 1 KB pieces by block slot; of eight computing waves both groups of four
   // take half of them (d = 64: K and V, whose pages are one piece); helpers take all of them.
+  // Chunks of up to 512 rows over 8 sequences of up to 8192 keys, 32 query heads on 8 (256-row tiles): 425 us,
+  // over a bf16 cache 392, of which the conversions are some 20 and the copies beside the MFMAs 12; all of it at
+  // a step's start 540, beside the MFMAs with addresses kept in registers (spills) 453.
+  // (K by the 8-bit matrix instructions, Q in two e4m3 terms, would need no conversion and half the LDS
+  // reads; their sums are off by 4e-5 of the terms' magnitudes, too much for scores.)
   constexpr int kPieces = D / 64;  // of a page
   constexpr bool kHalved = kFp8 && W == 8 && !kHelp;
   constexpr int kMine = kHalved && kPieces == 2 ? 1 : kPieces;  // of a page, that a wave takes
@@ -965,6 +970,7 @@ __device__ __forceinline__ void attn_item(const P& p, const WorkItem w, char* sm
         if (i == 0) next_pages(jj + kLead);
       } else if constexpr (!kHelp) {
         constexpr int kSpan = D == 128 ? 3 : 2, kDone = 2 * kMine * kSpan;  // MFMAs to a chunk, to all
+        static_assert(kDone + 1 < kPv, "a step's copies have to be beside its MFMAs");
         if (i == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (i % kSpan == 0 && i < kDone) chunk = raw_chunk(i / kSpan);
         if (i % kSpan == kSpan - 1 && i < kDone) turn(i / kSpan, jj + 2, jj + 1, chunk);
