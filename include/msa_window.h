@@ -18,6 +18,7 @@
  * sequence b, with its first and last query positions f and l, the kernels read
  * the table entries of the blocks that hold a position in
  * [max(0, f - window + 1), l] or below min(sinks, l + 1), and no others.
+ * Positions in those blocks that a row does not see are multiplied by 0: their V must be finite.
  */
 #ifndef MSA_WINDOW_H_
 #define MSA_WINDOW_H_

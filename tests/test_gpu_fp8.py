@@ -55,15 +55,23 @@ def test_widths_splits_precise_windows(heads, rows, split, precise, window, sink
     check(*forward(lay, plan, q, cache), lay.attend(q, cache[4], cache[5], window, sinks), precise)
 
 
-def test_many_narrow_tiles():
-    """128-row tiles, more than one for each CU: the form whose waves both copy and compute."""
-    lay = Layout([(260 + 7 * i, [(100, 128 + i)]) for i in range(24)], 32, 8, 128, seed=3)
+@pytest.mark.parametrize("precise", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_narrow_tiles(d, precise):
+    """128-row tiles, more than one for each CU: the form whose waves both copy and compute.  Over both kinds of cache."""
+    lay = Layout([(260 + 7 * i, [(100, 128 + i)]) for i in range(24)], 32, 8, d, seed=3)
     cache = cache8(lay, 7)
     q = normal(8, lay.rows, lay.hq, lay.d)
-    for window in (0, 77):
-        plan = lay.plan(msa, window, 2, flags=msa.MSA_PLAN_TILE_ROWS_128)
+    k16, v16 = cache[4].to(torch.bfloat16), cache[5].to(torch.bfloat16)
+    for window in (0, 140):
+        plan = lay.plan(msa, window, 2, flags=msa.MSA_PLAN_TILE_ROWS_128 | (msa.MSA_PLAN_PRECISE_WEIGHTS if precise else 0))
         assert plan.info()["num_workgroups"] > 256
-        check(*forward(lay, plan, q, cache), lay.attend(q, cache[4], cache[5], window, 2))
+        ref = lay.attend(q, cache[4], cache[5], window, 2)
+        check(*forward(lay, plan, q, cache), ref, precise)
+        o, lse = torch.empty_like(q), torch.empty(lay.rows, 32, device="cuda")
+        ws = torch.empty(max(1, plan.info()["workspace_bytes"]), dtype=torch.uint8, device="cuda")
+        msa.msa_forward(plan, q, k16, v16, lay.table, o, lse, ws)
+        check(o, lse, ref, precise)
 
 
 def test_long_rows():
