@@ -1,20 +1,22 @@
-// attn8_device.h -- work items of up to 32 rows over an 8-bit cache, read straight
-// into registers (decode_item of attn_device.h, which has the mathematics, over bytes).
+// attn8_device.h -- work items of up to 32 rows over an 8-bit cache (decode_item of
+// attn_device.h, which has the mathematics, over bytes).
 //
 // The four waves of a workgroup hold the same rows and take 32-key half-steps in
-// turn.  What differs is how keys and channels lie in the operands, so that every
-// load is 16 bytes:
+// turn.  A wave copies its half-steps' pages into LDS of its own, two stages of 8 KB (in
+// the area that its partial output takes at the end): every copy takes whole cache lines, so they can be
+// non-temporal, which the caches' lines read in parts cannot.  64 rows over 8000 keys, 32 query
+// heads on 8, d = 128: 164 us, 6.5 TB/s, where operands read straight into registers took 181 and these
+// copies without the hint 182 (bf16 350); 8 rows 26.5 (29.4, bf16 51.0); one over 120000 keys 47
+// (54.5), over 30000 18.0 with its merge (19.2, bf16 28.3).  Sequences that share all their blocks
+// lose up to 10% at d = 64 (16 over 30000 keys, 16 heads: 115 -> 127) and nothing at d = 128.
 //   * QK: lane half hl holds channels 32 i + 16 hl .. + 15 of its key (and of Q): a
-//     product does not mind the order of its terms.  A key's power of two goes into
-//     the conversion to bf16, which is exact.
+//     product does not mind the order of its terms, and a read from LDS is 16 bytes.  A key's
+//     power of two goes into the conversion to bf16, which is exact.
 //   * PV: a V chunk is 16 tokens of a channel, so lane half hl takes the tokens of
 //     block hl of the half-step's two.  K's rows are ordered such that the lane's 16
 //     scores are these tokens' too, in order: weights meet V without a move.  A
 //     token's power of two multiplies its weight (exactly), not its d values.
-// Half the bytes of the bf16 form leave registers for both K and V of the next
-// half-step while one is computed.  Bound by HBM where there are rows to fill it: 64 rows
-// over 8000 keys, 32 query heads on 8, d = 128: 182 us, 5.8 TB/s (bf16 350 us, 6.0); 8 rows
-// 29.7 us (51.0); one over 30000 keys 19.0 with its merge (28.3), 256 pieces' starts and one launch more.
+// Bound by HBM where there are rows to fill it, else by the pieces' starts and the merge's launch.
 #pragma once
 
 #include "attn_device.h"
@@ -25,6 +27,16 @@ namespace {
 __device__ __forceinline__ bf16x8 fp8_octet(uint32_t lo, uint32_t hi, float scale) {
   return __builtin_bit_cast(bf16x8, make_uint4(fp8_pair<false>(lo, scale), fp8_pair<true>(lo, scale),
                                                fp8_pair<false>(hi, scale), fp8_pair<true>(hi, scale)));
+}
+
+// 16 (4) bytes a lane straight into LDS, as dma16; the 16 are not kept in the caches
+__device__ __forceinline__ void stream16(const void* base, uint32_t off, void* lds) {
+  const uint32_t l = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "{m0}"(l) : "memory");
+}
+__device__ __forceinline__ void stream4(const void* src, void* lds) {
+  const uint32_t l = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "{m0}"(l) : "memory");
 }
 
 template <int D, bool kPrecise, class P>
@@ -75,14 +87,32 @@ __device__ __forceinline__ void decode8_item(const P& p, const WorkItem w, Decod
   // MFMA row m of K is token (m bits 4, 3, 1, 0) of block (m bit 2), so that lane half hl gets the
   // scores of block hl, register e those of token e
   const int kblk = (ln >> 2) & 1, ktok = ((ln >> 3) & 3) * 4 + (ln & 3);
+  // copies of a half-step into the wave's part of LDS, whole cache lines of K and of V each: token t's 16-byte
+  // chunk c goes to place c ^ swizzle(t), so that a chunk of all tokens lies over all banks
+  constexpr int kRowChunks = D / 16, kCopyToks = 64 / kRowChunks, kCopies = 16 / kCopyToks;  // of a block's K
+  constexpr int kStage = 2 * kHalf * D + 256, kOps = 4 * kCopies + 1;
+  static_assert(2 * kStage <= (int)sizeof(lds.mo[0]), "the copies fit the wave's part of the merge area");
+  char* const ring = reinterpret_cast<char*>(lds.mo[wave]);
+  auto swizzle = [](int token) { return token / (16 / kRowChunks) % kRowChunks; };
   const char* kbase = reinterpret_cast<const char*>(p.k) + (int64_t)w.kv_head * p.k_sh;
   const char* vbase = reinterpret_cast<const char*>(p.v) + (int64_t)w.kv_head * p.v_sh;
-  const uint32_t koff = (uint32_t)(ktok * p.k_st + hl * 16);
-  const uint32_t voff = (uint32_t)(ln * p.v_sd);
-  const uint32_t vdt = (uint32_t)(32 * p.v_sd);
-  const uint8_t* ksb = p.k_scale + w.kv_head * kBlockSize + ktok;
-  const uint8_t* vsb = p.v_scale + w.kv_head * kBlockSize;
-  const int64_t scales = (int64_t)p.num_kv_heads * kBlockSize;  // of a block
+  uint32_t koff[kCopies];
+#pragma unroll
+  for (int j = 0; j < kCopies; ++j) {
+    int token = j * kCopyToks + lane / kRowChunks;
+    asm volatile("" : "+v"(token));  // (else strides times constants are held in scalar registers over all items)
+    koff[j] = (uint32_t)(token * p.k_st + (lane % kRowChunks ^ swizzle(token)) * 16);
+  }
+  uint32_t voff[D / 64];
+#pragma unroll
+  for (int j = 0; j < D / 64; ++j) {
+    int channel = j * 64 + lane;
+    asm volatile("" : "+v"(channel));
+    voff[j] = (uint32_t)(channel * p.v_sd);
+  }
+  const uint8_t* sbase = (lane & 8 ? p.v_scale : p.k_scale) + w.kv_head * kBlockSize + (lane & 3) * 4;
+  int32_t scales = p.num_kv_heads * kBlockSize;  // of a block
+  asm volatile("" : "+v"(scales));  // (in vector registers: scalar ones are short)
 
   auto blocks = [&](int h, int64_t& id0, int64_t& id1) __attribute__((always_inline)) {
     const int i = (h - wave) / kWaves;  // wave-uniform
@@ -96,22 +126,20 @@ __device__ __forceinline__ void decode8_item(const P& p, const WorkItem w, Decod
       id1 = b;
     }
   };
-  constexpr int kChunks = D / 32;  // 16-byte chunks of a lane, of K and of V
-  uint4 ka[2][kChunks], va[2][kChunks], vs[2];
-  uint32_t ks[2];
-  auto load = [&](auto bsel, int h) __attribute__((always_inline)) {
-    constexpr int b = decltype(bsel)::value;
-    int64_t id0, id1;
-    blocks(h, id0, id1);
-    const int64_t kid = kblk ? id1 : id0, vid = hl ? id1 : id0;
-    const char* kp = kbase + kid * p.k_sb + koff;
-    const char* vp = vbase + vid * p.v_sb + voff;
-    ks[b] = ksb[kid * scales];
+  auto load = [&](int b, int h) __attribute__((always_inline)) {
+    int64_t id[2];
+    blocks(h, id[0], id[1]);
+    char* const to = ring + b * kStage;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) ka[b][i] = *reinterpret_cast<const uint4*>(kp + i * 32);
-    vs[b] = *reinterpret_cast<const uint4*>(vsb + vid * scales);
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) va[b][i] = *reinterpret_cast<const uint4*>(vp + i * vdt);
+      for (int j = 0; j < kCopies; ++j) stream16(kbase + id[u] * p.k_sb, koff[j], to + (u * kCopies + j) * 1024);
+    stream4(sbase + (lane & 4 ? id[1] : id[0]) * scales, to + 2 * kHalf * D);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j)
+        stream16(vbase + id[u] * p.v_sb, voff[j], to + kHalf * D + (u * D + j * 64) * 16);
   };
 
   const float c = p.scale_log2;
@@ -125,12 +153,29 @@ __device__ __forceinline__ void decode8_item(const P& p, const WorkItem w, Decod
   int pmin = 0, pmax = 0;  // positions of the tile's first and last row (set below, once loads are under way)
   auto half = [&](auto bsel, int h) __attribute__((always_inline)) {
     constexpr int b = decltype(bsel)::value;
-    if (h + kWaves < nh) load(std::integral_constant<int, 1 - b>{}, h + kWaves);
-    const float kf = __uint_as_float(ks[b] << 23);
+    if (h + kWaves < nh) {
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // the reads of that stage, lgkmcnt(0)
+      load(1 - b, h + kWaves);
+      wait_dma<kOps>();
+    } else {
+      wait_dma<0>();
+    }
+    asm volatile("" ::: "memory");
+    const char* const from = ring + b * kStage;
+    const uint8_t* const sc8 = reinterpret_cast<const uint8_t*>(from + 2 * kHalf * D);
+    const float kf = __uint_as_float((uint32_t)sc8[kblk * 16 + ktok] << 23);
+    uint4 ka[D / 32], va[D / 32];
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+      ka[i] = *reinterpret_cast<const uint4*>(from + (kblk * 16 + ktok) * D + (2 * i + hl ^ swizzle(ktok)) * 16);
+    const uint4 vs = *reinterpret_cast<const uint4*>(sc8 + 32 + hl * 16);
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+      va[i] = *reinterpret_cast<const uint4*>(from + kHalf * D + (hl * D + i * 32 + ln) * 16);
     f32x16 sc = {};
 #pragma unroll
     for (int kk = 0; kk < kQk; ++kk) {
-      const uint4& x = ka[b][kk >> 1];
+      const uint4& x = ka[kk >> 1];
       const bf16x8 a = kk & 1 ? fp8_octet(x.z, x.w, kf) : fp8_octet(x.x, x.y, kf);
       sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kk], sc, 0, 0, 0);
     }
@@ -178,7 +223,7 @@ __device__ __forceinline__ void decode8_item(const P& p, const WorkItem w, Decod
       }
     }
     l_run += ls;
-    const uint32_t sv[4] = {vs[b].x, vs[b].y, vs[b].z, vs[b].w};
+    const uint32_t sv[4] = {vs.x, vs.y, vs.z, vs.w};
 #pragma unroll
     for (int e = 0; e < 16; ++e) wv[e] *= __uint_as_float((sv[e >> 2] >> (8 * (e & 3)) & 0xff) << 23);
     uint32_t pk[8];
@@ -192,7 +237,7 @@ __device__ __forceinline__ void decode8_item(const P& p, const WorkItem w, Decod
       bf16x8 a[D / 32];
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt) {
-        a[dt] = ks ? fp8_octet(va[b][dt].z, va[b][dt].w, 1.0f) : fp8_octet(va[b][dt].x, va[b][dt].y, 1.0f);
+        a[dt] = ks ? fp8_octet(va[dt].z, va[dt].w, 1.0f) : fp8_octet(va[dt].x, va[dt].y, 1.0f);
         oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[dt], ph, oacc[dt], 0, 0, 0);
       }
       if (split) {
@@ -210,7 +255,7 @@ __device__ __forceinline__ void decode8_item(const P& p, const WorkItem w, Decod
       }
     }
   };
-  if (wave < nh) load(std::integral_constant<int, 0>{}, wave);
+  if (wave < nh) load(0, wave);
   pmin = __builtin_amdgcn_readfirstlane(row_of.first);
   pmax = __builtin_amdgcn_readlane(pos, w.nrows * G - 1);
   for (int h = wave; h < nh; h += 2 * kWaves) {

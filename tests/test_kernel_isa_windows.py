@@ -2,8 +2,8 @@
 cross-compiles), as test_kernel_isa.py makes them of the others:
 
 * no vector register goes to scratch memory; scalar registers go to lanes of vector ones only in
-  the tiles that have both a window and an 8-bit cache, and in the write kernel's 8-bit forms, which
-  hold most arguments (there once a workgroup);
+  the kernels that have both a window and an 8-bit cache, in the write kernel's 8-bit forms, which
+  hold most arguments (there once a workgroup), and one of an item's end in the 8-bit rows kernel;
 * tiles and rows keep two waves per SIMD, and their LDS lets two workgroups of 128-row tiles stay on a CU;
 * MFMA operand reads run ahead, and the pipelined step of an 8-bit tile has its conversions among its MFMAs;
 * numbers go to and from 8 bits by the conversion instructions.
@@ -41,7 +41,7 @@ def test_registers(compiled, src, kernels):
     assert len(found) == kernels
     for name, r in found.items():
         assert r.get("VGPRs Spill", 0) == 0 and r.get("ScratchSize", 0) == 0, (name, r)
-        most = 24 if "Fp8" in name and "Window" in name else 20 if "rope" in name else 0
+        most = 24 if "Fp8" in name and "Window" in name else 20 if "rope" in name else 1 if "Fp8" in name and "rows" in name else 0
         assert r.get("SGPRs Spill", 0) <= most, (name, r)
 
 
