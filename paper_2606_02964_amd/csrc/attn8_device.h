@@ -29,11 +29,7 @@ __device__ __forceinline__ bf16x8 fp8_octet(uint32_t lo, uint32_t hi, float scal
                                                fp8_pair<false>(hi, scale), fp8_pair<true>(hi, scale)));
 }
 
-// 16 (4) bytes a lane straight into LDS, as dma16; the 16 are not kept in the caches
-__device__ __forceinline__ void stream16(const void* base, uint32_t off, void* lds) {
-  const uint32_t l = (uint32_t)(uintptr_t)(lds_void_t*)lds;
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "{m0}"(l) : "memory");
-}
+// 4 bytes a lane straight into LDS, as dma16
 __device__ __forceinline__ void stream4(const void* src, void* lds) {
   const uint32_t l = (uint32_t)(uintptr_t)(lds_void_t*)lds;
   asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "{m0}"(l) : "memory");

@@ -146,6 +146,11 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t off, void* lds)
   const uint32_t l = (uint32_t)(uintptr_t)(lds_void_t*)lds;
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(l) : "memory");
 }
+// the same for lines that a copy takes whole and that nothing reads again: not kept in the caches
+__device__ __forceinline__ void stream16(const void* base, uint32_t off, void* lds) {
+  const uint32_t l = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "{m0}"(l) : "memory");
+}
 // wait until at most n copies issued by this wave are outstanding
 template <int n>
 __device__ __forceinline__ void wait_dma() {
@@ -1182,6 +1187,13 @@ __device__ __forceinline__ void merge_waves(const P& p, const WorkItem& w, Decod
 template <int D, bool kPrecise, class P>
 __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, DecodeLds<D>& lds) {
   constexpr bool kTree = P::kTree;
+  // With a window, K and V of a half-step come by way of LDS (the wave's part of the merge area), as in
+  // decode8_item: copies of whole cache lines, which may be non-temporal.  They are read into registers at once,
+  // and the next half-step's are under way while these are computed.  Registers loaded straight from the caches
+  // against this, us: 64 rows with windows of 4096 keys, 32 heads on 8, d = 128: 182 / 163 (6.6 TB/s), of 1024
+  // 50.9 / 45.0; 48 with 12000 keys 440 / 378; 64 over the same blocks 110 / 80; a row with 65000 keys 57 / 49;
+  // few short pieces, whose copies nothing hides, up to 3% more (64 rows, 1024 keys, 2 KV heads: 16.9 / 17.4).
+  constexpr bool kStream = P::kWindow;
   constexpr int kWaves = DecodeLds<D>::kWaves, kHalf = 32;
   if (w.nrows == 0) return;  // (uniform over the workgroup)
 
@@ -1255,7 +1267,7 @@ __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, Decode
   };
   constexpr int kQk = D / 16;       // QK MFMAs per half-step
   constexpr int kPv = 2 * (D / 32); // PV MFMAs per half-step, ordered (ks, dt)
-  bf16x8 ka[2][kQk], va[kPv];
+  bf16x8 ka[kStream ? 1 : 2][kQk], va[kPv];
   auto load_k = [&](auto bsel, int h) __attribute__((always_inline)) {
     constexpr int b = decltype(bsel)::value;
     int64_t id0, id1;
@@ -1274,6 +1286,51 @@ __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, Decode
     }
   };
 
+  // kStream: token t's 16-byte chunk c of K lies at place c ^ swizzle(t), channel n's chunk (8 tokens) of V
+  // at c ^ (n / 8 & 1), so that what 16 lanes read lies over all banks
+  constexpr int kRowChunks = D / 8, kCopies = D / 32;  // of a token of K; of a block, of K and of V
+  static_assert(4 * kHalf * D <= (int)sizeof(lds.mo[0]), "the copies fit the wave's part of the merge area");
+  char* const stage = reinterpret_cast<char*>(lds.mo[wave]);
+  auto swizzle = [](int token) { return token / (16 / kRowChunks) % kRowChunks; };
+  uint32_t kcopy[kStream ? kCopies : 1], vcopy[kStream ? kCopies : 1];
+  if constexpr (kStream) {
+#pragma unroll
+    for (int j = 0; j < kCopies; ++j) {
+      int at = j * 64 + lane;
+      asm volatile("" : "+v"(at));  // (else strides times constants are held in scalar registers over all items)
+      const int token = at / kRowChunks, channel = at >> 1;
+      kcopy[j] = (uint32_t)(token * p.k_st + (at % kRowChunks ^ swizzle(token)) * 8) * 2u;
+      vcopy[j] = (uint32_t)(channel * p.v_sd + ((at & 1) ^ (channel >> 3 & 1)) * 8) * 2u;
+    }
+  }
+  auto copy = [&](int h) __attribute__((always_inline)) {
+    int64_t id[2];
+    blocks(h, id[0], id[1]);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < kCopies; ++j) stream16(kbase + id[u] * ksb, kcopy[j], stage + (u * kCopies + j) * 1024);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < kCopies; ++j)
+        stream16(vbase + id[u] * vsb, vcopy[j], stage + 2 * kHalf * D + (u * kCopies + j) * 1024);
+  };
+  auto take = [&]() __attribute__((always_inline)) {
+    wait_dma<0>();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int kk = 0; kk < kQk; ++kk)
+      ka[0][kk] = *reinterpret_cast<const bf16x8*>(stage + krow * 2 * D + (2 * kk + hl ^ swizzle(krow & 15)) * 16);
+#pragma unroll
+    for (int i = 0; i < kPv; ++i) {
+      const int ks = i / (D / 32), dt = i % (D / 32);
+      va[i] = *reinterpret_cast<const bf16x8*>(stage + 2 * kHalf * D + ks * 32 * D + (dt * 32 + ln) * 32 +
+                                               (hl ^ (ln >> 3 & 1)) * 16);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  };
+
   const float c = p.scale_log2;
   float m_ref = -__builtin_inff(), l_run = 0.0f;
   f32x16 oacc[D / 32];
@@ -1287,8 +1344,13 @@ __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, Decode
   // one half-step h of this wave, its K in buffer b
   auto half = [&](auto bsel, int h) __attribute__((always_inline)) {
     constexpr int b = decltype(bsel)::value;
-    load_v(h);
-    if (h + kWaves < nh) load_k(std::integral_constant<int, 1 - b>{}, h + kWaves);
+    if constexpr (kStream) {
+      take();
+      if (h + kWaves < nh) copy(h + kWaves);
+    } else {
+      load_v(h);
+      if (h + kWaves < nh) load_k(std::integral_constant<int, 1 - b>{}, h + kWaves);
+    }
     f32x16 sc = {};
 #pragma unroll
     for (int kk = 0; kk < kQk; ++kk) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[b][kk], qf[kk], sc, 0, 0, 0);
@@ -1389,12 +1451,19 @@ __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, Decode
       }
     }
   };
-  if (wave < nh) load_k(std::integral_constant<int, 0>{}, wave);
+  if (wave < nh) {
+    if constexpr (kStream) copy(wave);
+    else load_k(std::integral_constant<int, 0>{}, wave);
+  }
   pmin = __builtin_amdgcn_readfirstlane(row_of.first);
   if constexpr (P::kWindow) pmax = __builtin_amdgcn_readlane(pos, w.nrows * G - 1);
-  for (int h = wave; h < nh; h += 2 * kWaves) {
-    half(std::integral_constant<int, 0>{}, h);
-    if (h + kWaves < nh) half(std::integral_constant<int, 1>{}, h + kWaves);
+  if constexpr (kStream) {
+    for (int h = wave; h < nh; h += kWaves) half(std::integral_constant<int, 0>{}, h);
+  } else {
+    for (int h = wave; h < nh; h += 2 * kWaves) {
+      half(std::integral_constant<int, 0>{}, h);
+      if (h + kWaves < nh) half(std::integral_constant<int, 1>{}, h + kWaves);
+    }
   }
 
   merge_waves<D>(p, w, lds, tid, wave, hl, ln, oacc, m_ref, l_run);

@@ -4,7 +4,7 @@
 // The kernels are those of attn.hip with a window's visibility and key axis (see
 // attn_device.h): a tile reads the keys that some row of it sees, in whole steps of
 // 64, and the planner cuts and deals out those alone.  Bound as those are: 48 rows over 32K keys
-// with a window of 4096 (32 query, 8 KV heads, d = 128) read K/V at 5.4 TB/s (148 us); a prompt of
+// with a window of 4096 (32 query, 8 KV heads, d = 128) read K/V at 6.2 TB/s (131 us); a prompt of
 // 12000 with 1024 keys runs at 870 TFLOP/s of visible pairs (233 us): its tiles have 18 steps, against
 // which an item's start and end weigh 5 or 6, and 6% of the keys in them are hidden.  (The next item's
 // descriptor and block ids loaded during the one before: the same within 1%.)
