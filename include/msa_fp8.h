@@ -56,7 +56,8 @@ msa_status msa_fp8_append(msa_plan_t plan, const void *k_new, const void *v_new,
  *
  * Cache positions past a row's own, inside a block that is read, must hold finite
  * numbers (s <= 247, no e4m3 NaN), as in msa.h.  MSA_ERR_UNSUPPORTED for a plan of
- * msa_plan_tree; otherwise the statuses of msa_forward.
+ * msa_plan_tree, or where K or V of a block spans 4 GiB or more; otherwise the statuses of
+ * msa_forward.
  */
 msa_status msa_fp8_forward(msa_plan_t plan, const void *q, const void *k_cache, const void *v_cache,
                            const uint8_t *k_scale, const uint8_t *v_scale,

@@ -38,7 +38,8 @@ extern "C" {
  *   window  >= 1; where it hides nothing from any row, the plan is msa_plan's
  *   sinks   >= 0
  *
- * The other arguments and the statuses are those of msa_plan.  A work item's
+ * The other arguments and the statuses are those of msa_plan; MSA_ERR_UNSUPPORTED also where a
+ * block's K or V, of 2 bytes a number, spans 4 GiB or more.  A work item's
  * kv_lo and kv_hi (msa_plan_export) count the keys of its tile's axis: the positions
  * below H = sinks rounded up to 64, then those from H + skip on, where skip is how far
  * the first row's window (its start rounded down to 64) lies past H, or 0.

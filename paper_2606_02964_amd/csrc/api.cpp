@@ -281,6 +281,8 @@ msa_status msa_plan_window(const msa_shape* shape, const int32_t* seq_kv_len, co
   if (out) *out = nullptr;
   if (window < 1) return set_error(MSA_ERR_INVALID_ARG, "msa_plan_window: window must be >= 1");
   if (sinks < 0) return set_error(MSA_ERR_INVALID_ARG, "msa_plan_window: sinks must be >= 0");
+  if (shape && shape->head_dim > 1 && !msa::block_spans_fit(*shape, 2))
+    return set_error(MSA_ERR_UNSUPPORTED, "msa_plan_window: K or V of a block spans 4 GiB or more");
   return make_plan("msa_plan_window", shape, seq_kv_len, seg_indptr, seg_start, seg_len, false, nullptr, window, sinks,
                    opts, hip_stream, out);
 }

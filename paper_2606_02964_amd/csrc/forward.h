@@ -31,6 +31,12 @@ msa_status merge_splits(const char* who, msa_plan_t plan, void* o, float* lse, v
 // MSA_OK, or MSA_ERR_DEVICE with a message, for the hipError_t of a launch.
 msa_status launched(const char* who, const char* what, int rc);
 
+// Whether a block's K and V, of `bytes` a number, span less than 4 GiB each: the kernels' offsets within one are 32 bits.
+inline bool block_spans_fit(const msa_shape& s, int bytes) {
+  const int64_t most = ((int64_t)1 << 32) / bytes;
+  return s.k_stride_tok <= (most - s.head_dim) / (kBlockSize - 1) && s.v_stride_dim <= (most - kBlockSize) / (s.head_dim - 1);
+}
+
 // Workspace bytes a plan's msa_forward needs (plan non-null).
 int64_t plan_workspace_bytes(msa_plan_t plan);
 

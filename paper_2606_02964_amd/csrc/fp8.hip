@@ -110,6 +110,7 @@ extern "C" msa_status msa_fp8_forward(msa_plan_t plan, const void* q, const void
   if (hp.has_trees) return msa::refuse(who, MSA_ERR_UNSUPPORTED, "plans of msa_plan_tree read bf16 caches");
   const std::string strides = msa::fp8_strides(hp.shape);
   if (!strides.empty()) return msa::refuse(who, MSA_ERR_INVALID_ARG, strides);
+  if (!msa::block_spans_fit(hp.shape, 1)) return msa::refuse(who, MSA_ERR_UNSUPPORTED, "K or V of a block spans 4 GiB or more");
   if (hp.work.empty()) return MSA_OK;
   if (!k_scale || !v_scale || !msa::aligned(k_scale, 16) || !msa::aligned(v_scale, 16))
     return msa::refuse(who, MSA_ERR_INVALID_ARG, "k_scale and v_scale must be non-null and 16-byte aligned");

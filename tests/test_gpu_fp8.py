@@ -257,6 +257,10 @@ def test_refusals():
     refused("msa_plan_tree", msa.MSA_ERR_UNSUPPORTED, p=tree)
     odd = lay.plan(msa, shape=lay.shape(msa, k_strides=(4104, 2048, 128)))
     refused("multiples of 16", p=odd)
+    for field, stride in (("k_stride_tok", 286331200), ("v_stride_dim", 33818656)):  # 15 and 127 of them: past 2^32
+        wide = lay.shape(msa)
+        setattr(wide, field, stride)
+        refused("4 GiB", msa.MSA_ERR_UNSUPPORTED, p=lay.plan(msa, shape=wide))
     with pytest.raises(msa.MsaError, match="multiples of 16"):
         msa.msa_fp8_append(odd, normal(1, lay.rows, 2, 128), normal(2, lay.rows, 2, 128), lay.table, *cache[:4])
 

@@ -125,3 +125,22 @@ def test_refusals():
     with pytest.raises(msa.MsaError, match="past seq_kv_len"):
         msa.msa_plan_window(shape, [1600], [0, 1], [1599], [4], 5, 0, flags=HOST)
     assert msa.msa_plan_window(shape, [0], [0, 0], [], [], 5, 0, flags=HOST).info()["num_work"] == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_blocks_of_4_gib_are_refused(d):
+    """The offsets within a block are 32 bits: (16 - 1) strides of a token and d - 1 of a channel have to fit."""
+    half = 1 << 31  # numbers of 2 bytes
+    for part, last, most in (("k", 15, half - d), ("v", d - 1, half - 16)):
+        for stride, fits in ((most // last // 8 * 8, True), ((most // last // 8 + 1) * 8, False), (1 << 62, False)):
+            shape = msa.make_shape(1, 8, 2, d, 100, 100, 0.1)
+            if part == "k":
+                shape.k_stride_tok = stride
+            else:
+                shape.v_stride_dim = stride
+            if fits:
+                assert msa.msa_plan_window(shape, [1600], [0, 1], [3], [4], 2, 0, flags=HOST).info()["num_work"] == 2
+            else:
+                with pytest.raises(msa.MsaError, match="4 GiB") as e:
+                    msa.msa_plan_window(shape, [1600], [0, 1], [3], [4], 2, 0, flags=HOST)
+                assert e.value.status == msa.MSA_ERR_UNSUPPORTED
