@@ -84,12 +84,14 @@ def sizes(plan: Plan):
 
 def rows_of(who: str, name: str, x, rows: int, heads: int, d: int, dev: int):
     """(address, strides by row and head) of bfloat16 rows [rows, heads, d]; an address means contiguous ones."""
-    if type(x) is Tensor and x.dim() == 3:  # (the common case: a few reads, as in tree.py)
+    if type(x) is Tensor and x.dtype in BF16 and x.get_device() == dev and x.dim() == 3:  # (a few reads, as in tree.py)
         n, h, c = x.shape
-        by_row, by_head, by_channel = x.stride()
-        # (what a dimension of one entry says of its stride does not matter)
-        if c == d and h == heads and n >= rows and by_channel == 1 and x.get_device() == dev and x.dtype in BF16:
-            return x.data_ptr(), by_row if n > 1 else heads * d, by_head if h > 1 else d
+        if c == d and h == heads and n >= rows:
+            if x.is_contiguous():
+                return x.data_ptr(), h * d, d
+            by_row, by_head, by_channel = x.stride()
+            if by_channel == 1:  # (what a dimension of one entry says of its stride does not matter)
+                return x.data_ptr(), by_row if n > 1 else h * d, by_head if h > 1 else d
     if x is None or type(x) is int or not hasattr(x, "stride"):
         return _addr(x), heads * d, d
     if x.dtype not in BF16 or x.get_device() != dev or not x.is_cuda:
@@ -121,8 +123,12 @@ def msa_rope_append(plan: Plan, rope: msa_rope, q, q_out, k_new, v_new, block_ta
     rows, hq, hkv, d, entries, powers = sizes(plan)
     if type(rope) is not msa_rope:
         raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: rope is not an msa_rope")
-    if getattr(rope, "device", dev) != dev:
-        raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: rope's frequencies are on device {rope.device}, the current device "
+    try:
+        on, at = rope.device, rope.address
+    except AttributeError:  # (not of make_rope)
+        on, at = dev, ctypes.addressof(rope)
+    if on != dev:
+        raise MsaError(MSA_ERR_INVALID_ARG, f"{who}: rope's frequencies are on device {on}, the current device "
                                             f"is {dev}")
     qa, qt, qh = rows_of(who, "q", q, rows, hq, d, dev)
     oa, ot, oh = rows_of(who, "q_out", q_out, rows, hq, d, dev)
@@ -135,7 +141,6 @@ def msa_rope_append(plan: Plan, rope: msa_rope, q, q_out, k_new, v_new, block_ta
         kc, vc = bytes_address(who, "k_cache", k_cache, dev), bytes_address(who, "v_cache", v_cache, dev)
         ks = address(who, "k_scale", k_scale, UINT8, powers, dev)
         vs = address(who, "v_scale", v_scale, UINT8, powers, dev)
-    _check(_lib.msa_rope_append(plan.handle, getattr(rope, "address", None) or ctypes.addressof(rope), qa, qt, qh, oa, ot,
-                                oh, ka, va, kt, kh, vt, vh,
+    _check(_lib.msa_rope_append(plan.handle, at, qa, qt, qh, oa, ot, oh, ka, va, kt, kh, vt, vh,
                                 None if positions is None else address(who, "positions", positions, INT32, rows, dev),
                                 address(who, "block_table", block_table, INT32, entries, dev), kc, vc, ks, vs, stream))
