@@ -11,8 +11,8 @@
  * msa_rope_append, msa_fp8_append, msa_check_block_table, msa_plan_info, whose figures
  * count visible pairs and keys, msa_plan_export), but for msa_kv_weights, which
  * refuses one that hides keys.  A model whose layers differ has a plan for each kind.
- * Rows of up to 128 keys (window + sinks) carry their weights as with
- * MSA_PLAN_PRECISE_WEIGHTS, as causal rows of up to 64 do.
+ * Where window + sinks <= 128, all rows carry their weights as with
+ * MSA_PLAN_PRECISE_WEIGHTS, as causal rows of up to 64 keys do.
  *
  * Blocks that are out of every window can be given to other sequences: of
  * sequence b, with its first and last query positions f and l, the kernels read
@@ -35,7 +35,8 @@ extern "C" {
 /*
  * msa_plan_window: msa_plan for rows that see a window and sinks.
  *
- *   window  >= 1; where it hides nothing from any row, the plan is msa_plan's
+ *   window  >= 1; where it hides nothing from any row, the plan is msa_plan's (with
+ *           MSA_PLAN_PRECISE_WEIGHTS where window + sinks <= 128)
  *   sinks   >= 0
  *
  * The other arguments and the statuses are those of msa_plan; MSA_ERR_UNSUPPORTED also where a

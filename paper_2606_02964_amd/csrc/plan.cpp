@@ -381,6 +381,12 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
         for (int32_t t = 0; t < seg_len[k]; ++t) P.row_pos[(size_t)r++] = seg_start[k] + t;
   }
   if (window > 0) {
+    // Rows of few keys carry all their weights as hi + lo terms.  A causal row of up to 64 does anyway, as
+    // they are in the step that holds its own position, but a window's keys start in the step before, and
+    // sinks are in another: with two keys, half the weight would be off by 2^-9.  Past 128 keys at
+    // least 64 share what is rounded, as in longer causal rows.  (By the caller's numbers alone, also where
+    // no row has a hidden key: a row's terms do not depend on how long the batch's other sequences are.)
+    if ((int64_t)window + sinks <= kFewKeys) P.precise_weights = true;
     int32_t top = 1;  // the most positions that a row has up to its own
     for (int32_t b = 0; b < B; ++b) top = std::max(top, seq_maxpos[b] + 1);
     if (window >= top) window = 0;  // nothing is hidden: a causal plan
@@ -388,11 +394,6 @@ msa_status build_plan(const msa_shape* shape, const int32_t* seq_kv_len, const i
   if (window > 0) {
     P.window = window;
     P.sinks = sinks = std::min(sinks, *std::max_element(seq_maxpos.begin(), seq_maxpos.end()) + 1);  // (sums stay within 32 bits)
-    // Rows of few keys carry all their weights as hi + lo terms.  A causal row of up to 64 does anyway, as
-    // they are in the step that holds its own position, but a window's keys start in the step before, and
-    // sinks are in another: with two keys, half the weight would be off by 2^-9.  Past 128 keys at
-    // least 64 share what is rounded, as in longer causal rows.
-    if ((int64_t)window + sinks <= kFewKeys) P.precise_weights = true;
   }
   P.seq_row0.assign(seq_row0.begin(), seq_row0.end());
   P.has_trees = with_trees;
