@@ -14,10 +14,11 @@
  * Where window + sinks <= 128, all rows carry their weights as with
  * MSA_PLAN_PRECISE_WEIGHTS, as causal rows of up to 64 keys do.
  *
- * Blocks that are out of every window can be given to other sequences: of
- * sequence b, with its first and last query positions f and l, the kernels read
- * the table entries of the blocks that hold a position in
- * [max(0, f - window + 1), l] or below min(sinks, l + 1), and no others.
+ * Blocks before the window of a sequence's first row, but for the sinks', can be given to
+ * other sequences: of sequence b, with its first and last query positions f and l, the kernels
+ * read the table entries of the blocks that hold a position in
+ * [max(0, f - window + 1), l] or below min(sinks, l + 1), and no others.  (Blocks between its
+ * segments are read also where no row sees them: one tile may hold rows of both sides.)
  * Positions in those blocks that a row does not see are multiplied by 0: their V must be finite.
  */
 #ifndef MSA_WINDOW_H_

@@ -51,8 +51,8 @@
 // are; only the masked steps begin at the tree's first slot, where a row's
 // few latest keys may be spread over several steps, all with hi + lo terms.
 // Windows (WindowAttnParams): a row sees its latest positions and the first few.
-// A tile's keys then lie on an axis that leaves out what none of its rows sees
-// (KeyAxis), a work item's key range counts along it, and steps that hold a window's
+// A tile's keys then lie on an axis that leaves out what lies between the sinks and
+// its first row's window (WindowAxis), a work item's key range counts along it, and steps that hold a window's
 // start or a part of the sinks are masked too; they come first, and run without overlap.
 // Both kernels also come in a precise-weights form (kPrecise, selected by
 // the plan): every step, or half-step, carries every row's weights as
