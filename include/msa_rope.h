@@ -43,8 +43,9 @@ typedef struct msa_rope {
 
 /* How the frequencies f_i = base^(-2 i / rotary_dim) are stretched for contexts
  * `factor` times as long as the ones trained on (original_len positions): */
-#define MSA_ROPE_SCALE_NONE 0   /* f_i */
-#define MSA_ROPE_SCALE_LINEAR 1 /* f_i / factor */
+#define MSA_ROPE_SCALE_NONE 0 /* f_i */
+/* f_i / factor */
+#define MSA_ROPE_SCALE_LINEAR 1
 /* base * factor^(rotary_dim / (rotary_dim - 2)) in place of base (rotary_dim > 2): the slowest
  * frequency is divided by factor, the fastest stays */
 #define MSA_ROPE_SCALE_BASE 2
@@ -53,7 +54,9 @@ typedef struct msa_rope {
  * turns, 0 <= low < high) */
 #define MSA_ROPE_SCALE_TURNS 3
 /* the same mixture, s falling evenly by pair from the pair that makes `high` turns (rounded down)
- * to the one that makes `low` turns (rounded up); the amplitude is 0.1 ln(factor) + 1 */
+ * to the one that makes `low` turns (rounded up), both taken within 0 .. rotary_dim - 1 (where that
+ * makes them the same pair, it keeps its frequency and those behind it are divided); the amplitude is
+ * 0.1 ln(factor) + 1 for factors above 1, else 1 */
 #define MSA_ROPE_SCALE_PAIRS 4
 
 typedef struct msa_rope_scaling {

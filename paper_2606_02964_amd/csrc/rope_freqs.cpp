@@ -51,6 +51,8 @@ extern "C" msa_status msa_rope_freqs(const msa_rope_scaling* scaling, int32_t ro
     keep = std::fmin(std::fmax(keep, 0.0), 1.0);
     inv_freq[i] = keep == 1.0 ? f : keep * f + (1.0 - keep) * (f / s.factor);
   }
-  if (amplitude) *amplitude = s.kind == MSA_ROPE_SCALE_PAIRS ? (float)(0.1 * std::log(s.factor) + 1.0) : 1.0f;
+  // (contexts that are not stretched keep their scores: the logarithm would lower them, below factor e^-10 past 0)
+  const bool raised = s.kind == MSA_ROPE_SCALE_PAIRS && s.factor > 1.0;
+  if (amplitude) *amplitude = raised ? (float)(0.1 * std::log(s.factor) + 1.0) : 1.0f;
   return MSA_OK;
 }
