@@ -44,19 +44,19 @@ typedef struct msa_rope {
 /* How the frequencies f_i = base^(-2 i / rotary_dim) are stretched for contexts
  * `factor` times as long as the ones trained on (original_len positions): */
 #define MSA_ROPE_SCALE_NONE 0 /* f_i */
-/* f_i / factor */
+/* f_i / factor ("position interpolation") */
 #define MSA_ROPE_SCALE_LINEAR 1
 /* base * factor^(rotary_dim / (rotary_dim - 2)) in place of base (rotary_dim > 2): the slowest
- * frequency is divided by factor, the fastest stays */
+ * frequency is divided by factor, the fastest stays ("NTK-aware" scaling of the base) */
 #define MSA_ROPE_SCALE_BASE 2
 /* by the turns n_i = original_len * f_i / (2 pi) that a pair makes over the original context:
  * s f_i + (1 - s) f_i / factor, s = (n_i - low) / (high - low) within [0, 1] (`low` and `high`
- * turns, 0 <= low < high) */
+ * turns, 0 <= low < high; "NTK by parts", with low and high frequency factors) */
 #define MSA_ROPE_SCALE_TURNS 3
 /* the same mixture, s falling evenly by pair from the pair that makes `high` turns (rounded down)
  * to the one that makes `low` turns (rounded up), both taken within 0 .. rotary_dim - 1 (where that
  * makes them the same pair, it keeps its frequency and those behind it are divided); the amplitude is
- * 0.1 ln(factor) + 1 for factors above 1, else 1 */
+ * 0.1 ln(factor) + 1 for factors above 1, else 1 ("YaRN"; `high` its beta_fast, `low` its beta_slow) */
 #define MSA_ROPE_SCALE_PAIRS 4
 
 typedef struct msa_rope_scaling {
@@ -74,7 +74,7 @@ typedef struct msa_rope_scaling {
  *   inv_freq   host [rotary_dim / 2] output
  *   amplitude  host output, or NULL
  *
- * rotary_dim even and >= 2, and > 2 for kind BASE; base > 1 for kind PAIRS.
+ * rotary_dim even and >= 2, and > 2 for kind BASE; base > 1 and low > 0 for kind PAIRS.
  * MSA_ERR_INVALID_ARG otherwise, or for other arguments that are not as above.
  */
 msa_status msa_rope_freqs(const msa_rope_scaling *scaling, int32_t rotary_dim, double *inv_freq,
