@@ -11,12 +11,14 @@
  *
  * s - 127 is the smallest whole number e >= -110 with max_c |x_c| <= 448 * 2^e, so
  * no number is cut off and each is rounded once, to the nearest e4m3 (ties to even):
- * relative to its value by at most 2^-4, down to 2^-14 of its row's largest, absolutely
- * below.  (A power of two leaves every stored value a bf16 number, so reading back and the
+ * relative to its value by at most 2^-4, down to 2^-13 of its row's largest (if that is 2^-102 or more),
+ * by at most 2^-10 * 2^e below.  (A power of two leaves every stored value a bf16 number, so reading back and the
  * matrix products are exact; a scale of more bits would gain no relative precision.)
- * Values that are written must be finite.
+ * Values that are written (of K: as they are rotated) must be finite and below 248 * 2^120 (3.29e38)
+ * in magnitude: from there on the nearest stored value is 2^128, which no bf16 or 32-bit number holds, and
+ * which is read as an infinity.
  *
- * d = 128, 8 KV heads: 2080 bytes a token where bf16 takes 4096.
+ * d = 128, 8 KV heads: 2064 bytes a token where bf16 takes 4096.
  * Statuses, the block table and ownership are those of msa.h; the shape's cache
  * strides must be multiples of 16.
  */
