@@ -394,10 +394,10 @@ msa_status msa_check_block_table(msa_plan_t plan, const int32_t* block_table, in
     for (int32_t i = 0; i < hp.seq_blocks[(size_t)b]; ++i) {
       if (i >= sink_blocks && i < first_block) continue;
       if (row[i] < 0 || row[i] >= s.num_blocks)
-          return set_error(MSA_ERR_INVALID_ARG,
+        return set_error(MSA_ERR_INVALID_ARG,
                          "msa_check_block_table: sequence " + std::to_string(b) + ", logical block " +
-                               std::to_string(i) + " maps to physical block " + std::to_string(row[i]) +
-                               ", outside [0, " + std::to_string(s.num_blocks) + ")");
+                             std::to_string(i) + " maps to physical block " + std::to_string(row[i]) +
+                             ", outside [0, " + std::to_string(s.num_blocks) + ")");
     }
   }
   return MSA_OK;

@@ -3,12 +3,17 @@
 //
 // The four waves of a workgroup hold the same rows and take 32-key half-steps in
 // turn.  A wave copies its half-steps' pages into LDS of its own, two stages of 8 KB (in
-// the area that its partial output takes at the end): every copy takes whole cache lines, so they can be
+// the area that its partial output takes at the end).  Where a (block, KV head) lies together, as in the layout
+// that make_shape gives, every copy takes whole cache lines, so they can be
 // non-temporal, which the caches' lines read in parts cannot.  64 rows over 8000 keys, 32 query
 // heads on 8, d = 128: 164 us, 6.5 TB/s, where operands read straight into registers took 181 and these
 // copies without the hint 182 (bf16 350); 8 rows 26.5 (29.4, bf16 51.0); one over 120000 keys 47
-// (54.5), over 30000 18.0 with its merge (19.2, bf16 28.3).  Sequences that share all their blocks
-// lose up to 10% at d = 64 (16 over 30000 keys, 16 heads: 115 -> 127) and nothing at d = 128.
+// (54.5), over 30000 18.0 with its merge (19.2, bf16 28.3); 48 rows with a window of 4096 keys 70.5 (without the
+// hint 76.7; bf16 129).  The hint costs, us with / without, where sequences share all their blocks (16 over 30000
+// keys, 16 heads of 64: 130 / 120; at d = 128 nothing), one short row (a window of 4096 keys: 11.2 / 10.6), and with
+// strides that put several heads into a line (a token's and a channel's heads side by side), which take
+// four times as long either way (64 over 8000, 8 heads of 128: 703 / 700, 16 of 64 790 / 745; windows of 4096 keys 302 /
+// 250, 319 / 283, in bf16 326 / 281), most of all if their blocks are shared (520 / 191).
 //   * QK: lane half hl holds channels 32 i + 16 hl .. + 15 of its key (and of Q): a
 //     product does not mind the order of its terms, and a read from LDS is 16 bytes.  A key's
 //     power of two goes into the conversion to bf16, which is exact.

@@ -41,8 +41,8 @@
 // before a diagonal step) run the same operations without overlap.
 // msa_decode: 32-row tiles of decode-like plans and 32-row items of plans with
 // few short tiles; the four waves of a workgroup split the tile's keys, read K
-// and V straight into registers and merge their softmax states through LDS
-// (see the kernel); the half-steps of a row's diagonal step carry its weights
+// and V straight into registers (with a window by way of LDS) and merge their
+// softmax states through LDS (see the kernel); the half-steps of a row's diagonal step carry its weights
 // as hi + lo terms, as above.
 // Both kernels' items also serve trees of drafted tokens (TreeAttnParams): a
 // tree's row sees the context before its tree and, of the tree's slots up to
@@ -53,7 +53,8 @@
 // Windows (WindowAttnParams): a row sees its latest positions and the first few.
 // A tile's keys then lie on an axis that leaves out what lies between the sinks and
 // its first row's window (WindowAxis), a work item's key range counts along it, and steps that hold a window's
-// start or a part of the sinks are masked too; they come first, and run without overlap.
+// start or a part of the sinks are masked too.  They come first, and run in the pipelined loop, masked behind the
+// step that takes their scores (mask_window); with precise weights they run without overlap.
 // Both kernels also come in a precise-weights form (kPrecise, selected by
 // the plan): every step, or half-step, carries every row's weights as
 // hi + lo terms.
@@ -1188,7 +1189,8 @@ template <int D, bool kPrecise, class P>
 __device__ __forceinline__ void decode_item(const P& p, const WorkItem w, DecodeLds<D>& lds) {
   constexpr bool kTree = P::kTree;
   // With a window, K and V of a half-step come by way of LDS (the wave's part of the merge area), as in
-  // decode8_item: copies of whole cache lines, which may be non-temporal.  They are read into registers at once,
+  // decode8_item: copies of whole cache lines, where a (block, KV head) of the cache lies together, which may be
+  // non-temporal (what the hint costs with other strides is told there).  They are read into registers at once,
   // and the next half-step's are under way while these are computed.  Registers loaded straight from the caches
   // against this, us: 64 rows with windows of 4096 keys, 32 heads on 8, d = 128: 182 / 163 (6.6 TB/s), of 1024
   // 50.9 / 45.0; 48 with 12000 keys 440 / 378; 64 over the same blocks 110 / 80; a row with 65000 keys 57 / 49;

@@ -64,7 +64,9 @@ constexpr int64_t kWideMinTiles64 = 1024;  // narrow tiles, head_dim 64
 constexpr double kWideMinFill = 0.9;
 // ... and, with a window, the steps of a tile: short tiles' start and end, 8.5 us of a workgroup, run beside
 // another's steps where a CU has two (us, wide / narrow: a prompt of 12000 with 32 heads, windows of 512 keys
-// 168 / 157, 1024 248 / 237, 2048 388 / 393; 4 of 6000, 336 / 322, 475 / 467, 689 / 708)
+// 168 / 157, 1024 248 / 237, 2048 388 / 393; 4 of 6000, 336 / 322, 475 / 467, 689 / 708).  The plan does not know
+// its cache's type, and chunks end less evenly: 12 of 153 to 298 rows, 64 heads on 8, 2000 keys, 32 steps, take 230 to
+// 244 / 215 in bf16 and 260 to 274 / 265 in 8 bits; the prompt of 12000 with 1024 keys 268 / 277 in 8 bits
 constexpr double kWideMinUnitSteps = 24.0;
 // uneven loads of a plan with a window, in key steps over the mean, up to which nothing is cut: its many short
 // items end nearly together, and partials and their merge launch cost more (us, whole / cut: the prompt of 12000
